@@ -10,7 +10,9 @@ Kinds of case
     kv4      fd_kv4_write + fd_kv4_read: K and V rows into the 4-bit cache and, as the values they stand for,
              out of it again
     attn4    fd_decode_attn_kv4: one query token a sequence over the paged 4-bit cache
-    latent   fd_latent_write + fd_latent_decode_attn: a decode step over a paged cache of latent rows
+    latent   fd_latent_write + fd_latent_decode_attn: a decode step over a paged cache of latent rows (the absorbed form)
+    prompt   fd_latent_prefill_attn: all tokens of a batch of prompts, with the keys and values that the latent rows
+             stand for (the expanded form)
 
 The 4-bit cache.  A group of ``group`` neighbouring elements of a row (128 elements of one token and KV head)
 shares a scale s and a lowest value l, both of the cache's type, and an element is l + s c with a code c of 0 .. 15:
@@ -34,8 +36,6 @@ def listed():
     return [
         # A decode step of a few users: launch latency and nothing else.
         dict(name="tables_b8_step_p16", kind="tables", batch=8, page=16, max_cached=2000, max_new=1, short=False, lens_seed=1),
-        # A decode step of a full serving batch, small pages.
-        dict(name="tables_b512_step_p16", kind="tables", batch=512, page=16, max_cached=4096, max_new=1, short=False, lens_seed=2),
         # Prompts of many requests admitted at once, some of which find no page left: over half a million slots.
         dict(name="tables_b300_prompts_p64", kind="tables", batch=300, page=64, max_cached=500, max_new=4001, short=True, lens_seed=3),
         # The rows of one decode step.
@@ -51,9 +51,6 @@ def listed():
         # Grouped heads at a full serving batch.
         dict(name="attn4_b32_gqa64x8_4k_bf16", kind="attn4", batch=32, hq=64, hkv=8, min_len=4096, max_len=4096, page=64, group=64,
              dtype="bf16", lens_seed=6),
-        # Long documents, one group a row.
-        dict(name="attn4_b4_gqa28x4_32k_bf16", kind="attn4", batch=4, hq=28, hkv=4, min_len=30001, max_len=32768, page=256, group=128,
-             dtype="bf16", lens_seed=7),
         # Latent attention: one user, the heads of one of eight GPUs.
         dict(name="latent_b1_h16_2k_bf16", kind="latent", batch=1, heads=16, min_len=2001, max_len=2001, page=64, dtype="bf16", lens_seed=8),
         # A few long ragged sequences.
@@ -62,6 +59,10 @@ def listed():
         # A serving batch with all heads on one GPU: as much arithmetic as memory traffic.
         dict(name="latent_b64_h128_4k_bf16", kind="latent", batch=64, heads=128, min_len=4096, max_len=4096, page=64, dtype="bf16",
              lens_seed=10),
+        # A batch of ordinary prompts, the heads of one of eight GPUs.
+        dict(name="prompt_b3_h16_ragged1k_bf16", kind="prompt", batch=3, heads=16, min_len=150, max_len=1000, dtype="bf16", lens_seed=11),
+        # One long prompt of an odd length.
+        dict(name="prompt_b1_h64_4001_fp16", kind="prompt", batch=1, heads=64, min_len=4001, max_len=4001, dtype="fp16", lens_seed=12),
     ]
 
 
@@ -70,7 +71,7 @@ def _log(rng, lo, hi):
 
 
 def draw(rng):
-    kind = rng.choice(["tables", "kv4", "attn4", "attn4", "latent", "latent"])
+    kind = rng.choice(["tables", "kv4", "attn4", "attn4", "latent", "latent", "prompt"])
     seed, page = rng.randrange(1 << 20), rng.choice([16, 32, 64, 128, 256])
     dtype = rng.choice(["fp16", "bf16"])
     if kind == "tables":
@@ -88,6 +89,11 @@ def draw(rng):
         return dict(kind=kind, batch=batch, hq=hq, hkv=hkv, min_len=max(1, max_len // rng.choice([1, 2, 8])), max_len=max_len, page=page,
                     group=rng.choice([32, 64, 128]), dtype=dtype, lens_seed=seed)
     heads = rng.choice([8, 16, 20, 32, 40, 64, 128])
+    if kind == "prompt":
+        max_len = _log(rng, 1, 5000)
+        batch = _log(rng, 1, max(1, min(16, 64 * 4001 ** 2 // (heads * max_len ** 2))))
+        heads = min(heads, max(1, 64 * 4001 ** 2 // (batch * max_len ** 2)))
+        return dict(kind=kind, batch=batch, heads=heads, min_len=max(1, max_len // rng.choice([1, 2, 8])), max_len=max_len, dtype=dtype, lens_seed=seed)
     max_len = _log(rng, 1, 32768)
     batch = _log(rng, 1, max(1, min(128, 64 * 4096 * 128 // (max_len * max(heads, 64)))))
     return dict(kind=kind, batch=batch, heads=heads, min_len=max(1, max_len // rng.choice([1, 2, 8])), max_len=max_len, page=page,
@@ -124,7 +130,7 @@ def prepare(case, seed):
         return torch.randperm(n_pages, generator=g, device=dev)[:batch * width].to(torch.int32).view(batch, width)
 
     s = dict(case)
-    kind, page = case["kind"], case["page"]
+    kind, page = case["kind"], case.get("page")
     if kind == "tables":
         cached, new, n_free = _step(case)
         batch, width = case["batch"], -(-(case["max_cached"] + case["max_new"]) // page)
@@ -154,7 +160,14 @@ def prepare(case, seed):
         pool = [x.view(n_pages, hkv, page, 2, per_row // 2) if x.dtype == dtype else x for x in pool]
         return dict(s, n_pages=n_pages, k=fused[:, 2 * hkv:3 * hkv], v=fused[:, 3 * hkv:], slots=slots, pool=pool,
                     k_back=torch.zeros(tokens, hkv, D, dtype=dtype, device=dev), v_back=torch.zeros(tokens, hkv, D, dtype=dtype, device=dev))
-    batch, width, lens = case["batch"], _width(case), _lens(case).to(dev)
+    batch, lens = case["batch"], _lens(case).to(dev)
+    if kind == "prompt":
+        # token-major, as projections leave them: a head's query 128 + 64 elements, its key's 128 and value's 128 side by side, the
+        # rotary part of the keys, which all heads share, at the end of the latent rows
+        heads, n = case["heads"], case["max_len"]
+        return dict(s, lens=lens, q=randn(batch, n, heads, D + ROPE, dtype=dtype), kv=randn(batch, n, heads, 2 * D, dtype=dtype),
+                    rows=randn(batch, n, LATENT + ROPE, dtype=dtype), out=torch.empty(batch, n, heads, D, dtype=dtype, device=dev))
+    width = _width(case)
     n_pages = batch * width + 3
     table = table_of(batch, width, n_pages)
     if kind == "attn4":
@@ -278,6 +291,19 @@ def _plain_latent(s):
     return [s["out"], s["rows"]]
 
 
+def _plain_prompt(s):
+    n = s["max_len"]
+    at = torch.arange(n, device=s["q"].device)
+    hidden = at[None, :] > at[:, None]
+    k = torch.cat([s["kv"][..., :D], s["rows"][:, :, None, LATENT:].expand(-1, -1, s["heads"], -1)], -1).float().permute(0, 2, 3, 1)
+    x = torch.matmul(s["q"].float().transpose(1, 2), k).mul_(_latent_scale()).masked_fill_(hidden, -math.inf)
+    x = x.sub_(x.amax(-1, keepdim=True)).exp_()
+    x = x.div_(x.sum(-1, keepdim=True))
+    o = torch.matmul(x, s["kv"][..., D:].float().transpose(1, 2)).transpose(1, 2)
+    s["out"].copy_(torch.where((at[None, :] < s["lens"][:, None])[:, :, None, None], o, 0.0))
+    return [s["out"]]
+
+
 def _latent_scale():
     return 1 / math.sqrt(D + ROPE)          # of the heads that the latent rows stand for: 128 elements and the rotary ones
 
@@ -287,13 +313,19 @@ def _latent_scale():
 def _own(s):
     from paper_2311_01282_amd import fdattn as fd
     stream = torch.cuda.current_stream().cuda_stream
-    kind, page = s["kind"], s["page"]
+    kind, page = s["kind"], s.get("page")
     if kind == "tables":
         fd.fd_page_tables(s["batch"], page, s["n_pages"], s["width"], s["max_tokens"], s["cached"].data_ptr(), s["new"].data_ptr(),
                           s["free"].data_ptr(), s["n_free"].data_ptr(), s["table"].data_ptr(), s["seq_lens"].data_ptr(),
                           s["starts"].data_ptr(), s["slots"].data_ptr(), s["n_left"].data_ptr(), stream)
         return [s["table"], s["seq_lens"], s["starts"], s["slots"], s["n_left"]]
     dtype = fd.FD_F16 if s["dtype"] == "fp16" else fd.FD_BF16
+    if kind == "prompt":
+        shape = fd.make_shape(s["batch"], s["heads"], s["heads"], D + ROPE, s["max_len"], 0, _latent_scale())
+        rope = s["rows"][..., LATENT:]
+        fd.fd_latent_prefill_attn(shape, dtype, s["q"].data_ptr(), s["kv"].data_ptr(), rope.data_ptr(), rope.stride(1), s["lens"].data_ptr(),
+                                  s["out"].data_ptr(), stream)
+        return [s["out"]]
     if kind == "latent":
         pool = fd.make_latent_pool(s["rows"].data_ptr(), s["n_pages"], page, LATENT, ROPE, dtype)
         fd.fd_latent_write(pool, s["latent"].data_ptr(), s["latent"].stride(0), s["rope"].data_ptr(), s["rope"].stride(0), s["batch"],
@@ -319,7 +351,7 @@ def _own(s):
 def run(state):
     if own:
         return _own(state)
-    return {"tables": _plain_tables, "kv4": _plain_kv4, "attn4": _plain_attn4, "latent": _plain_latent}[state["kind"]](state)
+    return {"tables": _plain_tables, "kv4": _plain_kv4, "attn4": _plain_attn4, "latent": _plain_latent, "prompt": _plain_prompt}[state["kind"]](state)
 
 
 def work(case):
@@ -336,6 +368,10 @@ def work(case):
         coded = 64 + 2 * 2 * (D // case["group"])
         return {"bytes": rows * (4 * D + 2 * coded) + 8 * case["tokens"], "flops": 8 * rows * D}
     keys, batch = int(_lens(case).sum()), case["batch"]
+    if kind == "prompt":
+        pairs = sum(n * (n + 1) // 2 for n in _lens(case).tolist())
+        return {"bytes": 2 * keys * (case["heads"] * (D + ROPE + 2 * D) + ROPE) + 2 * batch * case["max_len"] * case["heads"] * D + 4 * batch,
+                "flops": 2 * (2 * D + ROPE) * pairs * case["heads"]}
     table = 4 * batch + 4 * int(((_lens(case) + case["page"] - 1) // case["page"]).sum())
     if kind == "attn4":
         row = 64 + 2 * 2 * (D // case["group"])
@@ -353,8 +389,8 @@ def exact(case, seed):
     if kind == "tables":
         return None
     s = prepare(case, seed)
-    page = case["page"]
-    dev = s["table"].device if "table" in s else s["slots"].device
+    page = case.get("page")
+    dev = torch.device("cuda:0")
     element = torch.arange(D, device=dev)
     # byte and half of a byte that hold element d of a K row and of a V row
     word_k = 4 * ((element % 32) // 8) + element // 32
@@ -388,6 +424,15 @@ def exact(case, seed):
                 rows.append(torch.softmax(x, -1) @ v)
             out.append(torch.cat(rows))
         return [torch.stack(out)]
+    if kind == "prompt":
+        out = torch.zeros(case["batch"], case["max_len"], case["heads"], D, dtype=torch.float64, device=dev)
+        for b, n in enumerate(lens):
+            below = torch.ones(n, n, dtype=torch.bool, device=dev).tril()
+            for h in range(case["heads"]):
+                q, kv = s["q"][b, :n, h].double(), s["kv"][b, :n, h].double()
+                x = (q[:, :D] @ kv[:, :D].t() + q[:, D:] @ s["rows"][b, :n, LATENT:].double().t()) / (D + ROPE) ** 0.5
+                out[b, :n, h] = torch.softmax(torch.where(below, x, -math.inf), -1) @ kv[:, D:]
+        return [out]
     for b, n in enumerate(lens):
         c = s["rows"][s["table"][b, :-(-n // page)].long()].flatten(0, 1)[:n].double()
         c[n - 1, :LATENT], c[n - 1, LATENT:] = s["latent"][b].double(), s["rope"][b].double()
