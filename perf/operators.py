@@ -7,9 +7,9 @@ torch operations in 32 bits where it is not), ``exact`` the same result from the
 
 Kinds of case
     tables   fd_page_tables: pages for a step's new tokens, the block table, the slot of every token
-    kv4      fd_kv4_write + fd_kv4_read: K and V rows into the 4-bit cache and, as the values they stand for,
+    kv4      fd_nibble_write + fd_nibble_read: K and V rows into the 4-bit cache and, as the values they stand for,
              out of it again
-    attn4    fd_decode_attn_kv4: one query token a sequence over the paged 4-bit cache
+    attn4    fd_decode_attn_nibble: one query token a sequence over the paged 4-bit cache
     latent   fd_latent_write + fd_latent_decode_attn: a decode step over a paged cache of latent rows (the absorbed form)
     prompt   fd_latent_prefill_attn: all tokens of a batch of prompts, with the keys and values that the latent rows
              stand for (the expanded form)
@@ -335,15 +335,15 @@ def _own(s):
         fd.fd_latent_decode_attn(shape, pool, s["q_latent"].data_ptr(), s["q_rope"].data_ptr(), s["table"].data_ptr(), s["lens"].data_ptr(),
                                  s["out"].data_ptr(), s["ws"].data_ptr(), s["ws"].numel(), stream)
         return [s["out"], s["rows"]]
-    pool = fd.make_kv4_pool(*[x.data_ptr() for x in s["pool"]], s["n_pages"], page, s["hkv"], D, s["group"], dtype)
+    pool = fd.make_nibble_pool(*[x.data_ptr() for x in s["pool"]], s["n_pages"], page, s["hkv"], D, s["group"], dtype)
     if kind == "kv4":
-        fd.fd_kv4_write(pool, s["k"].data_ptr(), s["k"].stride(0), s["v"].data_ptr(), s["v"].stride(0), s["tokens"], s["slots"].data_ptr(), stream)
-        fd.fd_kv4_read(pool, s["slots"].data_ptr(), s["tokens"], s["k_back"].data_ptr(), s["k_back"].stride(0), s["v_back"].data_ptr(),
+        fd.fd_nibble_write(pool, s["k"].data_ptr(), s["k"].stride(0), s["v"].data_ptr(), s["v"].stride(0), s["tokens"], s["slots"].data_ptr(), stream)
+        fd.fd_nibble_read(pool, s["slots"].data_ptr(), s["tokens"], s["k_back"].data_ptr(), s["k_back"].stride(0), s["v_back"].data_ptr(),
                        s["v_back"].stride(0), stream)
         return [s["k_back"], s["v_back"]]
     shape = fd.make_shape(s["batch"], s["hq"], s["hkv"], D, s["width"] * page, 0, 1 / math.sqrt(D))
-    shape.chunk = fd.fd_kv4_pick_chunk(shape)
-    fd.fd_decode_attn_kv4(shape, pool, s["q"].data_ptr(), s["table"].data_ptr(), s["lens"].data_ptr(), s["out"].data_ptr(),
+    shape.chunk = fd.fd_nibble_pick_chunk(shape)
+    fd.fd_decode_attn_nibble(shape, pool, s["q"].data_ptr(), s["table"].data_ptr(), s["lens"].data_ptr(), s["out"].data_ptr(),
                           s["ws"].data_ptr(), s["ws"].numel(), stream)
     return [s["out"]]
 
