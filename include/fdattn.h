@@ -473,6 +473,127 @@ fd_status fd_prefill_attn(const fd_shape *shape, const void *q, const void *k_ca
  * the guard fired for a logit of those 64 queries (the tile they are in was recomputed). */
 fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uint8_t **tile_flags);
 
+/* ---- Smaller paged caches: page tables, a 4-bit cache, latent attention ----
+ *
+ * What a serving step over a paged cache needs besides fp16 attention: pages and slots for the step's
+ * tokens (fd_page_tables), a cache in 4 bits with the calls that fill, read and attend over it (fd_nibble_*,
+ * fd_decode_attn_nibble), and a cache of latent rows with its attention (fd_latent_*).  All of them take
+ * fp16 or bf16.  The softmax is the synchronized one (a running maximum): no phi, no bounds, no flags.
+ *   Slots.  Slot s of a pool is row s % page_size of page s / page_size; page_size is a power of two >= 16
+ *     and n_pages * page_size < 2^31.  A slot outside [0, n_pages * page_size), -1 for example, is padding: its
+ *     token is skipped.  The slots of one call that are no padding have to differ from each other.
+ *   Block tables.  As fd_decode_attn_paged: [batch, max_seq / page_size], max_seq a multiple of page_size; entries of pages
+ *     without a valid token are not followed, an entry in use that is out of range is the caller's error (it is
+ *     clamped and reads the wrong page).
+ *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
+ * Memory, stream, errors and threads: as stated at the top.  Nothing here needs an initialisation call; a workspace
+ * may hold anything before a call and serves one call at a time.                                              */
+typedef enum { FD_F16 = 0, FD_BF16 = 1 } fd_dtype;
+
+/*
+ * Pages for a step's new tokens, the block table and the slot of every token, on the GPU from the lengths alone.
+ * Request b has cached_lens[b] tokens in the cache (clamped to [0, pages_per_seq * page_size]) and new_lens[b] to come
+ * (negative: 0).  It holds its first ceil(cached / page_size) table entries and needs ceil((cached + new) / page_size);
+ * the missing pages are taken from the END of the list free_pages[0 .. *n_free - 1], in the order of the requests and,
+ * within one, of its tokens.
+ *   Served: cached + new fits the table's width, the new tokens up to and including this request's number at most
+ *     max_tokens, and the request needs no page or the list covers its pages and those of all requests in front of it that
+ *     the first two conditions pass.  Any other request takes no page and keeps its length; its tokens get slot -1.
+ *   block_table  [batch, pages_per_seq], in and out: entries of pages taken are written, all others left as they are
+ *   seq_lens     [batch] out: cached + new where served, cached where not (the caller's sign of a refusal)
+ *   token_starts [batch + 1] out: the new tokens of request b are token_starts[b] .. token_starts[b + 1] - 1 of the
+ *                step's tokens, whether it is served or not (values stop at max_tokens)
+ *   slot_map     [max_tokens] out: slot of each token; -1 for tokens of requests that are not served, for tokens whose
+ *                page (a table entry held before) is out of range, and behind the last token
+ *   n_left       [1] out: pages still in the list, free_pages[0 .. *n_left - 1]
+ * free_pages has room for n_pages entries; *n_free (device) is clamped to [0, n_pages].  Outputs must not overlap inputs or one
+ * another.  pages_per_seq * page_size and n_pages * page_size < 2^31, max_tokens <= 2^30.  Pointers 4-byte aligned.  One launch.
+ */
+fd_status fd_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int32_t pages_per_seq, int32_t max_tokens,
+                         const int32_t *cached_lens, const int32_t *new_lens, const int32_t *free_pages, const int32_t *n_free,
+                         int32_t *block_table, int32_t *seq_lens, int32_t *token_starts, int32_t *slot_map, int32_t *n_left,
+                         void *stream);
+
+/*
+ * A cache in 4 bits.  `group` (32, 64 or 128) neighbouring elements of a row share a scale s and a lowest value l of type
+ * `dtype`; an element stands for l + s c with its code c of 0 .. 15.
+ *   codes  [n_pages, n_kv_heads, page_size, 64] bytes, two codes a byte, the lower half first.  V: element d in place d.  K: the
+ *          row's 16 words of eight codes transposed as a 4 x 4 matrix, elements 32 t + 8 c .. + 7 in word 4 c + t
+ *   scales [n_pages, n_kv_heads, page_size, 2, 128 / group]: all s of a row, then all l
+ * The four pointers 16-byte aligned.  head_dim == 128.
+ */
+typedef struct {
+    void   *k_codes, *k_scales, *v_codes, *v_scales;
+    int32_t n_pages, page_size, n_kv_heads, head_dim, group;
+    int32_t dtype;             /* fd_dtype, also of the rows, queries and outputs  */
+} fd_nibble_pool;
+
+/*
+ * Rows into the cache.  k, v [n_tokens, n_kv_heads, 128], k_stride and v_stride elements from a token to the next (multiples of
+ * 8, at least n_kv_heads * 128; so a fused projection's parts can be given as they are); token t goes to slot slot_map[t].
+ * Per group, in fp32: l = min x; s = (max x - min x) / 15 rounded to dtype; c = (x - l) / s rounded to nearest, ties to even,
+ * limited to 0 .. 15; c = 0 where s is 0.  A group with an infinite element or a NaN reads as NaN, all of it.
+ */
+fd_status fd_nibble_write(const fd_nibble_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
+                       const int32_t *slot_map, void *stream);
+
+/* Rows out of the cache, l + s c rounded to dtype once.  Layouts and slots as fd_nibble_write; rows of padding are left as they are. */
+fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, int32_t n_tokens, void *k, int64_t k_stride, void *v,
+                      int64_t v_stride, void *stream);
+
+/*
+ * Decode attention over the 4-bit cache: out = softmax(scale q K^T) V with the values that the codes stand for (unrounded).
+ * q, out [batch, n_q_heads, 128] of the pool's dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of
+ * 64 from 64 to 16384 keys, for example fd_nibble_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
+ * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of dtype each (22
+ * significant bits in fp16, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch where chunk >= max_seq, else two.
+ */
+size_t    fd_nibble_workspace_bytes(const fd_shape *shape);
+int32_t   fd_nibble_pick_chunk(const fd_shape *shape);
+fd_status fd_decode_attn_nibble(const fd_shape *shape, const fd_nibble_pool *pool, const void *q, const int32_t *block_table,
+                             const int32_t *seq_lens, void *out, fd_workspace ws, void *stream);
+
+/*
+ * A cache of latent rows: one row of latent_dim + rope_dim elements a token (512 + 64, the one pair supported) that all heads share; the
+ * latent part stands for every head's keys and values, the rotary part is a further piece of every key.
+ *   rows [n_pages, page_size, 576] of type dtype, 16-byte aligned.
+ */
+typedef struct {
+    void   *rows;
+    int32_t n_pages, page_size, latent_dim, rope_dim;
+    int32_t dtype;             /* fd_dtype, also of the queries and outputs */
+} fd_latent_pool;
+
+/* Rows into the cache: latent [n_tokens, 512] and rope [n_tokens, 64] with strides of their own (elements, multiples of 8, at least
+ * 512 and 64), token t to slot slot_map[t]. */
+fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_t latent_stride, const void *rope, int64_t rope_stride,
+                          int32_t n_tokens, const int32_t *slot_map, void *stream);
+
+/*
+ * Decode attention in the absorbed form: x_j = scale (q_latent . latent_j + q_rope . rope_j), out = sum_j softmax(x)_j latent_j, the
+ * queries taken into the latent space by the caller, who takes the output out of it.
+ * q_latent, out [batch, n_q_heads, 512], q_rope [batch, n_q_heads, 64].  shape: n_kv_heads 1, head_dim 576; chunk a multiple of 32 from 32 to
+ * 16384 keys, for example fd_latent_pick_chunk(shape).  A sequence of length 0 gives zero rows.
+ */
+size_t    fd_latent_workspace_bytes(const fd_shape *shape);
+int32_t   fd_latent_pick_chunk(const fd_shape *shape);
+fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *pool, const void *q_latent, const void *q_rope,
+                                const int32_t *block_table, const int32_t *seq_lens, void *out, fd_workspace ws, void *stream);
+
+/*
+ * Prompts in the expanded form: every head has its own keys of 128 elements and values of 128, projected from the latent rows by the caller, and
+ * the 64 rotary elements of the keys are shared; token i attends to tokens 0 .. i.
+ *   q    [batch, max_seq, n_q_heads, 192]: 128 elements, then the rotary 64
+ *   kv   [batch, max_seq, n_q_heads, 256]: key, then value
+ *   rope [batch, max_seq, 64], rope_stride elements from a token to the next (a multiple of 8, 64 to 2^24; so the ends of
+ *        latent rows can be given as they are; sequences max_seq rows apart)
+ *   out  [batch, max_seq, n_q_heads, 128]; tokens at and behind seq_lens[b] get zero rows
+ * shape: n_kv_heads == n_q_heads (<= 65535), head_dim 192; chunk is ignored.  No workspace.  Scores and sums in fp32, the weights
+ * rounded to dtype for the second product; the denominator is the sum of the rounded ones.
+ */
+fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const void *q, const void *kv, const void *rope,
+                                 int64_t rope_stride, const int32_t *seq_lens, void *out, void *stream);
+
 /* Static, human-readable name of a status code. */
 const char *fd_status_str(fd_status status);
 

@@ -20,6 +20,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 FD_OK, FD_ERR_NULL, FD_ERR_SHAPE, FD_ERR_BOUNDS, FD_ERR_WORKSPACE, FD_ERR_UNSUPPORTED, FD_ERR_HIP, FD_ERR_STATIC_LIMIT = range(8)
 FD_STATIC_SCRATCH_BYTES = 8 << 20
+FD_F16, FD_BF16 = range(2)
 
 
 class Shape(ctypes.Structure):
@@ -38,6 +39,20 @@ class Bounds(ctypes.Structure):
 class Workspace(ctypes.Structure):
     """fd_workspace"""
     _fields_ = [("ptr", ctypes.c_void_p), ("bytes", ctypes.c_size_t)]
+
+
+class NibblePool(ctypes.Structure):
+    """fd_nibble_pool"""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class LatentPool(ctypes.Structure):
+    """fd_latent_pool"""
+    _fields_ = [("rows", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class FdError(RuntimeError):
@@ -103,6 +118,24 @@ def _bind(lib):
     lib.fd_prefill_attn.argtypes = [_sp, _vp, _vp, _vp, _vp, _f, Bounds, _vp, Workspace, _vp]
     lib.fd_prefill_get_flags.restype = ctypes.c_int
     lib.fd_prefill_get_flags.argtypes = [_sp, Workspace, ctypes.POINTER(_vp)]
+
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    nibble, latent = ctypes.POINTER(NibblePool), ctypes.POINTER(LatentPool)
+    for _name in ("fd_nibble_workspace_bytes", "fd_latent_workspace_bytes"):
+        getattr(lib, _name).restype = ctypes.c_size_t
+        getattr(lib, _name).argtypes = [_sp]
+    for _name in ("fd_nibble_pick_chunk", "fd_latent_pick_chunk"):
+        getattr(lib, _name).restype = ctypes.c_int32
+        getattr(lib, _name).argtypes = [_sp]
+    for _name, _args in (("fd_page_tables", [i32] * 5 + [_vp] * 10),
+                         ("fd_nibble_write", [nibble, _vp, i64, _vp, i64, i32, _vp, _vp]),
+                         ("fd_nibble_read", [nibble, _vp, i32, _vp, i64, _vp, i64, _vp]),
+                         ("fd_decode_attn_nibble", [_sp, nibble, _vp, _vp, _vp, _vp, Workspace, _vp]),
+                         ("fd_latent_write", [latent, _vp, i64, _vp, i64, i32, _vp, _vp]),
+                         ("fd_latent_decode_attn", [_sp, latent, _vp, _vp, _vp, _vp, _vp, Workspace, _vp]),
+                         ("fd_latent_prefill_attn", [_sp, i32, _vp, _vp, _vp, i64, _vp, _vp, _vp])):
+        getattr(lib, _name).restype = ctypes.c_int
+        getattr(lib, _name).argtypes = _args
     return lib
 
 
@@ -111,7 +144,9 @@ _lib = _bind(_lib)
 EXPORTS = ("fd_decode_attn_static", "fd_decode_attn_paged", "fd_decode_attn_paged_append", "fd_prefill_workspace_bytes", "fd_prefill_attn", "fd_prefill_get_flags", "fd_decode_attn_append", "fd_logit_histogram", "fd_calibrate", "fd_workspace_bytes", "fd_pick_chunk", "fd_workspace_init", "fd_decode_attn", "fd_decode_attn_gqa",
            "fd_decode_attn_multikernel", "fd_decode_attn_sync", "fd_list_flagged_rows",
            "fd_decode_attn_partial", "fd_decode_attn_gqa_partial", "fd_get_flags", "fd_get_partials",
-           "fd_status_str")
+           "fd_status_str", "fd_page_tables", "fd_nibble_write", "fd_nibble_read", "fd_nibble_workspace_bytes", "fd_nibble_pick_chunk",
+           "fd_decode_attn_nibble", "fd_latent_write", "fd_latent_workspace_bytes", "fd_latent_pick_chunk", "fd_latent_decode_attn",
+           "fd_latent_prefill_attn")
 
 
 def status_str(status):
@@ -241,3 +276,61 @@ def fd_prefill_get_flags(shape, ws_ptr, ws_bytes):
     out = _vp()
     _check(_lib.fd_prefill_get_flags(ctypes.byref(shape), Workspace(ws_ptr, ws_bytes), ctypes.byref(out)))
     return out.value
+
+
+def fd_page_tables(batch, page_size, n_pages, pages_per_seq, max_tokens, cached_lens, new_lens, free_pages, n_free, block_table,
+                   seq_lens, token_starts, slot_map, n_left, stream=0):
+    _check(_lib.fd_page_tables(int(batch), int(page_size), int(n_pages), int(pages_per_seq), int(max_tokens), cached_lens, new_lens,
+                               free_pages, n_free, block_table, seq_lens, token_starts, slot_map, n_left, stream))
+
+
+def make_nibble_pool(k_codes, k_scales, v_codes, v_scales, n_pages, page_size, n_kv_heads, head_dim, group, dtype):
+    return NibblePool(k_codes, k_scales, v_codes, v_scales, int(n_pages), int(page_size), int(n_kv_heads), int(head_dim), int(group),
+                   int(dtype))
+
+
+def fd_nibble_write(pool, k, k_stride, v, v_stride, n_tokens, slot_map, stream=0):
+    _check(_lib.fd_nibble_write(ctypes.byref(pool), k, int(k_stride), v, int(v_stride), int(n_tokens), slot_map, stream))
+
+
+def fd_nibble_read(pool, slot_map, n_tokens, k, k_stride, v, v_stride, stream=0):
+    _check(_lib.fd_nibble_read(ctypes.byref(pool), slot_map, int(n_tokens), k, int(k_stride), v, int(v_stride), stream))
+
+
+def fd_nibble_workspace_bytes(shape):
+    return int(_lib.fd_nibble_workspace_bytes(ctypes.byref(shape)))
+
+
+def fd_nibble_pick_chunk(shape):
+    return int(_lib.fd_nibble_pick_chunk(ctypes.byref(shape)))
+
+
+def fd_decode_attn_nibble(shape, pool, q, block_table, seq_lens, out, ws_ptr, ws_bytes, stream=0):
+    _check(_lib.fd_decode_attn_nibble(ctypes.byref(shape), ctypes.byref(pool), q, block_table, seq_lens, out,
+                                   Workspace(ws_ptr, ws_bytes), stream))
+
+
+def make_latent_pool(rows, n_pages, page_size, latent_dim, rope_dim, dtype):
+    return LatentPool(rows, int(n_pages), int(page_size), int(latent_dim), int(rope_dim), int(dtype))
+
+
+def fd_latent_write(pool, latent, latent_stride, rope, rope_stride, n_tokens, slot_map, stream=0):
+    _check(_lib.fd_latent_write(ctypes.byref(pool), latent, int(latent_stride), rope, int(rope_stride), int(n_tokens), slot_map,
+                                stream))
+
+
+def fd_latent_workspace_bytes(shape):
+    return int(_lib.fd_latent_workspace_bytes(ctypes.byref(shape)))
+
+
+def fd_latent_pick_chunk(shape):
+    return int(_lib.fd_latent_pick_chunk(ctypes.byref(shape)))
+
+
+def fd_latent_decode_attn(shape, pool, q_latent, q_rope, block_table, seq_lens, out, ws_ptr, ws_bytes, stream=0):
+    _check(_lib.fd_latent_decode_attn(ctypes.byref(shape), ctypes.byref(pool), q_latent, q_rope, block_table, seq_lens, out,
+                                      Workspace(ws_ptr, ws_bytes), stream))
+
+
+def fd_latent_prefill_attn(shape, dtype, q, kv, rope, rope_stride, seq_lens, out, stream=0):
+    _check(_lib.fd_latent_prefill_attn(ctypes.byref(shape), int(dtype), q, kv, rope, int(rope_stride), seq_lens, out, stream))
