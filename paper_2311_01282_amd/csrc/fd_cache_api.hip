@@ -241,8 +241,10 @@ size_t fd_latent_workspace_bytes(const fd_shape *shape)
 int32_t fd_latent_pick_chunk(const fd_shape *shape)
 {
     if (check_shape(shape, fd::kLatentRow) != FD_OK || shape->n_kv_heads != 1) return 0;
-    const long long units = (long long)shape->batch * ((shape->n_q_heads + 63) / 64);
-    return chunk_for(shape->max_seq, units, 256, 64, 32);
+    // a workgroup takes up to 64 heads, and two of them fit a compute unit, or, of more than 64, up to 128
+    const bool many = shape->n_q_heads > 64;
+    const long long units = (long long)shape->batch * ((shape->n_q_heads + 127) / 128);
+    return chunk_for(shape->max_seq, units, many ? 256 : 512, 64, 32);
 }
 
 fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *pool, const void *q_latent, const void *q_rope,

@@ -31,28 +31,35 @@ __global__ __launch_bounds__(256) void latent_write_kernel(LatentPool pool, cons
 //   scores   S^T[key][head] = C . Q^T: A = 16 rows of the tile in LDS, B = Q^T in registers for the whole kernel (18 operands).  Row 4 g + r of key
 //            block t is key 8 g + 4 t + r of the tile, so that the two blocks leave lane (n, g) holding keys 8 g .. 8 g + 7 of head n: the B operand of
 //   output   O^T[d][head] = C^T . P^T: A = the same rows, turned round by the transposing LDS read.  32 tiles of 16 elements.
-// The weights enter as the sum of two numbers of the type (hi + lo): one alone adds an error as large as the output's rounding.
-// A workgroup takes 64 heads of a sequence (a wavefront 16) and a chunk of its keys, 32 at a time: tiles of 32 rows, fetched straight into LDS by all four
-// wavefronts, in a ring of four.
-constexpr int kTile = 32, kRing = 4;
-constexpr int kRowBytes = kLatentRow * 2;                      // 1152 = 72 pieces of 16 bytes
-constexpr int kLatentTileBytes = kTile * kRowBytes;            // 36 KiB
-constexpr int kChunkPages = 1026;
+// The weights enter as the sum of two numbers of the type (hi + lo), since one alone adds an error as large as the output's rounding, and the second
+// half of the instructions is hidden behind memory; of more than 64 heads, where the matrix cores are the bound, as one, and their sum is that of the rounded
+// ones (64 x 128 heads x 4096 keys: 106 us with two, 93 with one).
+// A wavefront owns 16 heads: 72 registers of queries and 128 of sums.  A workgroup of NH wavefronts takes 16 NH heads of a sequence and a chunk of its keys,
+// TPW tiles of 32 at a time, which all its wavefronts fetch straight into LDS while they work on those before.
+constexpr int kTile = 32;
+// The reference of a head's weights follows its maximum only where that has grown by more than this (in units of log2): weights are at most 2^8 then, and
+// the sums, 128 registers of a wavefront, are brought to another reference once or twice a chunk; of 16 heads some maximum grows in most tiles.
+constexpr float kSlack = 8.f;
+constexpr int kRowBytes = kLatentRow * 2;                      // in the cache
+constexpr int kCBytes = kLatent * 2, kRBytes = kRope * 2;      // in LDS the two parts of a row lie apart
 
-struct LatentLds {
-    alignas(16) unsigned char rows[kRing][kLatentTileBytes];
-    int pages[kChunkPages];
+template <int TPW> struct LatentLds {
+    alignas(256) unsigned char c[2][TPW * kTile * kCBytes];    // piece x (16 bytes) of row r in place x ^ c_key(r)
+    alignas(256) unsigned char r[2][TPW * kTile * kRBytes];    // ... x ^ r_key(r)
 };
+// A cycle of the 16-byte operand reads holds every n once, from two neighbouring g: with these keys the 16 pieces lie in 16 different places modulo 256 bytes.  The
+// transposing reads take 32 bytes of eight rows at a time, 8 g + 4 h + (0 .. 3) of two neighbouring g: in eight different places.  Rows r and r + 4 have the same keys.
+__device__ __forceinline__ constexpr int c_key(int r) { return ((r & 1) << 1) | (((r >> 1) & 1) << 2) | (((r >> 3) & 1) << 3); }
+__device__ __forceinline__ constexpr int r_key(int r) { return (((r >> 3) & 1) << 1) | (((r >> 1) & 1) << 2); }
 
-// Piece x of row r lies in piece x ^ swizzle(r) of the row.  A cycle of the 16-byte operand reads holds every n once, from two neighbouring g;
-// with rows 128 bytes apart modulo 256 the 16 pieces then lie in 16 different places modulo 256 bytes.  The transposing reads take 32 bytes of eight
-// rows at a time, 8 g + 4 h + (0 .. 3) of two neighbouring g, in eight different places.
-__device__ __forceinline__ int swizzle(int r) { return 2 * ((r >> 3) & 1) + 4 * ((r >> 1) & 1); }
-
-__device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, const unsigned char *lds_1k)
+// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+__device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, int soff, unsigned lds_1k)
 {
-    const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)lds_1k));
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(at), "v"(voff), "s"(rs) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs), "s"(soff) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const void *p)
+{
+    return __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
 }
 template <int N> __device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void tile_barrier()
@@ -63,17 +70,32 @@ __device__ __forceinline__ void tile_barrier()
     asm volatile("" ::: "memory");
 }
 
-template <class T> __global__ __launch_bounds__(256, 1) void latent_decode_kernel(LatentProblem p)
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
+typedef __attribute__((address_space(3))) const u32x4_t *lds_u32x4;
+typedef __attribute__((address_space(4))) const int32_t *scalar_i32;      // read through the scalar cache
+
+template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) void latent_decode_kernel(LatentProblem p)
 {
-    __shared__ LatentLds lds;
+    constexpr bool kTwoParts = NH < 8;                         // of a weight
+    constexpr int kKeys = TPW * kTile, kRows = kKeys / NH;     // keys of a step; rows that a wavefront fetches
+    constexpr int kHalves = (kRows + 15) / 16;                 // ... from so many places of 16 rows
+    __shared__ LatentLds<TPW> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     // workgroups that read the same rows lie on one XCD (index modulo 8), one after the other
-    const int tiles = (p.H + 63) / 64, units = p.B * p.nc;
-    const int unit = (blockIdx.x / (8 * tiles)) * 8 + blockIdx.x % 8, head0 = (blockIdx.x / 8 % tiles) * 64 + 16 * wave;
+    const int tiles = (p.H + 16 * NH - 1) / (16 * NH), units = p.B * p.nc;
+    const int unit = (blockIdx.x / (8 * tiles)) * 8 + blockIdx.x % 8, head0 = (blockIdx.x / 8 % tiles) * (16 * NH) + 16 * wave;
     if (unit >= units) return;
     const int chunk = unit % p.nc, b = unit / p.nc;
-    const int len = min(max(p.seq_lens[b], 0), p.Smax);
-    const int start = chunk * p.C, end = min(len, start + p.C);
+    const int start = chunk * p.C, shift = p.pool.page_shift, mask = (1 << shift) - 1;
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)b * p.width);
+    // page of the 16 rows h of this wavefront in step s (of the last entry, behind the table)
+    auto page_of = [&](int s, int h) { return table[min((start + s * kKeys + wave * kRows + 16 * h) >> shift, p.width - 1)]; };
+    int page[kHalves];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) page[h] = page_of(0, h);
+    const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
+    const int end = min(len, start + p.C);
     const int heads = min(p.H - head0, 16);                    // of this wavefront; may be 0 or less: it only fetches
     if (start >= end) {
         if (p.nc == 1)                                         // no keys at all: zero rows
@@ -81,9 +103,36 @@ template <class T> __global__ __launch_bounds__(256, 1) void latent_decode_kerne
                 reinterpret_cast<u32x4_t *>(p.out + ((size_t)b * p.H + head0 + h) * kLatent)[lane] = u32x4_t{0u, 0u, 0u, 0u};
         return;
     }
-    const int shift = p.pool.page_shift, mask = (1 << shift) - 1, first_page = start >> shift;
-    const int used = ((end - 1) >> shift) - first_page + 1;
-    for (int i = tid; i < used; i += 256) lds.pages[i] = min(max(p.table[(size_t)b * p.width + first_page + i], 0), p.pool.n_pages - 1);
+
+    // Fetches: 1 KiB an instruction, the latent part of a row, or the rotary parts of eight; what lies behind the last key arrives as zeros.
+    const int steps = (end - start + kKeys - 1) / kKeys;
+    const unsigned lds_c = lds_address(lds.c[0]), lds_r = lds_address(lds.r[0]);
+    auto fetch = [&](int s) {
+        int l0 = lane;
+        asm volatile("" : "+v"(l0));    // (offsets are formed anew each time: there are no registers to keep them in)
+        const unsigned to_c = lds_c + (s & 1) * (kKeys * kCBytes) + wave * (kRows * kCBytes), to_r = lds_r + (s & 1) * (kKeys * kRBytes) + wave * (kRows * kRBytes);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+            const int key0 = start + s * kKeys + wave * kRows + 16 * h;
+            const int left = min(max(end - key0, 0), kRows < 16 ? kRows : 16);
+            const int pg = min(max(page[h], 0), p.pool.n_pages - 1);
+            const unsigned long long at = reinterpret_cast<unsigned long long>(p.pool.rows) + (((size_t)pg << shift) + (key0 & mask)) * kRowBytes;
+            const u32x4_t rs = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
+                                (unsigned)__builtin_amdgcn_readfirstlane(left * kRowBytes), 0x00027000u};
+#pragma unroll
+            for (int e = 0; e < (kRows < 16 ? 1 : 2); ++e) {                 // eight rows
+                const int odd = kRows < 16 ? wave & 1 : e;                   // (bit 3 of the row, which is in the keys)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    load_to_lds(rs, (l0 ^ c_key(i) ^ (odd << 3)) << 4, (8 * e + i) * kRowBytes, to_c + (16 * h + 8 * e + i) * kCBytes);
+                const int r = l0 >> 3;
+                load_to_lds(rs, r * kRowBytes + kCBytes + (((l0 & 7) ^ r_key(r) ^ (odd << 1)) << 4), 8 * e * kRowBytes, to_r + (16 * h + 8 * e) * kRBytes);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) page[h] = page_of(s + 1, h);
+    };
+    fetch(0);
 
     u32x4_t q[18];
 #pragma unroll
@@ -94,97 +143,110 @@ template <class T> __global__ __launch_bounds__(256, 1) void latent_decode_kerne
             q[kb] = *reinterpret_cast<const u32x4_t *>(kb < 16 ? p.q_latent + row * kLatent + 32 * kb + 8 * g : p.q_rope + row * kRope + 32 * (kb - 16) + 8 * g);
         }
     }
-    __syncthreads();                                           // the pages; and every load so far has arrived
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-
-    // Fetches: instruction k of 18 fills KiB k of 16 rows' 18 KiB.  576 pieces are 8 rows: instruction k + 9 is k, 8 rows further.  Wavefronts 0 and 1
-    // fetch rows 0 .. 15 of a tile, 2 and 3 the others.
-    int voff[9];
-#pragma unroll
-    for (int k = 0; k < 9; ++k) {
-        const int u = 64 * k + lane + 576 * (wave & 1), r = u / 72, x = u % 72;
-        voff[k] = r * kRowBytes + ((x ^ swizzle(r)) << 4);
-    }
-    const int steps = (end - start + kTile - 1) / kTile;
-    auto fetch = [&](int s) {
-        const int key0 = start + s * kTile + 16 * (wave >> 1);
-        const int left = min(max(end - key0, 0), 16);          // rows with keys: the others arrive as zeros
-        const int k0 = left > 0 ? key0 : start;
-        const int page = __builtin_amdgcn_readfirstlane(lds.pages[(k0 >> shift) - first_page]);
-        const unsigned long long at = reinterpret_cast<unsigned long long>(p.pool.rows) + (((size_t)page << shift) + (k0 & mask)) * kRowBytes;
-        const u32x4_t rs = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at), __builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
-                            (unsigned)__builtin_amdgcn_readfirstlane(left * kRowBytes), 0x00027000u};
-        const unsigned char *to = lds.rows[s % kRing] + wave * 9 * 1024;
-#pragma unroll
-        for (int k = 0; k < 9; ++k) load_to_lds(rs, voff[k], to + k * 1024);
-    };
-    fetch(0);
-    fetch(1);
-    fetch(2);
-
     f32x4_t acc[32];
 #pragma unroll
     for (int dt = 0; dt < 32; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     const float c1 = p.scale * kLog2e;
-    const int k_row = 8 * (n >> 2) + (n & 3), k_swz = swizzle(k_row);
-    const int v_row = 8 * g + (n >> 2), v_swz = swizzle(v_row);
+    // this lane's operand reads: piece 4 kb + g of row k_row; 32 bytes from element 16 dt of row v_row.  Pieces within 256 bytes differ by an exclusive or.
+    const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
+    const unsigned k_at = k_row * kCBytes + ((g ^ c_key(k_row)) << 4), kr_at = k_row * kRBytes + ((g ^ r_key(k_row)) << 4);
+    const unsigned v_at = v_row * kCBytes + (((n >> 1) & 1) << 4) + ((n & 1) << 3) + (c_key(v_row) << 4);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries (the compiler does not count the fetches)
 
     for (int s = 0; s < steps; ++s) {
-        wait_fetches<18>();                                    // tile s; s + 1 and s + 2 are under way
-        tile_barrier();                                        // ... and every wavefront is through with tile s - 1
-        fetch(s + 3);
-        if (heads > 0) {
-            unsigned char *rows = lds.rows[s % kRing];
-            f32x4_t sc[2];
+        wait_fetches<0>();                                     // step s
+        tile_barrier();                                        // ... for every wavefront, all of which are through with step s - 1
+        if (s + 1 < steps) fetch(s + 1);
+        if (heads <= 0) continue;
+#pragma unroll 1
+        for (int i = 0; i < TPW; ++i) {
+            const unsigned tile_c = lds_c + ((s & 1) * TPW + i) * (kTile * kCBytes), tile_r = lds_r + ((s & 1) * TPW + i) * (kTile * kRBytes);
+            f32x4_t sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            {
+                const unsigned kc = tile_c + k_at, kr = tile_r + kr_at;
+                auto read = [&](int kb, int t) {
+                    const unsigned x = kb < 16 ? (kc ^ ((kb & 3) << 6)) + ((kb >> 2) << 8) + t * 4 * kCBytes : (kr ^ ((kb & 1) << 6)) + t * 4 * kRBytes;
+                    return *(lds_u32x4)(uintptr_t)x;
+                };
+                // reads run kAhead operands ahead of the instructions that use them
+                constexpr int kAhead = 3;
+                u32x4_t a[kAhead + 1][2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int kb = 0; kb < kAhead; ++kb)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) a[kb][t] = read(kb, t);
 #pragma unroll
                 for (int kb = 0; kb < 18; ++kb) {
-                    const u32x4_t a = *reinterpret_cast<const u32x4_t *>(rows + (k_row + 4 * t) * kRowBytes + (((4 * kb + g) ^ k_swz) << 4));
-                    sc[t] = T::mfma(a, q[kb], sc[t]);
+                    if (kb + kAhead < 18)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) a[(kb + kAhead) % (kAhead + 1)][t] = read(kb + kAhead, t);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) sc[t] = T::mfma(a[kb % (kAhead + 1)][t], q[kb], sc[t]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            float z[8];
-            const int left = end - (start + s * kTile) - 8 * g;
+            const unsigned vc = tile_c + v_at;
+            auto read = [&](int dt) {
+                const unsigned x = (vc ^ ((dt & 7) << 5)) + ((dt >> 3) << 8);
+                const s16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)x);
+                const s16x4_t w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(x + 4 * kCBytes));
+                return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            constexpr int kAhead = 4;
+            u32x4_t a[kAhead + 2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = j < left ? sc[j >> 2][j & 3] * c1 : -INFINITY;
-            float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-            top = fmaxf(m, columns_max(top));
-            if (__any(top > m)) {
-                const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            for (int d = 0; d < kAhead; ++d) a[d] = read(d);
+            __builtin_amdgcn_sched_barrier(0);
+
+            const int left = end - (start + s * kKeys + i * kTile);         // keys from the tile's first
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] *= c1;
+            if (left < kTile) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] = 8 * g + j < left ? sc[j >> 2][j & 3] : -INFINITY;
+            }
+            float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+            top = columns_max(top);
+            if (__any(top > m + kSlack)) {                     // (also where there is no reference yet)
+                const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
                 l *= f;
 #pragma unroll
                 for (int dt = 0; dt < 32; ++dt)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[dt][r] *= f;
-                m = top;
+                m = to;
             }
             const float ref = m == -INFINITY ? 0.f : m;
             u32x4_t hi, lo;
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(z[j] - ref), e1 = __builtin_amdgcn_exp2f(z[j + 1] - ref);
-                l += e0 + e1;
+                const float e0 = __builtin_amdgcn_exp2f(sc[j >> 2][j & 3] - ref), e1 = __builtin_amdgcn_exp2f(sc[j >> 2][(j & 3) + 1] - ref);
                 const unsigned h = T::pack(e0, e1);
                 hi[j >> 1] = h;
-                lo[j >> 1] = T::pack(e0 - T::lo(h), e1 - T::hi(h));
+                if constexpr (kTwoParts) {
+                    l += e0 + e1;
+                    lo[j >> 1] = T::pack(e0 - T::lo(h), e1 - T::hi(h));
+                } else {
+                    l += T::lo(h) + T::hi(h);
+                }
             }
 #pragma unroll
-            for (int dt = 0; dt < 32; ++dt) {
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
-                unsigned char *at = rows + v_row * kRowBytes + (((2 * dt + ((n >> 1) & 1)) ^ v_swz) << 4) + ((n & 1) << 3);
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
-                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kRowBytes));
-                const u32x4_t a = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-                acc[dt] = T::mfma(a, hi, acc[dt]);
-                acc[dt] = T::mfma(a, lo, acc[dt]);
+            for (int dt = 0; dt < 32; dt += 2) {
+#pragma unroll
+                for (int d = 0; d < 2; ++d)
+                    if (dt + d + kAhead < 32) a[(dt + d + kAhead) % (kAhead + 2)] = read(dt + d + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(dt + d) % (kAhead + 2)], hi, acc[dt + d]);
+                if constexpr (kTwoParts)
+#pragma unroll
+                    for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(dt + d) % (kAhead + 2)], lo, acc[dt + d]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
-    wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
     if (n >= heads) return;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -203,6 +265,16 @@ template <class T> __global__ __launch_bounds__(256, 1) void latent_decode_kerne
     }
 }
 
+template <class T, int NH, int TPW> hipError_t decode(const LatentProblem &p, hipStream_t s)
+{
+    const long long tiles = (p.H + 16 * NH - 1) / (16 * NH), units = (long long)p.B * p.nc;
+    return launch(latent_decode_kernel<T, NH, TPW>, dim3((unsigned)((units + 7) / 8 * 8 * tiles)), dim3(64 * NH), s, p);
+}
+template <class T> hipError_t decode_heads(const LatentProblem &p, hipStream_t s)
+{
+    return p.H > 64 ? decode<T, 8, 2>(p, s) : decode<T, 4, 1>(p, s);
+}
+
 }  // namespace
 
 hipError_t launch_latent_write(const LatentPool &pool, const uint16_t *latent, long long latent_stride, const uint16_t *rope,
@@ -213,9 +285,7 @@ hipError_t launch_latent_write(const LatentPool &pool, const uint16_t *latent, l
 }
 hipError_t launch_latent_decode(const LatentProblem &p, hipStream_t s)
 {
-    const long long tiles = (p.H + 63) / 64, units = (long long)p.B * p.nc;
-    const dim3 grid((unsigned)((units + 7) / 8 * 8 * tiles));
-    const hipError_t e = p.pool.dtype == kF16 ? launch(latent_decode_kernel<F16>, grid, dim3(256), s, p) : launch(latent_decode_kernel<BF16>, grid, dim3(256), s, p);
+    const hipError_t e = p.pool.dtype == kF16 ? decode_heads<F16>(p, s) : decode_heads<BF16>(p, s);
     if (e != hipSuccess || p.nc == 1) return e;
     JoinProblem j{p.num, p.ml, p.seq_lens, p.out, p.B * p.H, p.H, p.C, p.nc, p.Smax, kLatent, p.pool.dtype};
     return launch_join(j, s);

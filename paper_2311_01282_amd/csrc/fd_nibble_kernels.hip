@@ -415,23 +415,51 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 }
 
 // ---- the join of rows that several workgroups share ----
+// A workgroup a row.  Its length is that of its loads, so all of them are asked for together: first the references and denominators of 64 chunks, then, with
+// their factors in LDS, eight partial vectors at a time.
+constexpr int kJoinWindow = 64;
 template <class T, int DIM> __global__ __launch_bounds__(DIM / 2) void join_kernel(JoinProblem p)
 {
-    const int row = blockIdx.x, b = row / p.H, tid = threadIdx.x;
+    __shared__ float factor[kJoinWindow];
+    const int row = blockIdx.x, b = row / p.H, tid = threadIdx.x, lane = tid & 63;
     const int len = min(max(p.seq_lens[b], 0), p.Smax), nb = (len + p.C - 1) / p.C;
     unsigned *out = reinterpret_cast<unsigned *>(p.out + (size_t)row * DIM) + tid;
     if (nb == 0) { *out = 0u; return; }
     const float2 *ml = p.ml + (size_t)row * p.nc;
-    float top = -INFINITY;
-    for (int i = 0; i < nb; ++i) top = fmaxf(top, ml[i].x);
-    float a0 = 0.f, a1 = 0.f, sum = 0.f;
     const float *num = p.num + (size_t)row * p.nc * DIM + 2 * tid;
-    for (int i = 0; i < nb; ++i) {
-        const float2 s = ml[i], x = *reinterpret_cast<const float2 *>(num + (size_t)i * DIM);
+    float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
+    for (int w0 = 0; w0 < nb; w0 += kJoinWindow) {
+        const int count = min(nb - w0, kJoinWindow);
+        float2 s = {-INFINITY, 0.f};
+        if (lane < count) s = ml[w0 + lane];
+        float t = columns_max(row16_max(s.x));
+        if (t > top) {                                          // (uniform) what the windows before left, to the new reference
+            const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - t);
+            a0 *= f;
+            a1 *= f;
+            sum *= f;
+            top = t;
+        }
         const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f(s.x - top);
-        a0 = __builtin_fmaf(x.x, f, a0);
-        a1 = __builtin_fmaf(x.y, f, a1);
-        sum = __builtin_fmaf(s.y, f, sum);
+        float d = lane < count ? s.y * f : 0.f;
+        d = row16_sum(d);
+        d = rows_sum(d, d);
+        sum += halves_sum(d, d);
+        __syncthreads();                                        // (the factors of the window before are out of use)
+        if (tid < kJoinWindow) factor[tid] = f;
+        __syncthreads();
+        for (int i = 0; i < count; i += 8) {
+            float2 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = i + k < count ? *reinterpret_cast<const float2 *>(num + (size_t)(w0 + i + k) * DIM) : float2{0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i + k < count) {
+                    a0 = __builtin_fmaf(x[k].x, factor[i + k], a0);
+                    a1 = __builtin_fmaf(x[k].y, factor[i + k], a1);
+                }
+        }
     }
     const float inv = 1.f / sum;
     *out = T::pack(a0 * inv, a1 * inv);

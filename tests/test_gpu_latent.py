@@ -75,7 +75,8 @@ def check(got, rows, table, lens, ql, qr, scale):
         k = want.gather(rows, table[b], n, rows.shape[1]).double()
         q = torch.cat([ql[b], qr[b]], -1)
         exp = want.attend(q, k, k[:, :512], scale)
-        tol = tolerance(rows.dtype, 2, 576, q, k, k[:, :512], scale, exp)
+        # (of more than 64 heads a weight is one number of the type: off by half a step of its own, as in the prompts)
+        tol = tolerance(rows.dtype, 2 if len(q) <= 64 else 1, 576, q, k, k[:, :512], scale, exp)
         off = (x - exp).abs()
         assert torch.isfinite(x).all() and (off <= tol).all(), "sequence %d (%d keys): %.3g of the tolerance" % (b, n, float((off / tol).max()))
 
