@@ -486,9 +486,16 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     without a valid token are not followed, an entry in use that is out of range is the caller's error (it is
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
- * Memory, stream, errors and threads: as stated at the top.  Nothing here needs an initialisation call; a workspace
- * may hold anything before a call and serves one call at a time.                                              */
+ *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
+ *     its first 16 KiB, arrival counters that every completed call leaves at zero again; what lies behind them may hold anything.  After that
+ *     shapes and calls may change from one use to the next.  A workspace serves one call at a time: calls that may overlap, captured
+ *     graphs that are replayed at the same time among them, need one each; so do these calls and the others of this
+ *     header.  After a call that did not complete prepare it again (a left-over count keeps rows from being written).
+ * Memory, stream, errors and threads: as stated at the top.                                                     */
 typedef enum { FD_F16 = 0, FD_BF16 = 1 } fd_dtype;
+
+/* Zeroes the arrival counters of a workspace for fd_decode_attn_nibble and fd_latent_decode_attn. */
+fd_status fd_cache_workspace_init(fd_workspace ws, void *stream);
 
 /*
  * Pages for a step's new tokens, the block table and the slot of every token, on the GPU from the lengths alone.
@@ -546,7 +553,8 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
  * q, out [batch, n_q_heads, 128] of the pool's dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of
  * 64 from 64 to 16384 keys, for example fd_nibble_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
  * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of dtype each (22
- * significant bits in fp16, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch where chunk >= max_seq, else two.
+ * significant bits in fp16, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch for up to 16
+ * chunks a row (and up to 4096 groups of up to 16 heads that share a KV head), else two.
  */
 size_t    fd_nibble_workspace_bytes(const fd_shape *shape);
 int32_t   fd_nibble_pick_chunk(const fd_shape *shape);

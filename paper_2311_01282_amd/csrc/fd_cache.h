@@ -37,7 +37,8 @@ struct NibbleProblem {
     const int32_t *seq_lens, *table;
     uint16_t *out;
     float *num;                                    // workspace: [B, Hq, nc, 128] sum e^{x-m} v
-    float2 *ml;                                    // [B, Hq, nc] (m, l), m the largest logit times log2 e
+    float2 *ml;                                    // [B, Hq, nc] (m, l), m the reference of the weights times log2 e
+    int32_t *counters;                             // [B, Hkv, tiles] chunks that have arrived, zero between calls; null: the join is a launch of its own
     int B, Hq, G, tiles, C, nc, Smax, width;       // tiles: of 16 query heads of a KV head
     float scale;
 };
@@ -77,7 +78,7 @@ struct LatentPromptProblem {
 hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s);
 
 // Splits of a row between workgroups, joined by a launch of its own: out = sum_c 2^{m_c - M} num_c / sum_c 2^{m_c - M} l_c over the
-// chunks that hold a key; rows of length 0 become zeros.  rows: [B, H] output rows of `dim` elements.
+// chunks that hold a key, of rows with two or more of them.  rows: [B, H] output rows of `dim` elements.
 struct JoinProblem {
     const float *num;
     const float2 *ml;

@@ -77,10 +77,12 @@ fd_status latent_pool(const fd_latent_pool *pool, fd::LatentPool *out)
     return FD_OK;
 }
 
-// A row is cut into chunks, one workgroup each, whose sums meet in the workspace.
+// A row is cut into chunks, one workgroup each, whose sums meet in the workspace.  It begins with arrival counters, a fixed number of them, so that
+// they stay where they are whatever the shape.
+constexpr int kCounters = 4096;
 struct Split {
     long long rows, nc;
-    size_t num, total;
+    size_t num, ml, total;
 };
 fd_status check_shape(const fd_shape *sh, int head_dim)
 {
@@ -100,8 +102,9 @@ fd_status split(const fd_shape *sh, int head_dim, int dim, int unit, Split *S)
     S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
     if (S->rows * S->nc >= (1ll << 31)) return FD_ERR_UNSUPPORTED;
     const size_t slots = (size_t)(S->rows * S->nc);
-    S->num = align_up(slots * dim * sizeof(float));
-    S->total = S->nc == 1 ? kAlign : align_up(S->num + slots * sizeof(float2)) + (slots == 0 ? kAlign : 0);
+    S->num = align_up(kCounters * sizeof(int32_t));
+    S->ml = align_up(S->num + (S->nc == 1 ? 0 : slots * dim * sizeof(float)));
+    S->total = align_up(S->ml + (S->nc == 1 ? 0 : slots * sizeof(float2)));
     return FD_OK;
 }
 inline bool bad_ws(fd_workspace ws, const Split &S) { return !ws.ptr || off(ws.ptr, kAlign) || ws.bytes < S.total; }
@@ -176,6 +179,13 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
     return FD_OK;
 }
 
+fd_status fd_cache_workspace_init(fd_workspace ws, void *stream)
+{
+    if (!ws.ptr || off(ws.ptr, kAlign) || ws.bytes < kCounters * sizeof(int32_t)) return FD_ERR_WORKSPACE;
+    FD_TRY(fd::launch_clear_tickets(static_cast<int32_t *>(ws.ptr), kCounters, static_cast<hipStream_t>(stream)));
+    return FD_OK;
+}
+
 size_t fd_nibble_workspace_bytes(const fd_shape *shape)
 {
     Split S;
@@ -207,9 +217,10 @@ fd_status fd_decode_attn_nibble(const fd_shape *shape, const fd_nibble_pool *poo
     p.seq_lens = seq_lens;
     p.table = block_table;
     p.out = static_cast<uint16_t *>(out);
-    p.num = static_cast<float *>(ws.ptr);
-    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.num);
+    p.num = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + S.num);
+    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.ml);
     p.B = shape->batch; p.Hq = shape->n_q_heads; p.G = shape->n_q_heads / shape->n_kv_heads; p.tiles = (p.G + 15) / 16;
+    if ((long long)p.B * shape->n_kv_heads * p.tiles <= kCounters) p.counters = static_cast<int32_t *>(ws.ptr);
     p.C = shape->chunk; p.nc = (int)S.nc; p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
     p.scale = shape->scale;
     FD_TRY(fd::launch_nibble_attn(p, static_cast<hipStream_t>(stream)));
@@ -266,8 +277,8 @@ fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *poo
     p.seq_lens = seq_lens;
     p.table = block_table;
     p.out = static_cast<uint16_t *>(out);
-    p.num = static_cast<float *>(ws.ptr);
-    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.num);
+    p.num = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + S.num);
+    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.ml);
     p.B = shape->batch; p.H = shape->n_q_heads; p.C = shape->chunk; p.nc = (int)S.nc; p.Smax = shape->max_seq;
     p.width = shape->max_seq / pool->page_size;
     p.scale = shape->scale;

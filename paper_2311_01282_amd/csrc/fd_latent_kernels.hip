@@ -98,7 +98,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
     const int end = min(len, start + p.C);
     const int heads = min(p.H - head0, 16);                    // of this wavefront; may be 0 or less: it only fetches
     if (start >= end) {
-        if (p.nc == 1)                                         // no keys at all: zero rows
+        if (chunk == 0)                                        // no keys at all: zero rows
             for (int h = 0; h < heads; ++h)
                 reinterpret_cast<u32x4_t *>(p.out + ((size_t)b * p.H + head0 + h) * kLatent)[lane] = u32x4_t{0u, 0u, 0u, 0u};
         return;
@@ -251,7 +251,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     const size_t row = (size_t)b * p.H + head0 + n;
-    if (p.nc == 1) {
+    if (len <= p.C) {                                          // the only chunk with keys
         const float inv = 1.f / l;
 #pragma unroll
         for (int dt = 0; dt < 32; ++dt)

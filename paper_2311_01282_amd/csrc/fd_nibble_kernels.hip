@@ -121,8 +121,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 // One query token a sequence over the coded rows, synchronized softmax with a running maximum.  The codes go to the matrix cores as the
 // numbers 16 + c, exact in both types, without touching the scales: of an element l + s c the product with a query is
 //     sum_d q_d (l_g + s_g c_d) = sum_g s_g (sum_{d in g} q_d c_d) + l_g (sum_{d in g} q_d),
-// four matrix instructions a row, one a group of 32, and a multiply-add with s and one with l a group; the 16 is taken off in the accumulator the
-// instruction starts from.  Of the output
+// four matrix instructions a row, one a group of 32, and a multiply-add with s and one with l a group; the 16 is taken off in the term with l.  Of the output
 //     sum_j p_j (l_jg + s_jg c_jd) = sum_j (p_j s_jg) (16 + c_jd) + sum_j p_j (l_jg - 16 s_jg),
 // the weights p s of a group as the operand, in two parts of the type (hi + lo: 16 significant bits in bf16, 22 in fp16; one part alone
 // would add an error as large as the output's rounding), the last sum in fp32.
@@ -130,66 +129,136 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 // Lanes (16 x 16 x 32): n = lane % 16, c = lane / 16.  Scores of 16 query heads (rows) and 16 keys (columns): the lane of a key has its
 // scales in registers.  Query head h of a tile sits in row 4 (h % 4) + h / 4, so that R = ceil(heads / 4) of a lane's four rows are in use.
 // The weights pass through LDS (a wavefront's own), where lane n then finds row n; V's codes pass through LDS too, and the transposing
-// read of 4-bit elements gives lane n the codes of element n of 16 keys: two operands of eight keys.
-// A wavefront takes 64 keys at a time, every fourth such block of its workgroup's chunk; the four are joined at the end.
+// read of 4-bit elements gives lane n the codes of element n of 16 keys: two operands of eight.
+// A wavefront takes 64 keys at a time, four tiles of 16, every fourth such block of its workgroup's chunk; the four are joined at the end.  (Workgroups of one wavefront, with
+// a chunk and a partial result each, did 32 x 64/8 heads x 4096 keys in 38.5 us at their best chunk, these in 35.4.)  Of the 64, operand u of
+// lanes c takes keys of two tiles, 2 (c / 2) and the next, 8 (c % 2) + 4 u .. + 3 of each: what a lane has of the two tiles then lies side by side (expand's pairs).
 constexpr int kBlock = 64;                       // keys of a wavefront step
+constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
 constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
-constexpr int kMaxPages = 1026;                  // table entries of a chunk (16384 keys in pages of 16)
+// The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.
+constexpr float kSlack = 8.f;
 
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
 template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; };
 template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; };
 
-// Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).
-template <class T> __device__ __forceinline__ u32x4_t expand(unsigned w)
+// Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).  sixteen: Magic::kSixteen in a register the compiler cannot see through, which keeps
+// "and" and "or" one instruction (of two constants only one can be other than a register).
+template <class T> __device__ __forceinline__ u32x4_t expand(unsigned w, unsigned sixteen)
 {
     constexpr int k = Magic<T>::kShift;
     u32x4_t x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned y = 4 * i <= k ? w << (k - 4 * i) : w >> (4 * i - k);
-        x[i] = (y & Magic<T>::kMask) | Magic<T>::kSixteen;
+        x[i] = (y & Magic<T>::kMask) | sixteen;
     }
     return x;
 }
 
-struct NibbleLds {
+template <int R> struct NibbleLds {
     union {
         struct {
-            alignas(16) unsigned char v[4][kBlock * 64];
-            alignas(16) unsigned char w[4][2][16 * kRowStride];       // weights, hi and lo parts
+            alignas(16) unsigned char v[4][2][kBlock * 64];            // of this step and of the next
+            alignas(16) unsigned char w[4][2][2][4 * R * kRowStride];  // weights of a group, two groups in turn: hi and lo parts; row 4 c + r in place R c + r
         };
-        float rows[4][16][kHeadDim];                                  // at the end: the wavefronts' sums
+        float rows[4][4 * R][kHeadDim];                                // at the end: the wavefronts' sums
     };
-    float m[4][16], l[4][16];
-    int pages[kMaxPages];
+    float m[4][4 * R], l[4][4 * R];
+    int last;
 };
+// Loads into LDS, 1 KiB at lds_1k.  In assembly: of those that the compiler knows it would wait before every transposing read.  They are older than the loads of K's codes of
+// the same step, and loads arrive in order: once K's codes are there, so are they.
+__device__ __forceinline__ void load_to_lds(const unsigned char *base, int voff, unsigned lds_1k)
+{
+    const unsigned long long at = reinterpret_cast<unsigned long long>(base);
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds_1k), "v"(voff), "s"(at) : "memory");
+}
 
 template <class T> __device__ __forceinline__ float scale_at(const unsigned *w, int i) { return (i & 1) ? T::hi(w[i >> 1]) : T::lo(w[i >> 1]); }
 
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
+typedef __attribute__((address_space(4))) const int32_t *scalar_i32;      // read through the scalar cache
+
 template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibble_attn_kernel(NibbleProblem p)
 {
-    __shared__ NibbleLds lds;
+    __shared__ NibbleLds<R> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, c = lane >> 4;
-    const int chunk = blockIdx.x % p.nc;
-    int unit = blockIdx.x / p.nc;
+    const int chunk = blockIdx.x % p.nc, group = blockIdx.x / p.nc;
+    int unit = group;
     const int tile = unit % p.tiles;
     unit /= p.tiles;
     const int hkv = unit % p.pool.Hkv, b = unit / p.pool.Hkv;
-    const int len = min(max(p.seq_lens[b], 0), p.Smax);
-    const int start = chunk * p.C, end = min(len, start + p.C);
+    const int start = chunk * p.C, shift = p.pool.page_shift, mask = (1 << shift) - 1;
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)b * p.width);
+    const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
+    const int end = min(len, start + p.C);
     const int heads = min(p.G - 16 * tile, 16), head0 = hkv * p.G + 16 * tile;      // query heads of this tile
     if (start >= end) {
-        // a sequence without keys: zero rows, by the first chunk (chunks without keys leave nothing: the join knows the lengths)
-        if (p.nc == 1)
+        // a sequence without keys: zero rows, by the first chunk (other chunks without keys leave nothing)
+        if (chunk == 0)
             for (int i = tid; i < heads * kHeadDim / 2; i += 256) reinterpret_cast<unsigned *>(p.out + ((size_t)b * p.Hq + head0) * kHeadDim)[i] = 0u;
         return;
     }
-    const int shift = p.pool.page_shift, mask = (1 << shift) - 1, first_page = start >> shift;
-    const int used = ((end - 1) >> shift) - first_page + 1;
-    for (int i = tid; i < used; i += 256) lds.pages[i] = min(max(p.table[(size_t)b * p.width + first_page + i], 0), p.pool.n_pages - 1);
+    constexpr int SW = NG;                         // 32-bit words of a row's scales
+    u32x4_t kc[4];
+    unsigned ks[4][SW], vs[4][SW];
+    // pages of the four tiles from key0 (of the last tile with a key, for those behind it)
+    const int last_tile = (end - 1) & ~15;
+    int page[4];
+    auto load_pages = [&](int key0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = table[min(key0 + 16 * i, last_tile) >> shift];
+    };
+    size_t row[4];                                 // of the pool: the tiles' first
+    auto find_rows = [&](int key0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pg = min(max(page[i], 0), p.pool.n_pages - 1);
+            row[i] = (((size_t)pg * p.pool.Hkv + hkv) << shift) + (min(key0 + 16 * i, last_tile) & mask);
+        }
+    };
+    // (a uniform base and a 32-bit offset of the lane)
+    auto load_codes = [&](const unsigned char *base, u32x4_t (&x)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(base + row[i] * 64 + (unsigned)(64 * n + 16 * c)));
+    };
+    auto load_scales = [&](const uint16_t *base, unsigned (&w)[4][SW]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned char *at = reinterpret_cast<const unsigned char *>(base) + row[i] * (4 * SW) + (unsigned)(4 * SW * n);
+            if constexpr (NG == 4) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(at);
+                w[i][0] = x[0]; w[i][1] = x[1]; w[i][2] = x[2]; w[i][3] = x[3];
+            } else if constexpr (NG == 2) {
+                const u32x2_t x = *reinterpret_cast<const u32x2_t *>(at);
+                w[i][0] = x[0]; w[i][1] = x[1];
+            } else {
+                w[i][0] = *reinterpret_cast<const unsigned *>(at);
+            }
+        }
+    };
+    // V's codes in LDS: row of key k of tile i at 64 (16 i + k), its 16-byte piece x in place x ^ (2 (i % 2) + (k / 4) % 2)
+    const int v_lane = 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 4) & 1));
+    const unsigned v_lds = __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)lds.v[wave][0]));
+    auto load_v = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            load_to_lds(p.pool.v_codes + row[i] * 64, v_lane ^ ((i & 1) << 5), v_lds + buffer * (kBlock * 64) + 1024 * i);
+    };
+    int key0 = start + kBlock * wave, buffer = 0;
+    if (key0 < end) {
+        load_pages(key0);
+        find_rows(key0);
+        load_v(0);
+        load_codes(p.pool.k_codes, kc);
+        load_scales(p.pool.k_scales, ks);
+        load_scales(p.pool.v_scales, vs);
+        load_pages(key0 + 4 * kBlock);
+    }
 
     // the query rows: A operand, elements 32 t + 8 c .. + 7 of row n in the order of the expanded codes
     u32x4_t qa[4];
@@ -209,16 +278,15 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
         }
     }
     // sums of the query over a group, for this lane's rows 4 c + r
-    float qsum[NG][4];
+    float qsum[NG][R];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         float s = 0.f;
 #pragma unroll
         for (int t = 0; t < 4 / NG; ++t) s += qs[g * (4 / NG) + t];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) qsum[g][r] = __shfl(s, 4 * c + r);
+        for (int r = 0; r < R; ++r) qsum[g][r] = __shfl(s, 4 * c + r);
     }
-    __syncthreads();
 
     const float c1 = p.scale * kLog2e;
     float m[R], l[R], low[R][NG];
@@ -232,143 +300,193 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     }
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    unsigned sixteen;
+    asm("v_mov_b32 %0, %1" : "=v"(sixteen) : "i"(Magic<T>::kSixteen));
 
-    constexpr int SW = NG;                         // 32-bit words of a row's scales
-    u32x4_t kc[4], vc[4];
-    unsigned ks[4][SW], vs[4][SW];
-    // row 0 of the 16 keys from key0 (those behind the last key: of the last 16 that hold one)
-    auto row_of = [&](int key0) -> size_t {
-        const int k0 = min(key0, (end - 1) & ~15);
-        const int page = __builtin_amdgcn_readfirstlane(lds.pages[(k0 >> shift) - first_page]);
-        return (((size_t)page * p.pool.Hkv + hkv) << shift) + (k0 & mask);
-    };
-    auto load_scales = [&](const uint16_t *base, size_t row, unsigned (&w)[SW]) {
-        const unsigned *at = reinterpret_cast<const unsigned *>(base) + (row + n) * SW;
-        if constexpr (NG == 4) {
-            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(at);
-            w[0] = x[0]; w[1] = x[1]; w[2] = x[2]; w[3] = x[3];
-        } else if constexpr (NG == 2) {
-            const u32x2_t x = *reinterpret_cast<const u32x2_t *>(at);
-            w[0] = x[0]; w[1] = x[1];
-        } else {
-            w[0] = *at;
-        }
-    };
-    auto load_block = [&](int key0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const size_t row = row_of(key0 + 16 * i);
-            kc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.pool.k_codes + row * 64) + 4 * n + c);
-            vc[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p.pool.v_codes + row * 64) + 4 * n + c);
-            load_scales(p.pool.k_scales, row, ks[i]);
-            load_scales(p.pool.v_scales, row, vs[i]);
-        }
-    };
-    unsigned char *v_at = lds.v[wave], *w_hi = lds.w[wave][0], *w_lo = lds.w[wave][1];
+    unsigned char *w_at = lds.w[wave][0][0];
+    constexpr int kLo = 4 * R * kRowStride, kTurn = 2 * kLo;               // from a hi part to its lo part, from a group to the next
+    const int w_row = (R * (n >> 2) + min(n & 3, R - 1)) * kRowStride;      // of row n (of rows that no head sits in: another's)
+    // this lane's row for the transposing reads of V's codes
+    const int v_tile = 2 * (c >> 1) + ((n >> 2) & 1), v_key = 8 * (c & 1) + 4 * (n >> 3) + (n & 3);
+    const unsigned char *v_row = lds.v[wave][0] + (16 * v_tile + v_key) * 64;
+    const int v_turn = 2 * (v_tile & 1) + ((v_key >> 2) & 1);
 
-    for (int key0 = start + kBlock * wave; key0 < end; key0 += 4 * kBlock) {
-        load_block(key0);
-        // scores, in units of log2
+    for (; key0 < end; key0 += 4 * kBlock, buffer ^= 1) {
+        const int next = key0 + 4 * kBlock;
+        // Scores, in units of log2.  The matrix instructions of a tile run while the codes of the next are expanded (left to itself the compiler takes one register
+        // after the other through expand, product and sum, and waits in between).
         float z[4][R];
+        {
+            u32x4_t e[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float x[R];
+            for (int t = 0; t < 4; ++t) e[t] = expand<T>(kc[0][t], sixteen);
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[r] = 0.f;
+            for (int i = 0; i < 4; ++i) {
+                f32x4_t a[NG];
+                u32x4_t en[4];
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                f32x4_t a = {-16.f * qsum[g][0], -16.f * qsum[g][1], -16.f * qsum[g][2], -16.f * qsum[g][3]};
+                for (int t = 0; t < 4; ++t) a[t * NG / 4] = T::mfma(qa[t], e[t], t % (4 / NG) == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : a[t * NG / 4]);
+                if (i < 3)
 #pragma unroll
-                for (int t = 0; t < 4 / NG; ++t) a = T::mfma(qa[g * (4 / NG) + t], expand<T>(kc[i][g * (4 / NG) + t]), a);
-                const float s = scale_at<T>(ks[i], g), lw = scale_at<T>(ks[i], NG + g);
+                    for (int t = 0; t < 4; ++t) en[t] = expand<T>(kc[i + 1][t], sixteen);
+                float s[NG], lw[NG];
 #pragma unroll
-                for (int r = 0; r < R; ++r) x[r] = __builtin_fmaf(s, a[r], __builtin_fmaf(lw, qsum[g][r], x[r]));
+                for (int g = 0; g < NG; ++g) {
+                    s[g] = scale_at<T>(ks[i], g);
+                    lw[g] = __builtin_fmaf(-16.f, s[g], scale_at<T>(ks[i], NG + g));
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);         // a matrix instruction ...
+                    __builtin_amdgcn_sched_group_barrier(0x002, 9, 0);         // ... and vector instructions behind it
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float x = lw[0] * qsum[0][r], y = s[0] * a[0][r];
+#pragma unroll
+                    for (int g = 1; g < NG; ++g) {
+                        x = __builtin_fmaf(lw[g], qsum[g][r], x);
+                        y = __builtin_fmaf(s[g], a[g][r], y);
+                    }
+                    z[i][r] = (x + y) * c1;
+                }
+                if (i < 3)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) e[t] = en[t];
             }
-            const bool live = key0 + 16 * i + n < end;
-#pragma unroll
-            for (int r = 0; r < R; ++r) z[i][r] = live ? x[r] * c1 : -INFINITY;
-            // V's scales of keys that are not there may be anything
-#pragma unroll
-            for (int k = 0; k < SW; ++k) vs[i][k] = live ? vs[i][k] : 0u;
         }
-        // V's codes into LDS: row of key k at 64 k, its 16-byte piece x in place x ^ ((k >> 2) & 3), with the halves of the odd 16 keys swapped
+        if (key0 + kBlock > end) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x4_t x = (i & 1) ? u32x4_t{vc[i][2], vc[i][3], vc[i][0], vc[i][1]} : vc[i];
-            *reinterpret_cast<u32x4_t *>(v_at + (16 * i + n) * 64 + ((c ^ ((n >> 2) & 3)) << 4)) = x;
+            for (int i = 0; i < 4; ++i) {
+                const bool live = key0 + 16 * i + n < end;
+#pragma unroll
+                for (int r = 0; r < R; ++r) z[i][r] = live ? z[i][r] : -INFINITY;
+#pragma unroll
+                for (int k = 0; k < SW; ++k) vs[i][k] = live ? vs[i][k] : 0u;          // of keys that are not there: may be anything
+            }
+        }
+        asm volatile("" ::: "memory");                                                 // K's codes have been used: V's are there
+        __builtin_amdgcn_s_waitcnt(0xc07f);                                            // ... and what was read of the step before has arrived
+        if (next < end) {                                                              // under way during the rest of the step
+            find_rows(next);
+            load_v(buffer ^ 1);
+            load_codes(p.pool.k_codes, kc);
+            load_scales(p.pool.k_scales, ks);
         }
         // the running maximum; what was summed is brought to it where it grew
         bool grew = false;
-        float mn[R];
+        float top[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float top = row16_max(fmaxf(fmaxf(z[0][r], z[1][r]), fmaxf(z[2][r], z[3][r])));
-            mn[r] = fmaxf(m[r], top);
-            grew |= mn[r] > m[r];
+            top[r] = row16_max(fmaxf(fmaxf(z[0][r], z[1][r]), fmaxf(z[2][r], z[3][r])));
+            grew |= top[r] > m[r] + kSlack;
         }
-        if (__any(grew)) {
+        if (__any(grew)) {                                                             // (also where there is no reference yet)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float f = mn[r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - mn[r]);
+                const float to = fmaxf(m[r], top[r]), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[r] - to);
                 l[r] *= f;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) low[r][g] *= f;
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) acc[dt][r] *= f;
-                m[r] = mn[r];
+                m[r] = to;
             }
         }
         // weights
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int r = 0; r < R; ++r) {
+            const float ref = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float e = __builtin_amdgcn_exp2f(z[i][r] - (m[r] == -INFINITY ? 0.f : m[r]));
+            for (int i = 0; i < 4; ++i) {
+                const float e = __builtin_amdgcn_exp2f(z[i][r] - ref);
                 l[r] += e;
                 z[i][r] = e;
             }
-        const int slot = ((n >> 3) << 3) + ((n & 3) << 1) + ((n >> 2) & 1);           // of a key in its run of 16: as expand orders the codes
+        }
+        auto put_weights = [&](int g) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float s = scale_at<T>(vs[i], g), lw = __builtin_fmaf(-16.f, s, scale_at<T>(vs[i], NG + g));
+            for (int i = 0; i < 4; i += 2) {
+                const float s0 = scale_at<T>(vs[i], g), s1 = scale_at<T>(vs[i + 1], g);
+                const float l0 = __builtin_fmaf(-16.f, s0, scale_at<T>(vs[i], NG + g)), l1 = __builtin_fmaf(-16.f, s1, scale_at<T>(vs[i + 1], NG + g));
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    low[r][g] = __builtin_fmaf(z[i][r], lw, low[r][g]);
-                    const float w = z[i][r] * s;
-                    const unsigned short h = T::bits(w);
-                    const unsigned short d = T::bits(w - T::lo(h));
-                    const int at = (4 * c + r) * kRowStride + 32 * i + 2 * slot;
-                    *reinterpret_cast<unsigned short *>(w_hi + at) = h;
-                    *reinterpret_cast<unsigned short *>(w_lo + at) = d;
+                    low[r][g] = __builtin_fmaf(z[i][r], l0, low[r][g]);
+                    low[r][g] = __builtin_fmaf(z[i + 1][r], l1, low[r][g]);
+                    const float w0 = z[i][r] * s0, w1 = z[i + 1][r] * s1;
+                    const unsigned h = T::pack(w0, w1);
+                    unsigned char *at = w_at + (g & 1) * kTurn + (R * c + r) * kRowStride + 32 * i + 4 * n;
+                    *reinterpret_cast<unsigned *>(at) = h;
+                    *reinterpret_cast<unsigned *>(at + kLo) = T::pack(w0 - T::lo(h), w1 - T::hi(h));
                 }
             }
-            wave_fence();
-            // keys 16 c + 8 u .. + 7 of row n
-            u32x4_t ah[2], al[2];
+        };
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
+        // 16 elements from 16 dt of this lane's row: lane n receives element n of the 16 rows
+        auto read_v = [&](int dt) {
+            return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2)(v_row + buffer * (kBlock * 64) + (((dt >> 1) ^ v_turn) << 4) + ((dt & 1) << 3)));
+        };
+        i32x2 vc[2][2];                                                                // of elements 32 pr .. + 31, two in turn
+        vc[0][0] = read_v(0);
+        vc[0][1] = read_v(1);
+        put_weights(0);
+        u32x4_t e[2][2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                ah[u] = *reinterpret_cast<const u32x4_t *>(w_hi + n * kRowStride + 32 * c + 16 * u);
-                al[u] = *reinterpret_cast<const u32x4_t *>(w_lo + n * kRowStride + 32 * c + 16 * u);
-            }
+        for (int d = 0; d < 2; ++d)
 #pragma unroll
-            for (int d = 0; d < 8 / NG; ++d) {
-                const int dt = g * (8 / NG) + d;
-                typedef int i32x2 __attribute__((ext_vector_type(2)));
-                typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
-                // 16 elements from 16 dt of key 16 c + n: lane n receives element n of the 16 keys
-                unsigned char *at = v_at + (16 * c + n) * 64 + (((dt >> 1) ^ ((n >> 2) & 3)) << 4) + (((dt & 1) ^ (c & 1)) << 3);
-                const i32x2 x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2)at);
+            for (int u = 0; u < 2; ++u) e[d][u] = expand<T>((unsigned)vc[0][d][u], sixteen);
+        u32x4_t ah[2], al[2];
+#pragma unroll
+        for (int pr = 0; pr < 4; ++pr) {
+            const int g = pr * NG / 4;
+            if (pr % (4 / NG) == 0) {
+                wave_fence();
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const u32x4_t vb = expand<T>((unsigned)x[u]);
-                    acc[dt] = T::mfma(ah[u], vb, acc[dt]);
-                    acc[dt] = T::mfma(al[u], vb, acc[dt]);
+                    const unsigned char *at = w_at + (g & 1) * kTurn + w_row + 32 * c + 16 * u;
+                    ah[u] = *reinterpret_cast<const u32x4_t *>(at);
+                    al[u] = *reinterpret_cast<const u32x4_t *>(at + kLo);
+                }
+                if (g + 1 < NG) put_weights(g + 1);
+                if (g == NG - 1 && next < end) {
+                    load_scales(p.pool.v_scales, vs);
+                    load_pages(next + 4 * kBlock);
                 }
             }
-            wave_fence();
+            if (pr < 3) {
+                vc[(pr + 1) & 1][0] = read_v(2 * pr + 2);
+                vc[(pr + 1) & 1][1] = read_v(2 * pr + 3);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            u32x4_t en[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = T::mfma(ah[u], e[d][u], acc[2 * pr + d]);
+#pragma unroll
+                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = T::mfma(al[u], e[d][u], acc[2 * pr + d]);
+            }
+            if (pr < 3) {
+#pragma unroll
+                for (int d = 0; d < 2; ++d)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) en[d][u] = expand<T>((unsigned)vc[(pr + 1) & 1][d][u], sixteen);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < 2; ++d)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) e[d][u] = en[d][u];
         }
+        wave_fence();
     }
 
     // the four wavefronts' sums: lane (n, c) holds element 16 dt + n of rows 4 c + r
@@ -380,15 +498,16 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
         for (int g = 0; g < NG; ++g) lw[g] = row16_sum(low[r][g]);
         if (n == 0) {
-            lds.m[wave][4 * c + r] = m[r];
-            lds.l[wave][4 * c + r] = ls;
+            lds.m[wave][R * c + r] = m[r];
+            lds.l[wave][R * c + r] = ls;
         }
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) lds.rows[wave][4 * c + r][16 * dt + n] = acc[dt][r] + lw[dt * NG / 8];
+        for (int dt = 0; dt < 8; ++dt) lds.rows[wave][R * c + r][16 * dt + n] = acc[dt][r] + lw[dt * NG / 8];
     }
     __syncthreads();
-    for (int i = tid; i < heads * (kHeadDim / 2); i += 256) {
-        const int h = i >> 6, d = (i & 63) * 2, row = 4 * (h & 3) + (h >> 2);
+    const int chunks = (len + p.C - 1) / p.C;                              // of this sequence
+    for (int h = wave; h < heads; h += 4) {
+        const int row = R * (h & 3) + (h >> 2);
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.m[w][row]);
@@ -398,19 +517,54 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
             const float mw = lds.m[w][row];
             // a wavefront without keys has m = -inf and zeros; one whose logits are all -inf or NaN has NaN, and keeps it
             const float f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top);
-            const float2 x = *reinterpret_cast<const float2 *>(&lds.rows[w][row][d]);
+            const float2 x = *reinterpret_cast<const float2 *>(&lds.rows[w][row][2 * lane]);
             a0 = __builtin_fmaf(x.x, f, a0);
             a1 = __builtin_fmaf(x.y, f, a1);
             sum = __builtin_fmaf(lds.l[w][row], f, sum);
         }
         const size_t out_row = (size_t)b * p.Hq + head0 + h;
-        if (p.nc == 1) {
+        if (chunks == 1) {
             const float inv = 1.f / sum;
-            *reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim + d) = T::pack(a0 * inv, a1 * inv);
+            reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
         } else {
-            *reinterpret_cast<float2 *>(p.num + (out_row * p.nc + chunk) * kHeadDim + d) = float2{a0, a1};
-            if (d == 0) p.ml[out_row * p.nc + chunk] = float2{top, sum};
+            // (past the caches, in case a workgroup on another XCD joins the row in this launch)
+            const size_t slot = out_row * p.nc + chunk;
+            store_coherent2(p.num + slot * kHeadDim + 2 * lane, a0, a1);
+            if (lane == 0) store_coherent2(reinterpret_cast<float *>(p.ml + slot), top, sum);
         }
+    }
+    if (!p.counters || chunks == 1) return;
+    // The workgroup of the group's last chunk to arrive joins its rows: a round trip to memory for the stores, one for the counter, one for the partial results.
+    wait_stores_performed();
+    __syncthreads();
+    if (tid == 0) {
+        const int arrived = __hip_atomic_fetch_add(p.counters + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lds.last = arrived == chunks - 1;
+        if (arrived == chunks - 1) store_coherent(p.counters + group, 0);          // ready for the next call
+    }
+    __syncthreads();
+    if (!lds.last) return;
+    for (int h = wave; h < heads; h += 4) {
+        const size_t out_row = (size_t)b * p.Hq + head0 + h, slot = out_row * p.nc;
+        // chunk i's reference and denominator in lane i of every 16; all partial vectors under way before the first is used
+        unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + min(n, chunks - 1))), x[kJoinInPlace];
+#pragma unroll
+        for (int i = 0; i < kJoinInPlace; ++i)
+            x[i] = load_coherent(reinterpret_cast<const unsigned long long *>(p.num + (slot + min(i, chunks - 1)) * kHeadDim) + lane);
+        const float mi = n < chunks ? as_f32((unsigned)s) : -INFINITY, top = row16_max(mi);
+        const float f = n >= chunks ? 0.f : mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+        const float sum = row16_sum(n < chunks ? as_f32((unsigned)(s >> 32)) * f : 0.f);
+        float a0 = 0.f, a1 = 0.f;
+        each16(std::make_integer_sequence<int, kJoinInPlace>{}, [&](auto of) {
+            constexpr int i = decltype(of)::value;
+            if (i < chunks) {
+                const float fi = row16_lane<i>(f);
+                a0 = __builtin_fmaf(as_f32((unsigned)x[i]), fi, a0);
+                a1 = __builtin_fmaf(as_f32((unsigned)(x[i] >> 32)), fi, a1);
+            }
+        });
+        const float inv = 1.f / sum;
+        reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
     }
 }
 
@@ -424,7 +578,7 @@ template <class T, int DIM> __global__ __launch_bounds__(DIM / 2) void join_kern
     const int row = blockIdx.x, b = row / p.H, tid = threadIdx.x, lane = tid & 63;
     const int len = min(max(p.seq_lens[b], 0), p.Smax), nb = (len + p.C - 1) / p.C;
     unsigned *out = reinterpret_cast<unsigned *>(p.out + (size_t)row * DIM) + tid;
-    if (nb == 0) { *out = 0u; return; }
+    if (nb <= 1) return;                                        // done by the launch before
     const float2 *ml = p.ml + (size_t)row * p.nc;
     const float *num = p.num + (size_t)row * p.nc * DIM + 2 * tid;
     float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
@@ -497,10 +651,12 @@ hipError_t launch_join(const JoinProblem &p, hipStream_t s)
         return p.dtype == kF16 ? launch(join_kernel<F16, kHeadDim>, grid, block, s, p) : launch(join_kernel<BF16, kHeadDim>, grid, block, s, p);
     return p.dtype == kF16 ? launch(join_kernel<F16, 512>, grid, block, s, p) : launch(join_kernel<BF16, 512>, grid, block, s, p);
 }
-hipError_t launch_nibble_attn(const NibbleProblem &p, hipStream_t s)
+hipError_t launch_nibble_attn(const NibbleProblem &p_, hipStream_t s)
 {
+    NibbleProblem p = p_;
+    if (p.nc > kJoinInPlace) p.counters = nullptr;
     const hipError_t e = p.pool.dtype == kF16 ? attn_groups<F16>(p, s) : attn_groups<BF16>(p, s);
-    if (e != hipSuccess || p.nc == 1) return e;
+    if (e != hipSuccess || p.nc == 1 || p.counters) return e;
     JoinProblem j{p.num, p.ml, p.seq_lens, p.out, p.B * p.Hq, p.Hq, p.C, p.nc, p.Smax, kHeadDim, p.pool.dtype};
     return launch_join(j, s);
 }

@@ -128,6 +128,7 @@ def _bind(lib):
         getattr(lib, _name).restype = ctypes.c_int32
         getattr(lib, _name).argtypes = [_sp]
     for _name, _args in (("fd_page_tables", [i32] * 5 + [_vp] * 10),
+                         ("fd_cache_workspace_init", [Workspace, _vp]),
                          ("fd_nibble_write", [nibble, _vp, i64, _vp, i64, i32, _vp, _vp]),
                          ("fd_nibble_read", [nibble, _vp, i32, _vp, i64, _vp, i64, _vp]),
                          ("fd_decode_attn_nibble", [_sp, nibble, _vp, _vp, _vp, _vp, Workspace, _vp]),
@@ -145,7 +146,7 @@ EXPORTS = ("fd_decode_attn_static", "fd_decode_attn_paged", "fd_decode_attn_page
            "fd_decode_attn_multikernel", "fd_decode_attn_sync", "fd_list_flagged_rows",
            "fd_decode_attn_partial", "fd_decode_attn_gqa_partial", "fd_get_flags", "fd_get_partials",
            "fd_status_str", "fd_page_tables", "fd_nibble_write", "fd_nibble_read", "fd_nibble_workspace_bytes", "fd_nibble_pick_chunk",
-           "fd_decode_attn_nibble", "fd_latent_write", "fd_latent_workspace_bytes", "fd_latent_pick_chunk", "fd_latent_decode_attn",
+           "fd_cache_workspace_init", "fd_decode_attn_nibble", "fd_latent_write", "fd_latent_workspace_bytes", "fd_latent_pick_chunk", "fd_latent_decode_attn",
            "fd_latent_prefill_attn")
 
 
@@ -295,6 +296,10 @@ def fd_nibble_write(pool, k, k_stride, v, v_stride, n_tokens, slot_map, stream=0
 
 def fd_nibble_read(pool, slot_map, n_tokens, k, k_stride, v, v_stride, stream=0):
     _check(_lib.fd_nibble_read(ctypes.byref(pool), slot_map, int(n_tokens), k, int(k_stride), v, int(v_stride), stream))
+
+
+def fd_cache_workspace_init(ws_ptr, ws_bytes, stream=0):
+    _check(_lib.fd_cache_workspace_init(Workspace(ws_ptr, ws_bytes), stream))
 
 
 def fd_nibble_workspace_bytes(shape):

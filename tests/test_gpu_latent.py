@@ -47,7 +47,9 @@ def decode(rows, table, lens, ql, qr, chunk, max_seq, scale, out=None, ws=None):
         assert shape.chunk % 32 == 0 and shape.chunk >= 32
     nbytes = fd.fd_latent_workspace_bytes(shape)
     assert nbytes > 0
-    ws = torch.full((nbytes,), 0xFF, dtype=torch.uint8, device=DEV) if ws is None else ws
+    if ws is None:
+        ws = torch.full((nbytes,), 0xFF, dtype=torch.uint8, device=DEV)
+        fd.fd_cache_workspace_init(ws.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream)
     out = torch.full((batch + 1, heads, 512), float("nan"), dtype=rows.dtype, device=DEV) if out is None else out
     pool = fd.make_latent_pool(rows.data_ptr(), rows.shape[0], rows.shape[1], 512, 64, of(rows.dtype))
     fd.fd_latent_decode_attn(shape, pool, ql.data_ptr(), qr.data_ptr(), table.data_ptr(), lens.data_ptr(), out.data_ptr(), ws.data_ptr(),
@@ -130,7 +132,7 @@ def test_decode_replays():
     ql, qr = queries(4, 3, 32, torch.float16)
     dr, dt, dl = rows.to(DEV), table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV)
     out = decode(dr, dt, dl, ql, qr, 128, max_seq, 0.07)
-    ws = torch.empty(lib().fd_latent_workspace_bytes(lib().make_shape(3, 32, 1, 576, max_seq, 128, 0.07)), dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(lib().fd_latent_workspace_bytes(lib().make_shape(3, 32, 1, 576, max_seq, 128, 0.07)), dtype=torch.uint8, device=DEV)
     torch.cuda.synchronize()
     side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):

@@ -160,7 +160,9 @@ def attend(pool, table, lens, q, chunk, max_seq, scale, out=None, ws=None, strea
     shape = fd.make_shape(batch, hq, pool.hkv, 128, max_seq, chunk, scale)
     nbytes = fd.fd_nibble_workspace_bytes(shape)
     assert nbytes > 0
-    ws = torch.full((nbytes,), 0xFF, dtype=torch.uint8, device=DEV) if ws is None else ws        # NaN wherever it is not written
+    if ws is None:
+        ws = torch.full((nbytes,), 0xFF, dtype=torch.uint8, device=DEV)        # NaN wherever it is not written
+        fd.fd_cache_workspace_init(ws.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream)
     out = torch.full((batch + 1, hq, 128), float("nan"), dtype=pool.dtype, device=DEV) if out is None else out
     fd.fd_decode_attn_nibble(shape, pool.handle(), q.data_ptr(), table.data_ptr(), lens.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel(),
                           (stream or torch.cuda.current_stream()).cuda_stream)
@@ -265,7 +267,7 @@ def test_another_stream_and_replays():
     torch.cuda.synchronize()
     out = torch.full_like(eager, float("nan"))
     shape = lib().make_shape(3, 16, 2, 128, max_seq, 128, 0.1)
-    ws = torch.empty(lib().fd_nibble_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(lib().fd_nibble_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
     side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):
         attend(pool, dt, dl, q, 128, max_seq, 0.1, out, ws)

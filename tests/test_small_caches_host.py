@@ -175,6 +175,11 @@ def test_latent_prefill_attn():
     assert call(changed(SHAPE_P, batch=0)) == fd.FD_OK
 
 
+def test_workspace_init():
+    init = lambda ptr, n: status(fd.fd_cache_workspace_init, ptr, n)      # noqa: E731
+    assert init(None, 1 << 20) == WORKSPACE and init(P + 128, 1 << 20) == WORKSPACE and init(P, 4 * 4096 - 1) == WORKSPACE
+
+
 def test_workspaces_grow_with_the_split():
     a, b = (fd.fd_nibble_workspace_bytes(fd.make_shape(**changed(SHAPE4, chunk=c))) for c in (1024, 64))
     assert 0 < a <= b and b >= 2 * 8 * 16 * (128 + 2) * 4
