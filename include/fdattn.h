@@ -580,7 +580,7 @@ fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_
 /*
  * Decode attention in the absorbed form: x_j = scale (q_latent . latent_j + q_rope . rope_j), out = sum_j softmax(x)_j latent_j, the
  * queries taken into the latent space by the caller, who takes the output out of it.
- * q_latent, out [batch, n_q_heads, 512], q_rope [batch, n_q_heads, 64].  shape: n_kv_heads 1, head_dim 576; chunk a multiple of 32 from 32 to
+ * q_latent, out [batch, n_q_heads, 512], q_rope [batch, n_q_heads, 64].  shape: n_kv_heads 1, head_dim 576; chunk a multiple of 64 from 64 to
  * 16384 keys, for example fd_latent_pick_chunk(shape).  A sequence of length 0 gives zero rows.  Scores and sums in fp32; the weights
  * enter the second product as two numbers of dtype each, of more than 64 heads as one (the denominator is then the sum of the rounded ones).
  */

@@ -112,7 +112,7 @@ inline bool bad_ws(fd_workspace ws, const Split &S) { return !ws.ptr || off(ws.p
 fd_status nibble_split(const fd_shape *sh, Split *S) { return split(sh, fd::kHeadDim, fd::kHeadDim, 64, S); }
 fd_status latent_split(const fd_shape *sh, Split *S)
 {
-    const fd_status st = split(sh, fd::kLatentRow, fd::kLatent, 32, S);
+    const fd_status st = split(sh, fd::kLatentRow, fd::kLatent, 64, S);
     if (st != FD_OK) return st;
     return sh->n_kv_heads == 1 ? FD_OK : FD_ERR_UNSUPPORTED;
 }
@@ -196,7 +196,16 @@ int32_t fd_nibble_pick_chunk(const fd_shape *shape)
 {
     if (check_shape(shape, fd::kHeadDim) != FD_OK) return 0;
     const long long units = (long long)shape->batch * shape->n_kv_heads * ((shape->n_q_heads / shape->n_kv_heads + 15) / 16);
-    return chunk_for(shape->max_seq, units, 1024, 256, 64);
+    // Two workgroups fit a compute unit, and a launch of one round of them is the fastest there is, ragged or not: a workgroup's beginning and end cost as much as
+    // three blocks of its four wavefronts.  Up to there 1024 keys are the best length where they fill the chip once, otherwise what does, down to a block a wavefront.
+    // (Whole call, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 16 x 32 heads x 2000 44 / 37.7 / 33.7 / *30.2, 64 x 32/8 x 4000 95 / 72 / 64 / 60 / *56.4, 32 x 32/8
+    // x 2000 33.5 / 27.4 / *22.9 / 23.3, 1 x 32 x 8192 21.7 / 16.7 / *15.9 / 21.8 / 35.6, 8 x 32/8 x 4000 17.8 / 14.4 / *14.0 / 18.2 / 26.7, 4 x 64/8 x 2000 *11.3 / 12.9 / 17.0.)
+    const long long chip = fd::kComputeUnits, rows = units > 0 ? units : 1;
+    for (int32_t c : {1024, 512, 256}) {
+        const long long w = rows * (((long long)shape->max_seq + c - 1) / c);
+        if (w <= 2 * chip && (w >= chip || c == 256)) return c;
+    }
+    return chunk_for(shape->max_seq, rows, 2 * chip, 256, 256);
 }
 
 fd_status fd_decode_attn_nibble(const fd_shape *shape, const fd_nibble_pool *pool, const void *q, const int32_t *block_table,
@@ -252,10 +261,18 @@ size_t fd_latent_workspace_bytes(const fd_shape *shape)
 int32_t fd_latent_pick_chunk(const fd_shape *shape)
 {
     if (check_shape(shape, fd::kLatentRow) != FD_OK || shape->n_kv_heads != 1) return 0;
-    // a workgroup takes up to 64 heads, and two of them fit a compute unit, or, of more than 64, up to 128
-    const bool many = shape->n_q_heads > 64;
-    const long long units = (long long)shape->batch * ((shape->n_q_heads + 127) / 128);
-    return chunk_for(shape->max_seq, units, many ? 256 : 512, 64, 32);
+    // A chunk of c keys takes c / 32 tiles of about 1 us (1.4 of 64 heads, 1.5 of 128), and every workgroup leaves 2 KiB of sums a head, written and read again: about
+    // 0.07 us for 128 heads.  The sum of the two is least near sqrt(k units max_seq) keys; a row of many pieces takes its join 0.07 us for each, which
+    // adds sqrt(2.2 max_seq); and more than one workgroup a compute unit gains nothing.  A row that would be cut into little goes in one piece, without the join's launch.
+    // (Whole call, chunks of 64 / 128 / 256 / 512 / 1024 keys: 8 x 128 heads x 4000 77 / 46 / 41.7 / 51 / 73 us, 1 x 16 x 30000 50 / 33 / 27.4 / 31 / 45, 64 x 64 x 4000 - / - / 124 / 99 / 89,
+    // 128 x 16 x 300 29 / 26 / 25.5 / 19.5.)
+    const double units = (double)shape->batch * ((shape->n_q_heads + 127) / 128), S = shape->max_seq;
+    const double k = shape->n_q_heads > 64 ? 1.5 : shape->n_q_heads / 76.0;
+    const double c = std::fmax(std::fmax(units * S / fd::kComputeUnits, std::sqrt(k * units * S)), std::sqrt(2.2 * S));
+    long long nc = (long long)(S / c);
+    if (nc < 2 || S * (1.0 - 1.0 / (double)nc) < 192.0) nc = 1;
+    const long long chunk = (((long long)shape->max_seq + nc - 1) / nc + 63) / 64 * 64;
+    return (int32_t)(chunk > 16384 ? 16384 : chunk);
 }
 
 fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *pool, const void *q_latent, const void *q_rope,

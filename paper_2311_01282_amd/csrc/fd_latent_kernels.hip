@@ -34,8 +34,9 @@ __global__ __launch_bounds__(256) void latent_write_kernel(LatentPool pool, cons
 // The weights enter as the sum of two numbers of the type (hi + lo), since one alone adds an error as large as the output's rounding, and the second
 // half of the instructions is hidden behind memory; of more than 64 heads, where the matrix cores are the bound, as one, and their sum is that of the rounded
 // ones (64 x 128 heads x 4096 keys: 106 us with two, 93 with one).
-// A wavefront owns 16 heads: 72 registers of queries and 128 of sums.  A workgroup of NH wavefronts takes 16 NH heads of a sequence and a chunk of its keys,
-// TPW tiles of 32 at a time, which all its wavefronts fetch straight into LDS while they work on those before.
+// A wavefront owns 16 heads: 72 registers of queries and 128 of sums.  A workgroup of NW wavefronts takes 16 NH heads of a sequence and a chunk of its keys,
+// TPW tiles of 32 at a time, which all its wavefronts fetch straight into LDS while they work on those before.  Where there are fewer heads than wavefronts, DS = NW / NH
+// of them share 16 heads: all form the weights, each adds up its part of the elements.
 constexpr int kTile = 32;
 // The reference of a head's weights follows its maximum only where that has grown by more than this (in units of log2): weights are at most 2^8 then, and
 // the sums, 128 registers of a wavefront, are brought to another reference once or twice a chunk; of 16 heads some maximum grows in most tiles.
@@ -43,9 +44,12 @@ constexpr float kSlack = 8.f;
 constexpr int kRowBytes = kLatentRow * 2;                      // in the cache
 constexpr int kCBytes = kLatent * 2, kRBytes = kRope * 2;      // in LDS the two parts of a row lie apart
 
+// Steps in LDS: one in work, one under way.  Two workgroups of up to 64 heads fit a compute unit, which covers the loads better than one with four steps: 16 x 64 heads x 2000 keys
+// 30.1 / 31.7 us, 64 x 16 x 1000 25.3 / 26.9; in long launches it is the other way round, 64 x 64 x 4000 88.7 / 86.6.
+constexpr int kSteps = 2;
 template <int TPW> struct LatentLds {
-    alignas(256) unsigned char c[2][TPW * kTile * kCBytes];    // piece x (16 bytes) of row r in place x ^ c_key(r)
-    alignas(256) unsigned char r[2][TPW * kTile * kRBytes];    // ... x ^ r_key(r)
+    alignas(256) unsigned char c[kSteps * TPW][kTile * kCBytes];      // piece x (16 bytes) of row r in place x ^ c_key(r)
+    alignas(256) unsigned char r[kSteps * TPW][kTile * kRBytes];      // ... x ^ r_key(r)
 };
 // A cycle of the 16-byte operand reads holds every n once, from two neighbouring g: with these keys the 16 pieces lie in 16 different places modulo 256 bytes.  The
 // transposing reads take 32 bytes of eight rows at a time, 8 g + 4 h + (0 .. 3) of two neighbouring g: in eight different places.  Rows r and r + 4 have the same keys.
@@ -75,16 +79,18 @@ typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
 typedef __attribute__((address_space(3))) const u32x4_t *lds_u32x4;
 typedef __attribute__((address_space(4))) const int32_t *scalar_i32;      // read through the scalar cache
 
-template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) void latent_decode_kernel(LatentProblem p)
+template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW, 2) void latent_decode_kernel(LatentProblem p)
 {
-    constexpr bool kTwoParts = NH < 8;                         // of a weight
-    constexpr int kKeys = TPW * kTile, kRows = kKeys / NH;     // keys of a step; rows that a wavefront fetches
+    constexpr int NH = NW / DS, kDt = 32 / DS;                 // groups of 16 heads; tiles of 16 elements of a wavefront
+    constexpr bool kTwoParts = NW < 8;                         // of a weight
+    constexpr int kKeys = TPW * kTile, kRows = kKeys / NW;     // keys of a step; rows that a wavefront fetches
     constexpr int kHalves = (kRows + 15) / 16;                 // ... from so many places of 16 rows
+    constexpr int kLoads = kRows / 8 * 9;                      // fetches of a wavefront a step
     __shared__ LatentLds<TPW> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     // workgroups that read the same rows lie on one XCD (index modulo 8), one after the other
     const int tiles = (p.H + 16 * NH - 1) / (16 * NH), units = p.B * p.nc;
-    const int unit = (blockIdx.x / (8 * tiles)) * 8 + blockIdx.x % 8, head0 = (blockIdx.x / 8 % tiles) * (16 * NH) + 16 * wave;
+    const int unit = (blockIdx.x / (8 * tiles)) * 8 + blockIdx.x % 8, head0 = (blockIdx.x / 8 % tiles) * (16 * NH) + 16 * (wave % NH), d0 = wave / NH * (16 * kDt);
     if (unit >= units) return;
     const int chunk = unit % p.nc, b = unit / p.nc;
     const int start = chunk * p.C, shift = p.pool.page_shift, mask = (1 << shift) - 1;
@@ -99,7 +105,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
     const int heads = min(p.H - head0, 16);                    // of this wavefront; may be 0 or less: it only fetches
     if (start >= end) {
         if (chunk == 0)                                        // no keys at all: zero rows
-            for (int h = 0; h < heads; ++h)
+            for (int h = wave / NH; h < heads; h += DS)
                 reinterpret_cast<u32x4_t *>(p.out + ((size_t)b * p.H + head0 + h) * kLatent)[lane] = u32x4_t{0u, 0u, 0u, 0u};
         return;
     }
@@ -110,7 +116,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
     auto fetch = [&](int s) {
         int l0 = lane;
         asm volatile("" : "+v"(l0));    // (offsets are formed anew each time: there are no registers to keep them in)
-        const unsigned to_c = lds_c + (s & 1) * (kKeys * kCBytes) + wave * (kRows * kCBytes), to_r = lds_r + (s & 1) * (kKeys * kRBytes) + wave * (kRows * kRBytes);
+        const unsigned to_c = lds_c + s % kSteps * (kKeys * kCBytes) + wave * (kRows * kCBytes), to_r = lds_r + s % kSteps * (kKeys * kRBytes) + wave * (kRows * kRBytes);
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
             const int key0 = start + s * kKeys + wave * kRows + 16 * h;
@@ -143,25 +149,28 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
             q[kb] = *reinterpret_cast<const u32x4_t *>(kb < 16 ? p.q_latent + row * kLatent + 32 * kb + 8 * g : p.q_rope + row * kRope + 32 * (kb - 16) + 8 * g);
         }
     }
-    f32x4_t acc[32];
+    f32x4_t acc[kDt];
 #pragma unroll
-    for (int dt = 0; dt < 32; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int dt = 0; dt < kDt; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     const float c1 = p.scale * kLog2e;
     // this lane's operand reads: piece 4 kb + g of row k_row; 32 bytes from element 16 dt of row v_row.  Pieces within 256 bytes differ by an exclusive or.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
     const unsigned k_at = k_row * kCBytes + ((g ^ c_key(k_row)) << 4), kr_at = k_row * kRBytes + ((g ^ r_key(k_row)) << 4);
     const unsigned v_at = v_row * kCBytes + (((n >> 1) & 1) << 4) + ((n & 1) << 3) + (c_key(v_row) << 4);
-    __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries (the compiler does not count the fetches)
+
+    __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries, and with them step 0 (the compiler, which does not count the fetches, would wait within the loop)
+#pragma unroll
+    for (int s = 1; s < kSteps - 1; ++s) fetch(s);
 
     for (int s = 0; s < steps; ++s) {
-        wait_fetches<0>();                                     // step s
+        wait_fetches<(kSteps - 2) * kLoads>();                 // step s (those behind the last one are fetched too: nothing, that is, and the count is the same)
         tile_barrier();                                        // ... for every wavefront, all of which are through with step s - 1
-        if (s + 1 < steps) fetch(s + 1);
+        fetch(s + kSteps - 1);
         if (heads <= 0) continue;
 #pragma unroll 1
         for (int i = 0; i < TPW; ++i) {
-            const unsigned tile_c = lds_c + ((s & 1) * TPW + i) * (kTile * kCBytes), tile_r = lds_r + ((s & 1) * TPW + i) * (kTile * kRBytes);
+            const unsigned tile_c = lds_c + (s % kSteps * TPW + i) * (kTile * kCBytes), tile_r = lds_r + (s % kSteps * TPW + i) * (kTile * kRBytes);
             f32x4_t sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
             {
                 const unsigned kc = tile_c + k_at, kr = tile_r + kr_at;
@@ -187,7 +196,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            const unsigned vc = tile_c + v_at;
+            const unsigned vc = tile_c + v_at + 2 * d0;
             auto read = [&](int dt) {
                 const unsigned x = (vc ^ ((dt & 7) << 5)) + ((dt >> 3) << 8);
                 const s16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)x);
@@ -213,7 +222,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
                 const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
                 l *= f;
 #pragma unroll
-                for (int dt = 0; dt < 32; ++dt)
+                for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[dt][r] *= f;
                 m = to;
@@ -233,10 +242,10 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
                 }
             }
 #pragma unroll
-            for (int dt = 0; dt < 32; dt += 2) {
+            for (int dt = 0; dt < kDt; dt += 2) {
 #pragma unroll
                 for (int d = 0; d < 2; ++d)
-                    if (dt + d + kAhead < 32) a[(dt + d + kAhead) % (kAhead + 2)] = read(dt + d + kAhead);
+                    if (dt + d + kAhead < kDt) a[(dt + d + kAhead) % (kAhead + 2)] = read(dt + d + kAhead);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(dt + d) % (kAhead + 2)], hi, acc[dt + d]);
@@ -247,6 +256,7 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
             }
         }
     }
+    wait_fetches<0>();                                         // (nothing may land in LDS after the workgroup's end)
     if (n >= heads) return;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -254,25 +264,28 @@ template <class T, int NH, int TPW> __global__ __launch_bounds__(64 * NH, 2) voi
     if (len <= p.C) {                                          // the only chunk with keys
         const float inv = 1.f / l;
 #pragma unroll
-        for (int dt = 0; dt < 32; ++dt)
-            *reinterpret_cast<u32x2_t *>(p.out + row * kLatent + 16 * dt + 4 * g) =
+        for (int dt = 0; dt < kDt; ++dt)
+            *reinterpret_cast<u32x2_t *>(p.out + row * kLatent + d0 + 16 * dt + 4 * g) =
                 u32x2_t{T::pack(acc[dt][0] * inv, acc[dt][1] * inv), T::pack(acc[dt][2] * inv, acc[dt][3] * inv)};
     } else {
         float *num = p.num + (row * p.nc + chunk) * kLatent;
 #pragma unroll
-        for (int dt = 0; dt < 32; ++dt) *reinterpret_cast<f32x4_t *>(num + 16 * dt + 4 * g) = acc[dt];
-        if (g == 0) p.ml[row * p.nc + chunk] = float2{m, l};
+        for (int dt = 0; dt < kDt; ++dt) *reinterpret_cast<f32x4_t *>(num + d0 + 16 * dt + 4 * g) = acc[dt];
+        if (g == 0 && d0 == 0) p.ml[row * p.nc + chunk] = float2{m, l};
     }
 }
 
-template <class T, int NH, int TPW> hipError_t decode(const LatentProblem &p, hipStream_t s)
+template <class T, int NW, int DS, int TPW> hipError_t decode(const LatentProblem &p, hipStream_t s)
 {
-    const long long tiles = (p.H + 16 * NH - 1) / (16 * NH), units = (long long)p.B * p.nc;
-    return launch(latent_decode_kernel<T, NH, TPW>, dim3((unsigned)((units + 7) / 8 * 8 * tiles)), dim3(64 * NH), s, p);
+    constexpr int heads = 16 * NW / DS;
+    const long long tiles = (p.H + heads - 1) / heads, units = (long long)p.B * p.nc;
+    return launch(latent_decode_kernel<T, NW, DS, TPW>, dim3((unsigned)((units + 7) / 8 * 8 * tiles)), dim3(64 * NW), s, p);
 }
 template <class T> hipError_t decode_heads(const LatentProblem &p, hipStream_t s)
 {
-    return p.H > 64 ? decode<T, 8, 2>(p, s) : decode<T, 4, 1>(p, s);
+    if (p.H > 64) return decode<T, 8, 1, 2>(p, s);
+    if (p.H > 32) return decode<T, 4, 1, 1>(p, s);
+    return p.H > 16 ? decode<T, 4, 2, 1>(p, s) : decode<T, 4, 4, 1>(p, s);
 }
 
 }  // namespace

@@ -134,6 +134,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 // a chunk and a partial result each, did 32 x 64/8 heads x 4096 keys in 38.5 us at their best chunk, these in 35.4.)  Of the 64, operand u of
 // lanes c takes keys of two tiles, 2 (c / 2) and the next, 8 (c % 2) + 4 u .. + 3 of each: what a lane has of the two tiles then lies side by side (expand's pairs).
 constexpr int kBlock = 64;                       // keys of a wavefront step
+constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
 constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
 // The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.
@@ -527,10 +528,15 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
             const float inv = 1.f / sum;
             reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
         } else {
-            // (past the caches, in case a workgroup on another XCD joins the row in this launch)
             const size_t slot = out_row * p.nc + chunk;
-            store_coherent2(p.num + slot * kHeadDim + 2 * lane, a0, a1);
-            if (lane == 0) store_coherent2(reinterpret_cast<float *>(p.ml + slot), top, sum);
+            float *num = p.num + slot * kHeadDim + 2 * lane, *ml = reinterpret_cast<float *>(p.ml + slot);
+            if (p.counters) {                                              // past the caches: a workgroup on another XCD may join the row
+                store_coherent2(num, a0, a1);
+                if (lane == 0) store_coherent2(ml, top, sum);
+            } else {
+                *reinterpret_cast<float2 *>(num) = float2{a0, a1};
+                if (lane == 0) *reinterpret_cast<float2 *>(ml) = float2{top, sum};
+            }
         }
     }
     if (!p.counters || chunks == 1) return;
@@ -569,24 +575,25 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 }
 
 // ---- the join of rows that several workgroups share ----
-// A workgroup a row.  Its length is that of its loads, so all of them are asked for together: first the references and denominators of 64 chunks, then, with
-// their factors in LDS, eight partial vectors at a time.
+// A workgroup a row, of several slices that take every kSlices-th eight of the partial vectors.  Its length is that of its loads, so as many as can be are asked for together:
+// first the references and denominators of 64 chunks, then, with their factors in LDS, eight vectors of a slice at a time.
 constexpr int kJoinWindow = 64;
-template <class T, int DIM> __global__ __launch_bounds__(DIM / 2) void join_kernel(JoinProblem p)
+template <class T, int DIM, int kSlices> __global__ __launch_bounds__(DIM / 2 * kSlices) void join_kernel(JoinProblem p)
 {
+    constexpr int kLanes = DIM / 2;
     __shared__ float factor[kJoinWindow];
-    const int row = blockIdx.x, b = row / p.H, tid = threadIdx.x, lane = tid & 63;
+    __shared__ float2 sums[kSlices][kLanes];
+    const int row = blockIdx.x, b = row / p.H, tid = threadIdx.x, lane = tid & 63, slice = tid / kLanes, at = tid % kLanes;
     const int len = min(max(p.seq_lens[b], 0), p.Smax), nb = (len + p.C - 1) / p.C;
-    unsigned *out = reinterpret_cast<unsigned *>(p.out + (size_t)row * DIM) + tid;
     if (nb <= 1) return;                                        // done by the launch before
     const float2 *ml = p.ml + (size_t)row * p.nc;
-    const float *num = p.num + (size_t)row * p.nc * DIM + 2 * tid;
+    const float *num = p.num + (size_t)row * p.nc * DIM + 2 * at;
     float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
     for (int w0 = 0; w0 < nb; w0 += kJoinWindow) {
         const int count = min(nb - w0, kJoinWindow);
         float2 s = {-INFINITY, 0.f};
         if (lane < count) s = ml[w0 + lane];
-        float t = columns_max(row16_max(s.x));
+        const float t = columns_max(row16_max(s.x));
         if (t > top) {                                          // (uniform) what the windows before left, to the new reference
             const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - t);
             a0 *= f;
@@ -602,7 +609,7 @@ template <class T, int DIM> __global__ __launch_bounds__(DIM / 2) void join_kern
         __syncthreads();                                        // (the factors of the window before are out of use)
         if (tid < kJoinWindow) factor[tid] = f;
         __syncthreads();
-        for (int i = 0; i < count; i += 8) {
+        for (int i = 8 * slice; i < count; i += 8 * kSlices) {
             float2 x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -615,8 +622,16 @@ template <class T, int DIM> __global__ __launch_bounds__(DIM / 2) void join_kern
                 }
         }
     }
+    sums[slice][at] = float2{a0, a1};
+    __syncthreads();
+    if (slice) return;
+#pragma unroll
+    for (int i = 1; i < kSlices; ++i) {
+        a0 += sums[i][at].x;
+        a1 += sums[i][at].y;
+    }
     const float inv = 1.f / sum;
-    *out = T::pack(a0 * inv, a1 * inv);
+    reinterpret_cast<unsigned *>(p.out + (size_t)row * DIM)[at] = T::pack(a0 * inv, a1 * inv);
 }
 
 template <class T, int NG> hipError_t attn_rows(const NibbleProblem &p, hipStream_t s)
@@ -644,17 +659,22 @@ hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hi
     const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 15) / 16));
     return pool.dtype == kF16 ? launch(nibble_read_kernel<F16>, grid, dim3(256), s, pool, rows) : launch(nibble_read_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
+template <class T, int DIM> static hipError_t join(const JoinProblem &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.rows);
+    // (of up to eight vectors a row every slice but one would be idle: 128 x 128 latent rows of two 83 us, with two slices 97)
+    return p.nc > 8 ? launch(join_kernel<T, DIM, 1024 / DIM>, grid, dim3(512), s, p) : launch(join_kernel<T, DIM, 1>, grid, dim3(DIM / 2), s, p);
+}
 hipError_t launch_join(const JoinProblem &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.rows), block((unsigned)p.dim / 2);
-    if (p.dim == kHeadDim)
-        return p.dtype == kF16 ? launch(join_kernel<F16, kHeadDim>, grid, block, s, p) : launch(join_kernel<BF16, kHeadDim>, grid, block, s, p);
-    return p.dtype == kF16 ? launch(join_kernel<F16, 512>, grid, block, s, p) : launch(join_kernel<BF16, 512>, grid, block, s, p);
+    if (p.dim == kHeadDim) return p.dtype == kF16 ? join<F16, kHeadDim>(p, s) : join<BF16, kHeadDim>(p, s);
+    return p.dtype == kF16 ? join<F16, kLatent>(p, s) : join<BF16, kLatent>(p, s);
 }
 hipError_t launch_nibble_attn(const NibbleProblem &p_, hipStream_t s)
 {
     NibbleProblem p = p_;
-    if (p.nc > kJoinInPlace) p.counters = nullptr;
+    // A workgroup that joins a unit's rows keeps the others of its compute unit waiting less than a second launch costs while there are few.
+    if (p.nc > kJoinInPlace || (long long)p.B * p.pool.Hkv * p.tiles * p.nc > kJoinWorkgroups) p.counters = nullptr;
     const hipError_t e = p.pool.dtype == kF16 ? attn_groups<F16>(p, s) : attn_groups<BF16>(p, s);
     if (e != hipSuccess || p.nc == 1 || p.counters) return e;
     JoinProblem j{p.num, p.ml, p.seq_lens, p.out, p.B * p.Hq, p.Hq, p.C, p.nc, p.Smax, kHeadDim, p.pool.dtype};

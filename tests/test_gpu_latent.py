@@ -44,7 +44,7 @@ def decode(rows, table, lens, ql, qr, chunk, max_seq, scale, out=None, ws=None):
     shape = fd.make_shape(batch, heads, 1, 576, max_seq, chunk, scale)
     if not chunk:
         shape.chunk = fd.fd_latent_pick_chunk(shape)
-        assert shape.chunk % 32 == 0 and shape.chunk >= 32
+        assert shape.chunk % 64 == 0 and shape.chunk >= 64
     nbytes = fd.fd_latent_workspace_bytes(shape)
     assert nbytes > 0
     if ws is None:
@@ -95,7 +95,7 @@ def test_heads(dtype, heads):
     rows, table = filled(dtype, lens, page, max_seq // page, heads)
     ql, qr = queries(heads, 4, heads, dtype)
     dl, dr = torch.tensor(lens, dtype=torch.int32, device=DEV), rows.to(DEV)
-    for chunk in (64, 224):
+    for chunk in (64, 256):
         got = decode(dr, table.to(DEV), dl, ql, qr, chunk, max_seq, 0.07)
         torch.cuda.synchronize()
         check(got, rows, table, lens, ql, qr, 0.07)
@@ -103,7 +103,7 @@ def test_heads(dtype, heads):
 
 
 @pytest.mark.parametrize("page", [16, 64, 512])
-@pytest.mark.parametrize("chunk", [32, 96, 160, 512, 1024, 0])
+@pytest.mark.parametrize("chunk", [64, 192, 320, 512, 1024, 0])
 def test_lengths_pages_and_chunks(page, chunk):
     lens = [1, 15, 16, 17, 31, 32, 33, 63, 65, 127, 128, 129, 500, 1023, 0, 1024, 5000, -3]
     max_seq = 1024
