@@ -8,6 +8,8 @@
 //   output   O^T[d][query] = V^T . P^T: A = V^T by the transposing LDS read.
 // Softmax with a running maximum per query; the weights are of the type (one rounding, as large as the output's own), their sum is that of the
 // rounded ones, in fp32.
+#include <utility>
+
 #include "fd_chunk.h"
 #include "fd_cache.h"
 #include "fd_types.h"
@@ -16,15 +18,15 @@ namespace fd {
 
 namespace {
 
-constexpr int kNope = 128, kQueryDim = kNope + kRope, kStep = 32, kTileQ = 128, kRing = 3;
+constexpr int kNope = 128, kQueryDim = kNope + kRope, kStep = 32, kTileQ = 128, kRingK = 4, kRingV = 3;
 // The reference of a query's weights follows its maximum only where that has grown by more than this (in units of log2): weights are then at
 // most 2^8, and the sums are brought to another reference a few times a row instead of at every new maximum.
 constexpr float kSlack = 8.f;
 
 struct PromptLds {
-    alignas(16) unsigned char k[kRing][kStep * kNope * 2];      // piece x (16 bytes) of row r in place x ^ key(r)
-    alignas(16) unsigned char r[kRing][kStep * kRope * 2];      // ... x ^ swizzle(r)
-    alignas(16) unsigned char v[kRing][kStep * kNope * 2];      // 32-byte unit x of row r in place x ^ v_unit(r)
+    alignas(256) unsigned char k[kRingK][kStep * kNope * 2];    // piece x (16 bytes) of row r in place x ^ k_place(r)
+    alignas(256) unsigned char r[kRingK][kStep * kRope * 2];    // ... x ^ r_place(r)
+    alignas(256) unsigned char v[kRingV][kStep * kNope * 2];    // 32-byte unit x of row r in place x ^ v_unit(r)
 };
 // With these the 16-byte operand reads, whose cycles hold every n once from two neighbouring g, and the transposing reads, which take 32 bytes of
 // rows 8 g + 4 h + (0 .. 3) of two neighbouring g at a time, have no bank conflicts.
@@ -32,11 +34,19 @@ __device__ __forceinline__ int k_place(int r) { return (r & 3) | (((r >> 3) & 3)
 __device__ __forceinline__ int r_place(int r) { return 2 * ((r >> 3) & 1) + 4 * ((r >> 1) & 1); }
 __device__ __forceinline__ int v_unit(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
 
-__device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, const unsigned char *lds_1k)
+__device__ __forceinline__ unsigned lds_address(const void *p)
 {
-    const unsigned at = __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)lds_1k));
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(at), "v"(voff), "s"(rs) : "memory");
+    return __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
 }
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4_t *lds_u32x4;
+// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+__device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, int soff, unsigned lds_1k)
+{
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs), "s"(soff) : "memory");
+}
+template <class F, int... I> __device__ __forceinline__ void slots(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N> __device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void tile_barrier()
 {
@@ -56,8 +66,11 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
 {
     __shared__ PromptLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int pairs = p.B * p.H, tiles = (p.Smax + kTileQ - 1) / kTileQ;
-    const int pair = blockIdx.x % pairs, i0 = (tiles - 1 - blockIdx.x / pairs) * kTileQ;      // the longest walks first
+    // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads: they lie 512 bytes apart, and a head's tokens 512 H, for many H a multiple of what its L2's channels
+    // cover between them -- eight heads 4 KiB apart kept an XCD on one or two of its channels (64 heads x 4001 tokens 441 us, ?? with neighbouring heads).
+    const int pairs = p.B * p.H, per = (pairs + 7) / 8, tiles = (p.Smax + kTileQ - 1) / kTileQ;
+    const int at = blockIdx.x % (8 * per), pair = at % 8 * per + at / 8, i0 = (tiles - 1 - blockIdx.x / (8 * per)) * kTileQ;
+    if (pair >= pairs) return;
     const int b = pair / p.H, h = pair % p.H;
     const int S = min(max(p.seq_lens[b], 0), p.Smax);
     const int w0 = i0 + 32 * wave;
@@ -71,130 +84,236 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
     const int steps = (min(i0 + kTileQ, S) - 1) / kStep + 1;
     const int mine = w0 < S ? (min(w0 + 32, S) - 1) / kStep + 1 : 0;
 
+    const unsigned lds_k = lds_address(lds.k[0]), lds_r = lds_address(lds.r[0]), lds_v = lds_address(lds.v[0]);
     u32x4_t q[2][6];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-        const int row = w0 + 16 * qb + n;
+        int row = w0 + 16 * qb + n;
+        asm volatile("" : "+v"(row));                          // (nothing of these addresses is kept for the output's)
 #pragma unroll
         for (int kb = 0; kb < 6; ++kb) {
             q[qb][kb] = u32x4_t{0u, 0u, 0u, 0u};
             if (row < S) q[qb][kb] = *reinterpret_cast<const u32x4_t *>(p.q + (((size_t)b * p.Smax + row) * p.H + h) * kQueryDim + 32 * kb + 8 * g);
+            q[qb][kb] ^= p.scale < 0.f ? 0x80008000u : 0u;     // (the largest product is then the largest logit)
         }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries have arrived: what is counted from here on are fetches
 
-    // A wavefront's five of the 20 KiB of a step: rows 8 wave .. + 7 of the keys and of the values, four rows an instruction, of the rotary parts all eight
+    // A wavefront's five of the 20 KiB of a step: rows 8 wave .. + 7 of the keys and of the values, four rows an instruction, of the rotary parts all eight.
+    // (The places of rows r and r + 4 are the same: the second instruction is the first, four rows on.)
     const int row_bytes = p.H * (2 * kNope * 2), rope_bytes = (int)(p.rope_stride * 2);
-    int koff[2], voff[2], roff;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int r = 8 * wave + 4 * k + (lane >> 4), x = lane & 15;
-        koff[k] = r * row_bytes + ((x ^ k_place(r)) << 4);
-        voff[k] = r * row_bytes + ((x ^ (v_unit(r) << 1)) << 4);
-    }
+    int koff, voff, roff;
     {
-        const int r = 8 * wave + (lane >> 3), x = lane & 7;
-        roff = r * rope_bytes + ((x ^ r_place(r)) << 4);
+        const int r = 8 * wave + (lane >> 4), x = lane & 15, rr = 8 * wave + (lane >> 3);
+        koff = r * row_bytes + ((x ^ k_place(r)) << 4);
+        voff = r * row_bytes + ((x ^ (v_unit(r) << 1)) << 4);
+        roff = rr * rope_bytes + (((lane & 7) ^ r_place(rr)) << 4);
     }
+    // The fetches walk along the rows: a place in memory, the rows left from there, a place in the ring.  Rows without keys arrive as zeros.
+    struct Walk { const unsigned char *from; int left; unsigned to; };
     const unsigned char *kv = reinterpret_cast<const unsigned char *>(p.kv) + ((size_t)b * p.Smax * p.H + h) * (2 * kNope * 2);
-    const unsigned char *rp = reinterpret_cast<const unsigned char *>(p.rope) + (size_t)b * p.Smax * rope_bytes;
-    auto fetch = [&](int s) {
-        const int left = min(max(S - s * kStep, 0), kStep), at = s % kRing;          // rows without keys arrive as zeros
-        const long long bytes = left > 0 ? (long long)(left - 1) * row_bytes + kNope * 2 : 0;
-        const unsigned char *base = kv + (size_t)s * kStep * row_bytes;
-        const u32x4_t rk = window(base, bytes), rv = window(base + kNope * 2, bytes);
-        const u32x4_t rr = window(rp + (size_t)s * kStep * rope_bytes, left > 0 ? (long long)(left - 1) * rope_bytes + kRope * 2 : 0);
+    Walk wk = {kv, S, 0u}, wv = {kv + kNope * 2, S, 0u};
+    const unsigned char *rope_from = reinterpret_cast<const unsigned char *>(p.rope) + (size_t)b * p.Smax * rope_bytes;
+    auto bytes_of = [&](int left, int stride, int row) { const int rows = min(left, kStep); return rows > 0 ? (rows - 1) * stride + row : 0; };
+    auto fetch_k = [&] {
+        const u32x4_t rk = window(wk.from, bytes_of(wk.left, row_bytes, kNope * 2)), rr = window(rope_from, bytes_of(wk.left, rope_bytes, kRope * 2));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) load_to_lds(rk, koff[k], lds.k[at] + (2 * wave + k) * 1024);
-        load_to_lds(rr, roff, lds.r[at] + wave * 1024);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) load_to_lds(rv, voff[k], lds.v[at] + (2 * wave + k) * 1024);
+        for (int k = 0; k < 2; ++k) load_to_lds(rk, koff, 4 * k * row_bytes, lds_k + wk.to * (kStep * kNope * 2) + (2 * wave + k) * 1024);
+        load_to_lds(rr, roff, 0, lds_r + wk.to * (kStep * kRope * 2) + wave * 1024);
+        wk.from += (size_t)kStep * row_bytes;
+        rope_from += (size_t)kStep * rope_bytes;
+        wk.left -= kStep;
+        wk.to = wk.to == kRingK - 1 ? 0 : wk.to + 1;
     };
-    fetch(0);
-    fetch(1);
+    auto fetch_v = [&] {
+        const u32x4_t rv = window(wv.from, bytes_of(wv.left, row_bytes, kNope * 2));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) load_to_lds(rv, voff, 4 * k * row_bytes, lds_v + wv.to * (kStep * kNope * 2) + (2 * wave + k) * 1024);
+        wv.from += (size_t)kStep * row_bytes;
+        wv.left -= kStep;
+        wv.to = wv.to == kRingV - 1 ? 0 : wv.to + 1;
+    };
+    // Entering step s, K of s + 2 and V of s have landed; the step fetches K of s + 4 and V of s + 2, whose places were last read in step s - 1 or before.
+    fetch_k();
+    fetch_k();
+    fetch_k(); fetch_v();
+    fetch_k(); fetch_v();
 
-    f32x4_t acc[8][2];
-    float m[2], l[2];
+    f32x4_t acc[8][2], sum[2];                                 // sum: of the rounded weights, in every element (V^T of ones)
+    float ref[2] = {0.f, 0.f};                                 // of the weights, in units of log2
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-        m[qb] = -INFINITY;
-        l[qb] = 0.f;
+        sum[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[dt][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    const float c1 = p.scale * kLog2e;
-    const int k_row = 8 * (n >> 2) + (n & 3);                  // (+ 4 t: the same places)
-    const int v_row = 8 * g + (n >> 2);
+    const unsigned one2 = T::pack(1.f, 1.f);
+    const float c1 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);     // (not 0: of a masked score it has to leave -inf)
+    // This lane's operand reads: piece 4 kb + g of row k_row (+ 4 t: the same places), 32 bytes from element 16 dt of row v_row.  Those of a row differ by an exclusive or
+    // with a constant.
+    const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
+    const unsigned k_at = k_row * (kNope * 2) + ((g ^ k_place(k_row)) << 4), r_at = k_row * (kRope * 2) + ((g ^ r_place(k_row)) << 4);
+    const unsigned v_at = v_row * (kNope * 2) + (v_unit(v_row) << 5) + ((n & 3) << 3);
 
-    for (int s = 0; s < steps; ++s) {
-        wait_fetches<5>();                                     // step s; s + 1 is under way
-        tile_barrier();
-        fetch(s + 2);
-        if (s >= mine) continue;
-        const int slot = s % kRing;
-        f32x4_t sc[2][2];
+    // operand op = 2 kb + t of a step's scores: 16 keys
+    auto read_k = [&](unsigned kk, unsigned rr, int op) {
+        const int kb = op >> 1, t = op & 1;
+        return *(lds_u32x4)(uintptr_t)(kb < 4 ? (kk ^ (kb << 6)) + 4 * t * (kNope * 2) : (rr ^ ((kb - 4) << 6)) + 4 * t * (kRope * 2));
+    };
+    auto read_v = [&](unsigned vv, int dt) {
+        const unsigned at = vv ^ (dt << 5);
+        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)at);
+        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at + 4 * kNope * 2));
+        return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+
+    // Step s from its scores sc[key block][query block], and the scores of step s + 1, which do not depend on it, in their place.  Vector instructions of one wavefront do not
+    // run under the matrix instructions of the other of its SIMD, but within a wavefront two or three independent ones do under each: so the two are woven by
+    // hand, a matrix instruction and what runs under it to a slot.  24 slots of scores hide the logits, their maxima and the first query block's exponentials, 18 of
+    // V^T P^T the second's.
+    unsigned k_next = 1, v_now = 0;
+    u32x4_t first[4];
+    auto step = [&](auto last_step, int s, f32x4_t (&sc)[2][2]) {
+        constexpr bool kLast = decltype(last_step)::value;
+        // places of K of s + 1 (whose first four operands are there already), of K of s + 2, of V of s
+        unsigned kk = lds_k + k_next * (kStep * kNope * 2) + k_at, rr = lds_r + k_next * (kStep * kRope * 2) + r_at, vv = lds_v + v_now * (kStep * kNope * 2) + v_at;
+        k_next = k_next == kRingK - 1 ? 0 : k_next + 1;
+        v_now = v_now == kRingV - 1 ? 0 : v_now + 1;
+        unsigned k2 = lds_k + k_next * (kStep * kNope * 2) + k_at;
+        asm("" : "+v"(kk), "+v"(rr), "+v"(vv), "+v"(k2));      // (or addresses of every place are kept in registers of their own)
+        // key 8 g + j of the step is visible to query 16 qb + n of the wavefront where j - 16 qb <= own
+        const int own = n - 8 * g;
+        float z[2][8], top[2];
+        f32x4_t scn[2][2];
+        u32x4_t a[12], av[8], w[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int op = 0; op < 4; ++op) a[op] = first[op];
+        auto score_slot = [&](auto mi) {
+            constexpr int mm = decltype(mi)::value, op = mm >> 1, kb = op >> 1, t = op & 1, qb = mm & 1;
+            scn[t][qb] = T::mfma(a[op], q[qb][kb], kb == 0 ? zero : scn[t][qb]);
+            if constexpr (qb == 0 && op + 4 < 12) a[op + 4] = read_k(kk, rr, op + 4);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        slots(std::make_integer_sequence<int, 12>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            if constexpr (!kLast) score_slot(mi);
+            if constexpr (mm < 8) {                            // two logits a slot, against the reference so far
+                constexpr int qb = mm >> 2, j = 2 * (mm & 3);
 #pragma unroll
-            for (int qb = 0; qb < 2; ++qb) sc[qb][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < 2; ++i) {
+                    const float x = __builtin_fmaf(sc[j >> 2][qb][(j & 3) + i], c1, -ref[qb]);
+                    z[qb][j + i] = !kLast || j + i - 16 * qb <= own ? x : -INFINITY;
+                }
+            }
+            if constexpr (mm >= 4 && mm < 10) {                // maxima, two slots behind the logits
+                constexpr int qb = mm >= 8, i = qb ? mm - 8 : mm - 4;
+                if constexpr (qb == 0) {
+                    if constexpr (i == 0) top[0] = fmaxf(fmaxf(z[0][0], z[0][1]), z[0][2]);
+                    if constexpr (i == 1) top[0] = fmaxf(fmaxf(top[0], z[0][3]), z[0][4]);
+                    if constexpr (i == 2) top[0] = fmaxf(fmaxf(top[0], z[0][5]), z[0][6]);
+                    if constexpr (i == 3) top[0] = fmaxf(top[0], z[0][7]);
+                } else {
+                    if constexpr (i == 0) top[1] = fmaxf(fmaxf(fmaxf(fmaxf(z[1][0], z[1][1]), z[1][2]), z[1][3]), z[1][4]);
+                    if constexpr (i == 1) top[1] = fmaxf(fmaxf(fmaxf(top[1], z[1][5]), z[1][6]), z[1][7]);
+                }
+            }
+            if constexpr (mm == 9) top[0] = columns_max(top[0]);
+            if constexpr (mm == 11) top[1] = columns_max(top[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (s == 0 || __any((top[0] > kSlack) | (top[1] > kSlack))) {              // relative to the reference
 #pragma unroll
-            for (int kb = 0; kb < 6; ++kb) {
-                const unsigned char *at = kb < 4 ? lds.k[slot] + (k_row + 4 * t) * (kNope * 2) + (((4 * kb + g) ^ k_place(k_row)) << 4)
-                                                 : lds.r[slot] + (k_row + 4 * t) * (kRope * 2) + (((4 * (kb - 4) + g) ^ r_place(k_row)) << 4);
-                const u32x4_t a = *reinterpret_cast<const u32x4_t *>(at);
+            for (int qb = 0; qb < 2; ++qb) {
+                float d = s == 0 ? top[qb] : fmaxf(top[qb], 0.f);
+                d = d == -INFINITY ? 0.f : d;
+                const float f = __builtin_amdgcn_exp2f(-d);
+                ref[qb] += d;
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb) sc[qb][t] = T::mfma(a, q[qb][kb], sc[qb][t]);
+                for (int j = 0; j < 8; ++j) z[qb][j] -= d;
+                if (s > 0)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        sum[qb][r] *= f;
+#pragma unroll
+                        for (int dt = 0; dt < 8; ++dt) acc[dt][qb][r] *= f;
+                    }
             }
         }
-        const bool last = s == mine - 1;
-        u32x4_t w[2];
-#pragma unroll
-        for (int qb = 0; qb < 2; ++qb) {
-            float z[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                z[j] = sc[qb][j >> 2][j & 3] * c1;
-                if (last && s * kStep + 8 * g + j > w0 + 16 * qb + n) z[j] = -INFINITY;
+        __builtin_amdgcn_sched_barrier(0);
+        slots(std::make_integer_sequence<int, 12>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            if constexpr (!kLast) score_slot(std::integral_constant<int, mm + 12>{});
+            if constexpr (mm >= 2 && mm < 10) av[mm - 2] = read_v(vv, mm - 2);
+            if constexpr (mm < 8) {
+                z[0][mm] = __builtin_amdgcn_exp2f(z[0][mm]);
+                if constexpr (mm & 1) w[0][mm >> 1] = T::pack(z[0][mm - 1], z[0][mm]);
             }
-            float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-            top = columns_max(top);
-            if (__any(top > m[qb] + kSlack)) {                 // (also where there is no reference yet)
-                const float to = fmaxf(top, m[qb]), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[qb] - to);
-                l[qb] *= f;
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[dt][qb][r] *= f;
-                m[qb] = to;
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        const u32x4_t ones = {one2, one2, one2, one2};
+        slots(std::make_integer_sequence<int, 9>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            if constexpr (mm == 0) sum[0] = T::mfma(ones, w[0], sum[0]);
+            else acc[mm - 1][0] = T::mfma(av[mm - 1], w[0], acc[mm - 1][0]);
+            if constexpr (mm < 8) {
+                z[1][mm] = __builtin_amdgcn_exp2f(z[1][mm]);
+                if constexpr (mm & 1) w[1][mm >> 1] = T::pack(z[1][mm - 1], z[1][mm]);
             }
-            const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const unsigned x = T::pack(__builtin_amdgcn_exp2f(z[j] - ref), __builtin_amdgcn_exp2f(z[j + 1] - ref));
-                l[qb] += T::lo(x) + T::hi(x);
-                w[qb][j >> 1] = x;
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        slots(std::make_integer_sequence<int, 9>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            if constexpr (mm == 0) sum[1] = T::mfma(ones, w[1], sum[1]);
+            else acc[mm - 1][1] = T::mfma(av[mm - 1], w[1], acc[mm - 1][1]);
+            if constexpr (!kLast && mm < 8) {
+                constexpr int t = mm >> 2, qb = (mm >> 1) & 1, r = 2 * (mm & 1);
+                sc[t][qb][r] = scn[t][qb][r];
+                sc[t][qb][r + 1] = scn[t][qb][r + 1];
+                if constexpr (mm >= 1 && mm < 5) first[mm - 1] = read_k(k2, 0u, mm - 1);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    f32x4_t scA[2][2];
+    wait_fetches<10>();                                        // K of steps 0 and 1
+    tile_barrier();
+    if (mine > 0) {
+        unsigned kk = lds_k + k_at, rr = lds_r + r_at, k1 = lds_k + kStep * kNope * 2 + k_at;
+        asm("" : "+v"(kk), "+v"(rr), "+v"(k1));
+#pragma unroll
+        for (int op = 0; op < 12; ++op) {
+            const u32x4_t a = read_k(kk, rr, op);
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) scA[op & 1][qb] = T::mfma(a, q[qb][op >> 1], op < 2 ? zero : scA[op & 1][qb]);
         }
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
-            unsigned char *at = lds.v[slot] + v_row * (kNope * 2) + ((dt ^ v_unit(v_row)) << 5) + ((n & 3) << 3);
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * kNope * 2));
-            const u32x4_t a = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int qb = 0; qb < 2; ++qb) acc[dt][qb] = T::mfma(a, w[qb], acc[dt][qb]);
-        }
+        for (int op = 0; op < 4; ++op) first[op] = read_k(k1, 0u, op);
     }
+    auto enter = [&] {
+        wait_fetches<5>();                                     // K of s + 2 and V of s; what step s - 1 fetched is under way
+        tile_barrier();
+        fetch_k();
+        fetch_v();
+    };
+    int s = 0;
+#pragma unroll 1
+    for (; s < mine - 1; ++s) {
+        enter();
+        step(std::false_type{}, s, scA);
+    }
+    if (mine > 0) {
+        enter();
+        step(std::true_type{}, s, scA);
+        ++s;
+    }
+    for (; s < steps; ++s) enter();                           // the steps that only later wavefronts have
     wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int row = w0 + 16 * qb + n;
-        float sum = l[qb];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        const float inv = row < S ? 1.f / sum : 0.f;
+        const float inv = row < S ? 1.f / sum[qb][0] : 0.f;
         if (row >= p.Smax) continue;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
@@ -209,7 +328,7 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
 
 hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)p.B * p.H * ((p.Smax + kTileQ - 1) / kTileQ)));
+    const dim3 grid((unsigned)(((long long)p.B * p.H + 7) / 8 * 8 * ((p.Smax + kTileQ - 1) / kTileQ)));
     return p.dtype == kF16 ? launch(latent_prefill_kernel<F16>, grid, dim3(256), s, p) : launch(latent_prefill_kernel<BF16>, grid, dim3(256), s, p);
 }
 
