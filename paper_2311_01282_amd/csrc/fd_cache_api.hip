@@ -56,7 +56,7 @@ fd_status nibble_rows(const fd_nibble_pool *pool, const void *k, int64_t k_strid
     if (n_tokens < 0 || off(k, 16) || off(v, 16) || off(slot_map, 4) || k_stride < width || v_stride < width || k_stride % 8 != 0 ||
         v_stride % 8 != 0)
         return FD_ERR_SHAPE;
-    if ((long long)n_tokens * 2 * P->Hkv >= (1ll << 35)) return FD_ERR_UNSUPPORTED;          // 16 rows a workgroup
+    if ((long long)n_tokens * 2 * P->Hkv >= (1ll << 31)) return FD_ERR_UNSUPPORTED;
     *R = fd::NibbleRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)), const_cast<uint16_t *>(static_cast<const uint16_t *>(v)),
                      k_stride, v_stride, slot_map, n_tokens};
     return FD_OK;
@@ -246,6 +246,7 @@ fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_
     if (n_tokens < 0 || off(latent, 16) || off(rope, 16) || off(slot_map, 4) || latent_stride < fd::kLatent || rope_stride < fd::kRope ||
         latent_stride % 8 != 0 || rope_stride % 8 != 0)
         return FD_ERR_SHAPE;
+    if (n_tokens > (1 << 28)) return FD_ERR_UNSUPPORTED;
     if (n_tokens == 0) return FD_OK;
     FD_TRY(fd::launch_latent_write(P, static_cast<const uint16_t *>(latent), latent_stride, static_cast<const uint16_t *>(rope), rope_stride,
                                    n_tokens, slot_map, static_cast<hipStream_t>(stream)));

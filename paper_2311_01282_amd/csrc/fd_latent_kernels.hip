@@ -11,18 +11,16 @@ namespace fd {
 namespace {
 
 // ---- rows into the cache: 72 pieces of 16 bytes a row, 64 of the latent part and 8 of the rotary one ----
-__global__ __launch_bounds__(256) void latent_write_kernel(LatentPool pool, const uint16_t *latent, long long latent_stride, const uint16_t *rope,
-                                                           long long rope_stride, int n_tokens, const int32_t *slots)
+constexpr int kPieces = kLatentRow / 8, kWriteTokens = 4;      // tokens of a workgroup: a thread a piece
+__global__ __launch_bounds__(kPieces * kWriteTokens) void latent_write_kernel(LatentPool pool, const uint16_t *latent, long long latent_stride, const uint16_t *rope,
+                                                                              long long rope_stride, int n_tokens, const int32_t *slots)
 {
-    constexpr int kPieces = kLatentRow / 8;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long token = i / kPieces;
-    const int piece = (int)(i - token * kPieces);
+    const int i = threadIdx.x / kPieces, piece = threadIdx.x - i * kPieces, token = blockIdx.x * kWriteTokens + i;
     if (token >= n_tokens) return;
     const int slot = slots[token];
+    const u32x4_t x = *reinterpret_cast<const u32x4_t *>(piece < kLatent / 8 ? latent + token * latent_stride + 8 * piece : rope + token * rope_stride + (8 * piece - kLatent));
     if (slot < 0 || (slot >> pool.page_shift) >= pool.n_pages) return;      // padding
-    const uint16_t *src = piece < kLatent / 8 ? latent + token * latent_stride + 8 * piece : rope + token * rope_stride + (8 * piece - kLatent);
-    *reinterpret_cast<u32x4_t *>(pool.rows + (size_t)slot * kLatentRow + 8 * piece) = *reinterpret_cast<const u32x4_t *>(src);
+    *reinterpret_cast<u32x4_t *>(pool.rows + (size_t)slot * kLatentRow + 8 * piece) = x;
 }
 
 // ---- attention ----
@@ -293,8 +291,8 @@ template <class T> hipError_t decode_heads(const LatentProblem &p, hipStream_t s
 hipError_t launch_latent_write(const LatentPool &pool, const uint16_t *latent, long long latent_stride, const uint16_t *rope,
                                long long rope_stride, int n_tokens, const int32_t *slots, hipStream_t s)
 {
-    const dim3 grid((unsigned)(((long long)n_tokens * (kLatentRow / 8) + 255) / 256));
-    return launch(latent_write_kernel, grid, dim3(256), s, pool, latent, latent_stride, rope, rope_stride, n_tokens, slots);
+    const dim3 grid((unsigned)((n_tokens + kWriteTokens - 1) / kWriteTokens));
+    return launch(latent_write_kernel, grid, dim3(kPieces * kWriteTokens), s, pool, latent, latent_stride, rope, rope_stride, n_tokens, slots);
 }
 hipError_t launch_latent_decode(const LatentProblem &p, hipStream_t s)
 {

@@ -66,8 +66,8 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
 {
     __shared__ PromptLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads: they lie 512 bytes apart, and a head's tokens 512 H, for many H a multiple of what its L2's channels
-    // cover between them -- eight heads 4 KiB apart kept an XCD on one or two of its channels (64 heads x 4001 tokens 441 us, ?? with neighbouring heads).
+    // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads, all tiles of a head on one: its keys and values are read into one L2 only.  (Heads
+    // dealt out to the XCDs in turn measured the same.)
     const int pairs = p.B * p.H, per = (pairs + 7) / 8, tiles = (p.Smax + kTileQ - 1) / kTileQ;
     const int at = blockIdx.x % (8 * per), pair = at % 8 * per + at / 8, i0 = (tiles - 1 - blockIdx.x / (8 * per)) * kTileQ;
     if (pair >= pairs) return;

@@ -14,15 +14,15 @@ namespace fd {
 namespace {
 
 // ---- rows in and out ----
-// 16 lanes to a row, eight elements (16 bytes, one word of codes) to a lane: a row is read, coded and written within a DPP row.  The
-// arithmetic is in fp32: the differences and the division are rounded once each.  What bounds both calls is memory.
+// A row is read, coded and written within eight lanes, 16 elements to a lane (read back: 16 lanes, eight elements to a lane).  The arithmetic is in fp32: the
+// differences and the division are rounded once each.  What bounds the coding is its vector instructions, some 15 an element; with eight elements
+// to a lane the places and the two divisions of a group cost as much again (16001 tokens x 8 heads, fp16: 26.8 us so, 20.3 with 16).  Reading back is bound by memory.
 
 template <class F> __device__ __forceinline__ float group_reduce(float x, int lanes, F f)
 {
     x = f(x, dpp_swap<0xB1>(x));
-    x = f(x, dpp_swap<0x4E>(x));
+    if (lanes > 2) x = f(x, dpp_swap<0x4E>(x));
     if (lanes > 4) x = f(x, dpp_swap<0x141>(x));
-    if (lanes > 8) x = f(x, dpp_swap<0x140>(x));
     return x;
 }
 
@@ -32,17 +32,15 @@ struct RowPlace {
     bool is_v, live;
 };
 
-// Row r of the call: K and V rows of a token's heads, one after the other.
-__device__ __forceinline__ RowPlace row_place(const NibblePool &pool, const int32_t *slots, int n_tokens, long long r)
+// Row r of the call: K and V rows of a token's heads, one after the other.  (32 bits: a division of 64 is a hundred instructions.)
+__device__ __forceinline__ RowPlace row_place(const NibblePool &pool, const int32_t *slots, int n_tokens, unsigned r)
 {
     RowPlace at;
-    const int per = 2 * pool.Hkv;
-    const long long token = r / per;
-    const int rest = (int)(r - token * per);
-    at.is_v = rest >= pool.Hkv;
+    const unsigned per = 2 * pool.Hkv, token = r / per, rest = r - token * per;
+    at.is_v = rest >= (unsigned)pool.Hkv;
     at.head = at.is_v ? rest - pool.Hkv : rest;
     at.token = (int)token;
-    at.live = token < n_tokens;
+    at.live = token < (unsigned)n_tokens;
     const int slot = at.live ? slots[token] : -1;
     at.live = slot >= 0 && (slot >> pool.page_shift) < pool.n_pages;         // anything else: padding, left alone
     const int page = at.live ? slot >> pool.page_shift : 0;
@@ -52,45 +50,64 @@ __device__ __forceinline__ RowPlace row_place(const NibblePool &pool, const int3
 
 template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(NibblePool pool, NibbleRows rows)
 {
-    const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int j = threadIdx.x & 15;                                         // eight elements from 8 j
-    const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, r);
-    if (!at.live) return;                                                   // (whole rows of 16 lanes)
-    const uint16_t *src = (at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim + 8 * j;
-    const u32x4_t x = *reinterpret_cast<const u32x4_t *>(src);
-    float f[8];
+    const unsigned row = blockIdx.x * 32 + (threadIdx.x >> 3);
+    const int j = threadIdx.x & 7;                                          // 16 elements from 16 j: words 2 j and 2 j + 1
+    const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, row);
+    if (!at.live) return;                                                   // (whole rows of 8 lanes)
+    const u32x4_t *src = reinterpret_cast<const u32x4_t *>((at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim + 16 * j);
+    const u32x4_t x[2] = {src[0], src[1]};
+    float f[16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned w = x[i];
+    for (int i = 0; i < 8; ++i) {
+        const unsigned w = x[i >> 2][i & 3];
         f[2 * i] = T::lo(w);
         f[2 * i + 1] = T::hi(w);
     }
     float lo = f[0], hi = f[0], odd = 0.f;                                  // odd: NaN where an element is infinite or NaN
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 16; ++i) {
         lo = fminf(lo, f[i]);
         hi = fmaxf(hi, f[i]);
-        odd += f[i] - f[i];
+        odd = __builtin_fmaf(f[i], 0.f, odd);
     }
-    const int lanes = 16 / pool.NG;
+    const int lanes = 8 / pool.NG;
     lo = group_reduce(lo, lanes, [](float a, float b) { return fminf(a, b); });
     hi = group_reduce(hi, lanes, [](float a, float b) { return fmaxf(a, b); });
     odd = group_reduce(odd, lanes, [](float a, float b) { return a + b; });
-    // the scale as it is stored is the one that the codes are taken against
-    unsigned short s_bits = T::bits((hi - lo) / 15.f), l_bits = T::bits(lo);
-    const float s = T::lo(s_bits);
-    unsigned word = 0;
-    if (odd == 0.f && s > 0.f) {
+    // The scale as it is stored is the one that the codes are taken against.  Quotients are those of fp32 division: with r = 1 / s rounded, q = t r and one correction, q +
+    // r (t - q s), give the correctly rounded t / s (Markstein) where nothing leaves the range of normal numbers; where it might, divisions do.  (With a division for
+    // each element the call was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)
+    const float span = hi - lo;
+    const bool ordinary = (span > 0x1p-80f && span < 0x1p100f) || span == 0.f;
+    constexpr float kFifteenth = 1.f / 15.f;
+    float fifteenth = span * kFifteenth;
+    fifteenth = __builtin_fmaf(__builtin_fmaf(-fifteenth, 15.f, span), kFifteenth, fifteenth);
+    if (!__all(ordinary)) fifteenth = span / 15.f;
+    unsigned short s_bits = T::bits(fifteenth), l_bits = T::bits(lo);
+    const float s = T::lo(s_bits), inv = 1.f / s;
+    float quarter[4] = {0.f, 0.f, 0.f, 0.f};                                // four codes each: whole numbers below 2^16
+    auto put = [&](int i, float q) { quarter[i >> 2] = __builtin_fmaf(quarter[i >> 2], 16.f, fminf(__builtin_rintf(q), 15.f)); };       // (t is not negative)
+    if (__all(ordinary)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = fminf(fmaxf(__builtin_rintf((f[i] - lo) / s), 0.f), 15.f);
-            word |= (unsigned)c << (4 * i);
+        for (int i = 15; i >= 0; --i) {
+            const float t = f[i] - lo, q = t * inv;
+            put(i, __builtin_fmaf(__builtin_fmaf(-q, s, t), inv, q));
         }
+    } else {
+#pragma unroll
+        for (int i = 15; i >= 0; --i) put(i, (f[i] - lo) / s);
+    }
+    unsigned word[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        word[i] = (unsigned)quarter[2 * i] | ((unsigned)quarter[2 * i + 1] << 16);
+        if (odd != 0.f || !(s > 0.f)) word[i] = 0;                          // (what was put together is NaN, then)
     }
     if (odd != 0.f) s_bits = l_bits = 0x7fff;                               // NaN in both types: the group reads as NaN
-    unsigned char *codes = (at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64;
-    const int place = at.is_v ? j : 4 * (j & 3) + (j >> 2);
-    *reinterpret_cast<unsigned *>(codes + 4 * place) = word;
+    unsigned *codes = reinterpret_cast<unsigned *>((at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64);
+    const int place = at.is_v ? 2 * j : 8 * (j & 1) + (j >> 1), apart = at.is_v ? 1 : 4;
+    codes[place] = word[0];
+    codes[place + apart] = word[1];
     uint16_t *scales = (at.is_v ? pool.v_scales : pool.k_scales) + at.row * (2 * pool.NG);
     const int g = j / lanes;
     if (j % lanes == 0) scales[g] = s_bits;
@@ -99,7 +116,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
 
 template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(NibblePool pool, NibbleRows rows)
 {
-    const long long r = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);
     const int j = threadIdx.x & 15;
     const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, r);
     if (!at.live) return;
@@ -651,7 +668,7 @@ template <class T> hipError_t attn_groups(const NibbleProblem &p, hipStream_t s)
 
 hipError_t launch_nibble_write(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
 {
-    const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 15) / 16));
+    const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
     return pool.dtype == kF16 ? launch(nibble_write_kernel<F16>, grid, dim3(256), s, pool, rows) : launch(nibble_write_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
 hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)

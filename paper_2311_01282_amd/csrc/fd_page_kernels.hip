@@ -17,11 +17,12 @@ namespace fd {
 namespace {
 
 constexpr int kThreads = 512, kItems = 4, kWindow = kThreads * kItems;      // requests scanned at a time
-constexpr int kTokens = 8;                                                  // tokens of a thread
+constexpr int kTokens = 2;                                                  // tokens of a thread
 
 struct PageLds {
     int start[kWindow];         // first token of a request, at most max_tokens
     int offset[kWindow];        // pages taken before it; -1: not served
+    int cached[kWindow];
     long long tokens[kThreads / 64], pages[kThreads / 64];
     long long taken[kThreads / 64];
 };
@@ -100,6 +101,7 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             if (b < p.batch) {
                 const int s = (int)min(at, (long long)p.max_tokens);
                 lds.start[r] = s;
+                lds.cached[r] = c[i];
                 lds.offset[r] = served ? (int)min(off, (long long)n_free) : -1;     // (beyond the list only where nothing is needed)
                 if ((b / kWindow + r / 64) % gridDim.x == blockIdx.x) {     // the workgroups share these out by 64 requests
                     p.starts[b] = s;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             }
             if (lds.offset[lo] < 0) continue;
             const int b = w0 + lo;
-            const int cached = (int)min((long long)max(p.cached[b], 0), room);
+            const int cached = lds.cached[lo];
             const int pos = cached + t - lds.start[lo];
             const int held = (int)(((long long)cached + P - 1) >> p.page_shift), j = pos >> p.page_shift;
             int32_t *entry = p.table + (size_t)b * p.width + j;
