@@ -486,6 +486,7 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     without a valid token are not followed, an entry in use that is out of range is the caller's error (it is
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
+ *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128).
  *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
  *     its first 16 KiB, arrival counters that every completed call leaves at zero again; what lies behind them may hold anything.  After that
  *     shapes and calls may change from one use to the next.  A workspace serves one call at a time: calls that may overlap, captured
@@ -539,7 +540,8 @@ typedef struct {
  * Rows into the cache.  k, v [n_tokens, n_kv_heads, 128], k_stride and v_stride elements from a token to the next (multiples of
  * 8, at least n_kv_heads * 128; so a fused projection's parts can be given as they are); token t goes to slot slot_map[t].
  * Per group, in fp32: l = min x; s = (max x - min x) / 15 rounded to dtype; c = (x - l) / s rounded to nearest, ties to even,
- * limited to 0 .. 15; c = 0 where s is 0.  A group with an infinite element or a NaN reads as NaN, all of it.
+ * limited to 0 .. 15; c = 0 where s is 0.  A group with an infinite element, a NaN or a range beyond fp32 reads as NaN, all of it.
+ * n_tokens * n_kv_heads < 2^27 (fd_nibble_read too).
  */
 fd_status fd_nibble_write(const fd_nibble_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
                        const int32_t *slot_map, void *stream);
@@ -553,8 +555,8 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
  * q, out [batch, n_q_heads, 128] of the pool's dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of
  * 64 from 64 to 16384 keys, for example fd_nibble_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
  * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of dtype each (22
- * significant bits in fp16, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch for up to 16
- * chunks a row (and up to 4096 groups of up to 16 heads that share a KV head), else two.
+ * significant bits in fp16, down to 2^-24, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch for up to 16
+ * chunks a row and up to 512 workgroups (one for each chunk of up to 16 heads that share a KV head), else two.
  */
 size_t    fd_nibble_workspace_bytes(const fd_shape *shape);
 int32_t   fd_nibble_pick_chunk(const fd_shape *shape);
@@ -573,7 +575,7 @@ typedef struct {
 } fd_latent_pool;
 
 /* Rows into the cache: latent [n_tokens, 512] and rope [n_tokens, 64] with strides of their own (elements, multiples of 8, at least
- * 512 and 64), token t to slot slot_map[t]. */
+ * 512 and 64), token t to slot slot_map[t]; n_tokens <= 2^25. */
 fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_t latent_stride, const void *rope, int64_t rope_stride,
                           int32_t n_tokens, const int32_t *slot_map, void *stream);
 
@@ -598,7 +600,8 @@ fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *poo
  *        latent rows can be given as they are; sequences max_seq rows apart)
  *   out  [batch, max_seq, n_q_heads, 128]; tokens at and behind seq_lens[b] get zero rows
  * shape: n_kv_heads == n_q_heads (<= 65535), head_dim 192; chunk is ignored.  No workspace.  Scores and sums in fp32, the weights
- * rounded to dtype for the second product; the denominator is the sum of the rounded ones.
+ * rounded to dtype for the second product; the denominator is the sum of the rounded ones.  (A value row with an infinite element or a NaN
+ * can turn that element of up to 31 outputs in front of it to NaN: weights of 0 are multiplied with it.)
  */
 fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const void *q, const void *kv, const void *rope,
                                  int64_t rope_stride, const int32_t *seq_lens, void *out, void *stream);

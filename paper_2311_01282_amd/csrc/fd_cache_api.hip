@@ -11,6 +11,8 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline bool off(const void *p, size_t to) { return ((uintptr_t)p % to) != 0; }
 inline bool is_page_size(int32_t page_size) { return page_size >= 16 && (page_size & (page_size - 1)) == 0; }
 
+constexpr long long kMostThreads = 1ll << 32;      // of a launch
+
 #define FD_TRY(expr) do { if ((expr) != hipSuccess) return FD_ERR_HIP; } while (0)
 
 // A pool's pages: a power of two of rows each, and slots that fit 31 bits.
@@ -56,7 +58,7 @@ fd_status nibble_rows(const fd_nibble_pool *pool, const void *k, int64_t k_strid
     if (n_tokens < 0 || off(k, 16) || off(v, 16) || off(slot_map, 4) || k_stride < width || v_stride < width || k_stride % 8 != 0 ||
         v_stride % 8 != 0)
         return FD_ERR_SHAPE;
-    if ((long long)n_tokens * 2 * P->Hkv >= (1ll << 31)) return FD_ERR_UNSUPPORTED;
+    if ((long long)n_tokens * 2 * P->Hkv >= kMostThreads / 16) return FD_ERR_UNSUPPORTED;
     *R = fd::NibbleRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)), const_cast<uint16_t *>(static_cast<const uint16_t *>(v)),
                      k_stride, v_stride, slot_map, n_tokens};
     return FD_OK;
@@ -89,7 +91,7 @@ fd_status check_shape(const fd_shape *sh, int head_dim)
     if (!sh) return FD_ERR_NULL;
     if (sh->batch < 0 || sh->n_q_heads <= 0 || sh->n_kv_heads <= 0 || sh->head_dim <= 0 || sh->max_seq <= 0) return FD_ERR_SHAPE;
     if (sh->n_q_heads % sh->n_kv_heads != 0 || !std::isfinite(sh->scale)) return FD_ERR_SHAPE;
-    if (sh->head_dim != head_dim) return FD_ERR_UNSUPPORTED;
+    if (sh->head_dim != head_dim || sh->max_seq > (1 << 30)) return FD_ERR_UNSUPPORTED;      // (a chunk's end fits 31 bits)
     return FD_OK;
 }
 fd_status split(const fd_shape *sh, int head_dim, int dim, int unit, Split *S)
@@ -100,7 +102,7 @@ fd_status split(const fd_shape *sh, int head_dim, int dim, int unit, Split *S)
     if (sh->chunk % unit != 0 || sh->chunk > 16384) return FD_ERR_UNSUPPORTED;
     S->rows = (long long)sh->batch * sh->n_q_heads;
     S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
-    if (S->rows * S->nc >= (1ll << 31)) return FD_ERR_UNSUPPORTED;
+    if (S->rows * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;     // (no more workgroups than these, of 512 threads at most)
     const size_t slots = (size_t)(S->rows * S->nc);
     S->num = align_up(kCounters * sizeof(int32_t));
     S->ml = align_up(S->num + (S->nc == 1 ? 0 : slots * dim * sizeof(float)));
@@ -246,7 +248,7 @@ fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_
     if (n_tokens < 0 || off(latent, 16) || off(rope, 16) || off(slot_map, 4) || latent_stride < fd::kLatent || rope_stride < fd::kRope ||
         latent_stride % 8 != 0 || rope_stride % 8 != 0)
         return FD_ERR_SHAPE;
-    if (n_tokens > (1 << 28)) return FD_ERR_UNSUPPORTED;
+    if (n_tokens > (1 << 25)) return FD_ERR_UNSUPPORTED;                    // (72 threads each)
     if (n_tokens == 0) return FD_OK;
     FD_TRY(fd::launch_latent_write(P, static_cast<const uint16_t *>(latent), latent_stride, static_cast<const uint16_t *>(rope), rope_stride,
                                    n_tokens, slot_map, static_cast<hipStream_t>(stream)));
@@ -310,7 +312,7 @@ fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const voi
     const fd_status st = check_shape(shape, 128 + fd::kRope);
     if (st != FD_OK) return st;
     if (shape->n_kv_heads != shape->n_q_heads || shape->n_q_heads > 65535 || !known_type(dtype)) return FD_ERR_UNSUPPORTED;
-    if ((long long)shape->batch * shape->n_q_heads * (((long long)shape->max_seq + 127) / 128) >= (1ll << 31)) return FD_ERR_UNSUPPORTED;
+    if ((long long)shape->batch * shape->n_q_heads * (((long long)shape->max_seq + 127) / 128) > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
     if (!q || !kv || !rope || !seq_lens || !out) return FD_ERR_NULL;
     if (off(q, 16) || off(kv, 16) || off(rope, 16) || off(out, 16) || off(seq_lens, 4) || rope_stride < fd::kRope || rope_stride % 8 != 0 ||
         rope_stride > (1 << 24))

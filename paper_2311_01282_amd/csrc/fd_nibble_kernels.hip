@@ -63,7 +63,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
         f[2 * i] = T::lo(w);
         f[2 * i + 1] = T::hi(w);
     }
-    float lo = f[0], hi = f[0], odd = 0.f;                                  // odd: NaN where an element is infinite or NaN
+    float lo = f[0], hi = f[0], odd = 0.f;                                  // odd: NaN where an element is infinite or NaN ...
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         lo = fminf(lo, f[i]);
@@ -78,6 +78,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
     // r (t - q s), give the correctly rounded t / s (Markstein) where nothing leaves the range of normal numbers; where it might, divisions do.  (With a division for
     // each element the call was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)
     const float span = hi - lo;
+    odd = __builtin_fmaf(span, 0.f, odd);                                   // (or where the group's range is)
     const bool ordinary = (span > 0x1p-80f && span < 0x1p100f) || span == 0.f;
     constexpr float kFifteenth = 1.f / 15.f;
     float fifteenth = span * kFifteenth;
@@ -154,12 +155,12 @@ constexpr int kBlock = 64;                       // keys of a wavefront step
 constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
 constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
-// The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.
-constexpr float kSlack = 8.f;
 
+// kSlack: the reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.  In fp16 a weight times
+// its scale, which may be (65504 + 65504) / 15, has to be a number of the type: four times that is.  (32 x 64/8 heads x 4096 keys, bf16, 37.5 us with 2, 35.6 with 8.)
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
-template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; };
-template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; };
+template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; static constexpr float kSlack = 2.f; };
+template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; static constexpr float kSlack = 8.f; };
 
 // Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).  sixteen: Magic::kSixteen in a register the compiler cannot see through, which keeps
 // "and" and "or" one instruction (of two constants only one can be other than a register).
@@ -399,7 +400,7 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             top[r] = row16_max(fmaxf(fmaxf(z[0][r], z[1][r]), fmaxf(z[2][r], z[3][r])));
-            grew |= top[r] > m[r] + kSlack;
+            grew |= top[r] > m[r] + Magic<T>::kSlack;
         }
         if (__any(grew)) {                                                             // (also where there is no reference yet)
 #pragma unroll

@@ -4,7 +4,7 @@
 // taken from the end of the free list, in the order of the requests, so that request b's share starts where the needs of those
 // before it add up to: a prefix sum.  A token's place follows from another prefix sum (whose token it is) and the table.
 //
-// Every workgroup forms both prefix sums itself, over all requests, and then serves its own 4096 tokens: a token looks its
+// Every workgroup forms both prefix sums itself, over all requests, and then serves its own 1024 tokens: a token looks its
 // request up among the starts in LDS and takes its page from the table if the request held it before, and straight from the free list
 // if it is fresh (another workgroup may be the one to write that entry).  Each fresh page has a first token, which writes the
 // table's entry.  What bounds it is latency: a scan by one workgroup followed by a launch that fills would pay a second launch.

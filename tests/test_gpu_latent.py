@@ -126,6 +126,59 @@ def test_large_logits_and_growing_maxima(dtype):
         check(got, rows, table, lens, ql, qr, 0.07)
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.07])
+@pytest.mark.parametrize("heads", [5, 70])
+def test_scales_of_zero_and_below(scale, heads):
+    lens, max_seq = [300, 1, 65], 320
+    rows, table = filled(torch.float16, lens, 16, max_seq // 16, 13)
+    ql, qr = queries(8, 3, heads, torch.float16)
+    for chunk in (64, 1024):
+        got = decode(rows.to(DEV), table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), ql, qr, chunk, max_seq, scale)
+        torch.cuda.synchronize()
+        check(got, rows, table, lens, ql, qr, scale)
+
+
+@pytest.mark.parametrize("heads", [2, 66])
+def test_rows_of_many_chunks(heads):
+    lens, max_seq = [12800, 4161, 63], 12800
+    rows, table = filled(torch.bfloat16, lens, 64, max_seq // 64, 14)
+    ql, qr = queries(9, 3, heads, torch.bfloat16)
+    got = decode(rows.to(DEV), table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), ql, qr, 64, max_seq, 0.07)
+    torch.cuda.synchronize()
+    check(got, rows, table, lens, ql, qr, 0.07)
+
+
+def test_nan_stays_in_its_sequence():
+    lens, max_seq = [300, 300], 320
+    rows, table = filled(torch.float16, lens, 16, max_seq // 16, 4)
+    ql, qr = queries(5, 2, 20, torch.float16)
+    dl, dt = torch.tensor(lens, dtype=torch.int32, device=DEV), table.to(DEV)
+    clean = decode(rows.to(DEV), dt, dl, ql, qr, 128, max_seq, 0.07)
+    rows[int(table[0, 5]), 3, 520] = float("nan")
+    got = decode(rows.to(DEV), dt, dl, ql, qr, 128, max_seq, 0.07)
+    torch.cuda.synchronize()
+    assert got[0].isnan().all() and torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("heads", [16, 100])
+def test_pools_beyond_32_bits(heads):
+    page = 256
+    n_pages = (5 << 30) // (1152 * page)
+    pool = torch.empty(n_pages, page, 576, dtype=torch.bfloat16, device=DEV)
+    lens, max_seq = [400, 30], 512
+    table = torch.tensor([[n_pages - 1, n_pages - 2], [n_pages - 3, -1]], dtype=torch.int32)
+    slots = torch.tensor([int(table[b, t // page]) * page + t % page for b, n in enumerate(lens) for t in range(n)], dtype=torch.int32).to(DEV)
+    x = torch.randn(sum(lens), 576, generator=torch.Generator().manual_seed(5)).bfloat16().to(DEV)
+    lib().fd_latent_write(lib().make_latent_pool(pool.data_ptr(), n_pages, page, 512, 64, lib().FD_BF16), x.data_ptr(), 576, x[:, 512:].data_ptr(), 576,
+                          len(x), slots.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    ql, qr = queries(6, 2, heads, torch.bfloat16)
+    got = decode(pool, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), ql, qr, 128, max_seq, 0.07)
+    torch.cuda.synchronize()
+    last = pool[-3:].cpu()
+    assert torch.equal(last[1, 399 - 256], x[399].cpu())
+    check(got, last, torch.where(table < 0, table, table - (n_pages - 3)), lens, ql, qr, 0.07)
+
+
 def test_decode_replays():
     lens, max_seq = [500, 33, 511], 512
     rows, table = filled(torch.float16, lens, 64, max_seq // 64, 3)
@@ -230,6 +283,29 @@ def test_prompts_with_large_logits(dtype):
     got = prefill(q, kv, rope, torch.tensor([400, 257], dtype=torch.int32, device=DEV), 0.0722)
     torch.cuda.synchronize()
     check_prompt(got, q, kv, rope, [400, 257], 0.0722)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.07])
+def test_prompts_with_scales_of_zero_and_below(scale):
+    q, kv, rope = prompt(torch.float16, [170, 33], 3, 200, 64, 5)
+    got = prefill(q, kv, rope, torch.tensor([170, 33], dtype=torch.int32, device=DEV), scale)
+    torch.cuda.synchronize()
+    check_prompt(got, q, kv, rope, [170, 33], scale)
+
+
+def test_prompts_beyond_32_bits():
+    """The second sequence starts 4.6 GB into the keys and values."""
+    heads, max_seq, n = 128, 70000, 150
+    q, kv = (torch.empty(2, max_seq, heads, d, dtype=torch.bfloat16, device=DEV) for d in (192, 256))
+    rope = torch.empty(2, max_seq, 64, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator().manual_seed(6)
+    for x in (q, kv, rope):
+        x[1, :n] = torch.randn(n, *x.shape[2:], generator=g).bfloat16().to(DEV)
+    got = prefill(q, kv, rope, torch.tensor([0, n], dtype=torch.int32, device=DEV), 0.07)
+    torch.cuda.synchronize()
+    assert not got[0].any() and not got[1, n:].any() and got[2, :5].isnan().all()
+    few = [0, 77, 127]
+    check_prompt(got[1:2, :n, few], q[1:2, :n, few], kv[1:2, :n, few], rope[1:2, :n], [n], 0.07)
 
 
 def test_prompt_replays():

@@ -143,14 +143,14 @@ def filled(dtype, group, batch, hkv, page, lens, seed, width, spread=1.0):
     return pool, table
 
 
-def tolerance(dtype, q, k, v, s_max, scale, exp):
+def tolerance(dtype, q, k, v, sk, sv, scale, exp):
     """What the arithmetic may be off by, per output element.  A score is a sum of 128 products (16 + c) q in fp32 and 8 more with the scales: at most 160
-    roundings of 2^-24, each of a partial sum of at most sum |q| (31 s + |l|), l within |k| + 15 s; a weight carries twice that (it and the sum) and 2^-21 of its own
-    exponential.  Weights times s are 16 (bf16) or 22 bits, times (16 + c) <= 31 of them; sums of (keys / 32 + 16) terms in fp32.  One rounding at the end."""
-    dx = 160 * 2.0 ** -24 * abs(scale) * q.abs().sum(-1).max() * (46 * s_max + k.abs().max())
+    roundings of 2^-24, each of a partial sum of at most sum |q| (31 s + |l|), l within |k| + 15 s, with s the largest of K's (sk); a weight carries twice that (it and the sum) and 2^-21 of its own
+    exponential.  Weights times s (V's, sv) are 16 (bf16) or 22 bits, times (16 + c) <= 31 of them; sums of (keys / 32 + 16) terms in fp32.  One rounding at the end."""
+    dx = 160 * 2.0 ** -24 * abs(scale) * q.abs().sum(-1).max() * (46 * sk + k.abs().max())
     part = 2.0 ** -17 if dtype == torch.bfloat16 else 2.0 ** -22
     weights = 2 * dx + 2.0 ** -21
-    sums = (part + 2.0 ** -24 * (len(k) / 32 + 16)) * (62 * s_max + v.abs().max())
+    sums = (part + 2.0 ** -24 * (len(k) / 32 + 16)) * (62 * sv + v.abs().max())
     return exp.abs() * want.HALF_STEP[dtype] * 1.01 + weights * v.abs().max() * 2 + sums + 2.0 ** -25
 
 
@@ -183,8 +183,8 @@ def check(got, pool, table, lens, q, scale):
             if n == 0:
                 assert (x == 0).all()
                 continue
-            s_max = float(max(rows[1][:, 0].double().max(), rows[3][:, 0].double().max()))
-            tol = tolerance(pool.dtype, qh.double(), k, v, s_max, scale, exp)
+            sk, sv = (float(rows[i][:, 0].double().max()) for i in (1, 3))
+            tol = tolerance(pool.dtype, qh.double(), k, v, sk, sv, scale, exp)
             off = (x - exp).abs()
             assert torch.isfinite(x).all() and (off <= tol).all(), "sequence %d (%d keys), KV head %d: %.3g of %.3g" % (
                 b, n, h, float((off / tol).max()), 1.0)
@@ -244,6 +244,127 @@ def test_large_logits_and_growing_maxima(dtype):
         got = attend(pool, table.to(DEV), dl, q, chunk, max_seq, 0.1)
         torch.cuda.synchronize()
         check(got, pool, table, lens, q, 0.1)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["fp16", "bf16"])
+def test_scales_of_v_as_large_as_the_type_allows(dtype):
+    """Weights times scales near the end of fp16, with maxima that grow a little at a time."""
+    lens, max_seq = [2000, 999], 2048
+    pool, table = filled(dtype, 32, 2, 2, 64, lens, 12, max_seq // 64)
+    pool.scales[1] *= 2.0 ** 14
+    assert float(pool.scales[1].float().nan_to_num().abs().max()) > 40000
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    for size in (1.0, 2.0, 4.0):
+        q = (size * torch.randn(2, 8, 128, generator=torch.Generator().manual_seed(int(size)))).to(dtype).to(DEV)
+        got = attend(pool, table.to(DEV), dl, q, 4096, max_seq, 0.05)
+        torch.cuda.synchronize()
+        check(got, pool, table, lens, q, 0.05)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.08])
+def test_scales_of_zero_and_below(scale):
+    lens, max_seq = [300, 1, 65], 320
+    pool, table = filled(torch.bfloat16, 64, 3, 2, 16, lens, 13, max_seq // 16)
+    q = torch.randn(3, 6, 128, generator=torch.Generator().manual_seed(8)).bfloat16().to(DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    for chunk in (64, 1024):
+        got = attend(pool, table.to(DEV), dl, q, chunk, max_seq, scale)
+        torch.cuda.synchronize()
+        check(got, pool, table, lens, q, scale)
+
+
+def test_rows_of_many_chunks():
+    """More chunks than the launch joins itself, and than the join reads at a time."""
+    lens, max_seq = [12800, 4161, 63], 12800
+    pool, table = filled(torch.float16, 32, 3, 1, 64, lens, 14, max_seq // 64)
+    q = torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(9)).half().to(DEV)
+    got = attend(pool, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), q, 64, max_seq, 0.1)
+    torch.cuda.synchronize()
+    check(got, pool, table, lens, q, 0.1)
+
+
+def test_groups_of_every_size_of_number():
+    """Ranges from nothing to the largest of bf16: codes, scales and lowest values bit for bit."""
+    g = torch.Generator().manual_seed(4)
+    tokens = 64
+    x = torch.randn(tokens, 2, 128, generator=g).double() * 10.0 ** torch.linspace(-41, 37, tokens).double()[:, None, None]
+    x[0] = 0
+    x[1, :, :32] = torch.finfo(torch.bfloat16).max * torch.tensor([-1.0, 1.0]).repeat(16)       # a range that is no number: reads as NaN
+    x[2, :, 5] = -0.0
+    x = x.to(torch.bfloat16)
+    pool = Pool(4, 16, 1, 32, torch.bfloat16)
+    dev, slots = x.to(DEV), torch.arange(tokens, dtype=torch.int32, device=DEV)
+    write(pool, dev, 0, slots)
+    torch.cuda.synchronize()
+    for which in range(2):
+        with np.errstate(all="ignore"):
+            codes, s, low = want.nibble_code(x[:, which], 32)
+        bad = torch.zeros_like(s, dtype=torch.bool)
+        bad[1, 0] = True
+        codes[1, :32] = 0
+        packed = want.nibble_pack(codes, which)
+        got, scales = pool.codes[which].cpu().reshape(tokens, 64), pool.scales[which].cpu().reshape(tokens, 2, 4)
+        assert torch.equal(got, packed)
+        assert scales[:, :, :][bad[:, None].expand(-1, 2, -1)].isnan().all()
+        for i, e in enumerate((s, low)):
+            assert torch.equal(scales[:, i][~bad], e[~bad])
+
+
+def test_captured_rows_and_strides_beyond_32_bits():
+    """A captured write and read follow the slots of each replay; two tokens 2^31 elements apart."""
+    stride = 2 ** 31
+    big = torch.empty(stride + 512, dtype=torch.float16, device=DEV)
+    for t in range(2):
+        big[t * stride:t * stride + 512] = torch.randn(512, generator=torch.Generator().manual_seed(t)).half().to(DEV)
+    pool = Pool(4, 16, 2, 128, torch.float16)
+    slots = torch.tensor([3, 40], dtype=torch.int32, device=DEV)
+    back = torch.zeros(2, 2, 2, 128, dtype=torch.float16, device=DEV)
+    handle, side, graph = pool.handle(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        s = torch.cuda.current_stream().cuda_stream
+        lib().fd_nibble_write(handle, big.data_ptr(), stride, big[256:].data_ptr(), stride, 2, slots.data_ptr(), s)
+        lib().fd_nibble_read(handle, slots.data_ptr(), 2, back[0].data_ptr(), 256, back[1].data_ptr(), 256, s)
+    x = torch.stack([big[t * stride:t * stride + 512] for t in range(2)]).cpu().reshape(2, 2, 2, 128)      # [token, K or V, head]
+    for where in ([3, 40], [63, 0], [-1, 17], [5, 6]):
+        slots.copy_(torch.tensor(where, dtype=torch.int32))
+        back.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, slot in enumerate(where):
+            for which in range(2):
+                if slot < 0:
+                    assert (back[which, t] == 7).all()
+                    continue
+                codes, sc, low = want.nibble_code(x[t, which], 128)
+                packed = want.nibble_pack(codes, which)
+                assert torch.equal(pool.codes[which][slot // 16, :, slot % 16].cpu(), packed)
+                values = want.nibble_values(packed, torch.stack([sc, low], 1), which)
+                off = (back[which, t].cpu().double() - values).abs()
+                assert (off <= values.abs() * (2.0 ** -11 + 2.0 ** -23) + 2.0 ** -25).all()
+
+
+def test_pools_beyond_32_bits():
+    page, hkv = 512, 8
+    n_pages = (5 << 30) // (64 * hkv * page)                           # 5 GiB of codes, K and V each
+    codes = [torch.empty(n_pages, hkv, page, 64, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.empty(n_pages, hkv, page, 2, 4, dtype=torch.float16, device=DEV) for _ in range(2)]
+    pool = Pool(1, page, hkv, 32, torch.float16)
+    pool.n_pages, pool.codes, pool.scales = n_pages, codes, scales
+    lens, max_seq = [700, 30], 1024
+    table = torch.tensor([[n_pages - 1, n_pages - 2], [n_pages - 3, -1]], dtype=torch.int32)
+    slots = torch.tensor([int(table[b, t // page]) * page + t % page for b, n in enumerate(lens) for t in range(n)], dtype=torch.int32)
+    x = torch.randn(sum(lens), 2 * hkv, 128, generator=torch.Generator().manual_seed(5)).half().to(DEV)
+    write(pool, x, 0, slots.to(DEV))
+    q = torch.randn(2, 16, 128, generator=torch.Generator().manual_seed(6)).half().to(DEV)
+    got = attend(pool, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), q, 256, max_seq, 0.1)
+    torch.cuda.synchronize()
+    small = Pool(3, page, hkv, 32, torch.float16)
+    small.codes, small.scales = [c[-3:].clone() for c in codes], [c[-3:].clone() for c in scales]
+    small_table = torch.where(table < 0, table, table - (n_pages - 3))
+    check(got, small, small_table, lens, q, 0.1)
+    k, s, low = want.nibble_code(x[699:700, 3].cpu(), 32)               # sequence 0's last row of K, head 3
+    assert torch.equal(codes[0][n_pages - 2, 3, 699 - 512].cpu(), want.nibble_pack(k, 0)[0])
 
 
 def test_nan_stays_in_its_row():

@@ -49,6 +49,7 @@ BAD_NIBBLE = [
 ROWS = dict(k=P, k_stride=256, v=P, v_stride=256, n_tokens=4, slots=P)
 BAD_ROWS = [
     (dict(k=None), NULL), (dict(v=None), NULL), (dict(slots=None), NULL), (dict(k=P + 8), SHAPE), (dict(v=P + 2), SHAPE), (dict(slots=P + 2), SHAPE),
+    (dict(n_tokens=1 << 26), UNSUPPORTED),
     (dict(k_stride=255), SHAPE), (dict(k_stride=260), SHAPE), (dict(v_stride=128), SHAPE), (dict(v_stride=-256), SHAPE), (dict(n_tokens=-1), SHAPE),
 ]
 
@@ -87,7 +88,7 @@ def attn4(shape=SHAPE4, pool=NIBBLE, ws_bytes=None, **kw):
 BAD_SHAPES = [
     (dict(batch=-1), SHAPE), (dict(n_q_heads=0), SHAPE), (dict(max_seq=0), SHAPE), (dict(chunk=0), SHAPE), (dict(chunk=-64), SHAPE),
     (dict(chunk=16385), UNSUPPORTED), (dict(chunk=32768), UNSUPPORTED), (dict(scale=math.inf), SHAPE), (dict(scale=math.nan), SHAPE),
-    (dict(max_seq=1 << 30, batch=1 << 12), UNSUPPORTED),
+    (dict(max_seq=1 << 30, batch=1 << 12), UNSUPPORTED), (dict(max_seq=(1 << 30) + 16, chunk=16384), UNSUPPORTED), (dict(batch=1 << 19), UNSUPPORTED),
 ]
 
 
@@ -126,7 +127,8 @@ def test_latent_write():
     for kw, want in BAD_LATENT:
         assert latent_write(changed(LATENT, **kw)) == want, kw
     for kw, want in [(dict(latent=None), NULL), (dict(rope=None), NULL), (dict(slots=None), NULL), (dict(latent=P + 8), SHAPE), (dict(rope=P + 2), SHAPE),
-                     (dict(slots=P + 2), SHAPE), (dict(ls=504), SHAPE), (dict(ls=516), SHAPE), (dict(rs=56), SHAPE), (dict(rs=68), SHAPE), (dict(n=-1), SHAPE)]:
+                     (dict(slots=P + 2), SHAPE), (dict(ls=504), SHAPE), (dict(ls=516), SHAPE), (dict(rs=56), SHAPE), (dict(rs=68), SHAPE), (dict(n=-1), SHAPE),
+                     (dict(n=(1 << 25) + 1), UNSUPPORTED)]:
         assert latent_write(**kw) == want, kw
     assert latent_write(n=0) == fd.FD_OK
 
@@ -166,7 +168,7 @@ def test_latent_prefill_attn():
         return status(fd.fd_latent_prefill_attn, fd.make_shape(**shape), *c.values())
     for kw, want in [(dict(batch=-1), SHAPE), (dict(n_q_heads=0), SHAPE), (dict(max_seq=0), SHAPE), (dict(head_dim=128), UNSUPPORTED),
                      (dict(n_kv_heads=8), UNSUPPORTED), (dict(scale=math.nan), SHAPE), (dict(n_q_heads=65536, n_kv_heads=65536), UNSUPPORTED),
-                     (dict(batch=1 << 20, max_seq=1 << 20), UNSUPPORTED)]:
+                     (dict(batch=1 << 20, max_seq=1 << 20), UNSUPPORTED), (dict(max_seq=(1 << 30) + 1), UNSUPPORTED)]:
         assert call(changed(SHAPE_P, **kw)) == want, kw
     for kw, want in [(dict(dtype=2), UNSUPPORTED), (dict(q=None), NULL), (dict(kv=None), NULL), (dict(rope=None), NULL), (dict(lens=None), NULL),
                      (dict(out=None), NULL), (dict(q=P + 8), SHAPE), (dict(kv=P + 8), SHAPE), (dict(rope=P + 8), SHAPE), (dict(out=P + 8), SHAPE),
