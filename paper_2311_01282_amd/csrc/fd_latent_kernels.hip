@@ -45,9 +45,10 @@ constexpr int kCBytes = kLatent * 2, kRBytes = kRope * 2;      // in LDS the two
 // Steps in LDS: one in work, one under way.  Two workgroups of up to 64 heads fit a compute unit, which covers the loads better than one with four steps: 16 x 64 heads x 2000 keys
 // 30.1 / 31.7 us, 64 x 16 x 1000 25.3 / 26.9; in long launches it is the other way round, 64 x 64 x 4000 88.7 / 86.6.
 constexpr int kSteps = 2;
-template <int TPW> struct LatentLds {
+template <int NW, int DS, int TPW> struct LatentLds {
     alignas(256) unsigned char c[kSteps * TPW][kTile * kCBytes];      // piece x (16 bytes) of row r in place x ^ c_key(r)
     alignas(256) unsigned char r[kSteps * TPW][kTile * kRBytes];      // ... x ^ r_key(r)
+    alignas(256) f32x4_t x[NW / DS][DS][DS == 1 ? 1 : 64];               // parts of the scores of 16 heads
 };
 // A cycle of the 16-byte operand reads holds every n once, from two neighbouring g: with these keys the 16 pieces lie in 16 different places modulo 256 bytes.  The
 // transposing reads take 32 bytes of eight rows at a time, 8 g + 4 h + (0 .. 3) of two neighbouring g: in eight different places.  Rows r and r + 4 have the same keys.
@@ -84,7 +85,8 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     constexpr int kKeys = TPW * kTile, kRows = kKeys / NW;     // keys of a step; rows that a wavefront fetches
     constexpr int kHalves = (kRows + 15) / 16;                 // ... from so many places of 16 rows
     constexpr int kLoads = kRows / 8 * 9;                      // fetches of a wavefront a step
-    __shared__ LatentLds<TPW> lds;
+    constexpr int kParts = DS == 4 ? 2 : 1, kBlocks = DS == 1 ? 2 : 1, kOperands = 18 / kParts;        // of the scores, of a wavefront
+    __shared__ LatentLds<NW, DS, TPW> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     // workgroups that read the same rows lie on one XCD (index modulo 8), one after the other
     const int tiles = (p.H + 16 * NH - 1) / (16 * NH), units = p.B * p.nc;
@@ -138,13 +140,16 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     };
     fetch(0);
 
-    u32x4_t q[18];
+    // this wavefront's part of the scores: key block t (or both), operands kParts i + odd
+    const int part = DS == 1 ? 0 : wave / NH, odd = part / 2;
+    u32x4_t q[kOperands];
 #pragma unroll
-    for (int kb = 0; kb < 18; ++kb) {
-        q[kb] = u32x4_t{0u, 0u, 0u, 0u};
+    for (int i = 0; i < kOperands; ++i) {
+        q[i] = u32x4_t{0u, 0u, 0u, 0u};
         if (n < heads) {
             const size_t row = (size_t)b * p.H + head0 + n;
-            q[kb] = *reinterpret_cast<const u32x4_t *>(kb < 16 ? p.q_latent + row * kLatent + 32 * kb + 8 * g : p.q_rope + row * kRope + 32 * (kb - 16) + 8 * g);
+            const int kb = kParts * i + odd;
+            q[i] = *reinterpret_cast<const u32x4_t *>(kParts * i < 16 ? p.q_latent + row * kLatent + 32 * kb + 8 * g : p.q_rope + row * kRope + 32 * (kb - 16) + 8 * g);
         }
     }
     f32x4_t acc[kDt];
@@ -154,7 +159,8 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     const float c1 = p.scale * kLog2e;
     // this lane's operand reads: piece 4 kb + g of row k_row; 32 bytes from element 16 dt of row v_row.  Pieces within 256 bytes differ by an exclusive or.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
-    const unsigned k_at = k_row * kCBytes + ((g ^ c_key(k_row)) << 4), kr_at = k_row * kRBytes + ((g ^ r_key(k_row)) << 4);
+    const int k_first = k_row + (DS == 1 ? 0 : 4 * (part & 1));
+    const unsigned k_at = k_first * kCBytes + ((g ^ c_key(k_row)) << 4 ^ odd << 6), kr_at = k_first * kRBytes + ((g ^ r_key(k_row)) << 4 ^ odd << 6);
     const unsigned v_at = v_row * kCBytes + (((n >> 1) & 1) << 4) + ((n & 1) << 3) + (c_key(v_row) << 4);
 
     __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries, and with them step 0 (the compiler, which does not count the fetches, would wait within the loop)
@@ -172,26 +178,39 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
             f32x4_t sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
             {
                 const unsigned kc = tile_c + k_at, kr = tile_r + kr_at;
-                auto read = [&](int kb, int t) {
+                auto read = [&](int i, int t) {
+                    const int kb = kParts * i;
                     const unsigned x = kb < 16 ? (kc ^ ((kb & 3) << 6)) + ((kb >> 2) << 8) + t * 4 * kCBytes : (kr ^ ((kb & 1) << 6)) + t * 4 * kRBytes;
                     return *(lds_u32x4)(uintptr_t)x;
                 };
                 // reads run kAhead operands ahead of the instructions that use them
                 constexpr int kAhead = 3;
-                u32x4_t a[kAhead + 1][2];
+                u32x4_t a[kAhead + 1][kBlocks];
 #pragma unroll
-                for (int kb = 0; kb < kAhead; ++kb)
+                for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) a[kb][t] = read(kb, t);
+                    for (int t = 0; t < kBlocks; ++t) a[i][t] = read(i, t);
 #pragma unroll
-                for (int kb = 0; kb < 18; ++kb) {
-                    if (kb + kAhead < 18)
+                for (int i = 0; i < kOperands; ++i) {
+                    if (i + kAhead < kOperands)
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) a[(kb + kAhead) % (kAhead + 1)][t] = read(kb + kAhead, t);
+                        for (int t = 0; t < kBlocks; ++t) a[(i + kAhead) % (kAhead + 1)][t] = read(i + kAhead, t);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) sc[t] = T::mfma(a[kb % (kAhead + 1)][t], q[kb], sc[t]);
+                    for (int t = 0; t < kBlocks; ++t) {
+                        const int to = kBlocks == 1 ? i & 1 : t;             // (of one block: two chains)
+                        sc[to] = T::mfma(a[i % (kAhead + 1)][t], q[i], sc[to]);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (DS > 1) {                            // the wavefronts of 16 heads exchange their parts
+                lds.x[wave % NH][part][lane] = sc[0] + sc[1];
+                tile_barrier();
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    sc[t] = lds.x[wave % NH][t][lane];
+                    if constexpr (DS == 4) sc[t] += lds.x[wave % NH][t + 2][lane];
                 }
             }
             const unsigned vc = tile_c + v_at + 2 * d0;

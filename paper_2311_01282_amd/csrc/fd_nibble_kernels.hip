@@ -157,7 +157,7 @@ constexpr int kJoinInPlace = 16;                 // chunks of a row that the lau
 constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
 
 // kSlack: the reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.  In fp16 a weight times
-// its scale, which may be (65504 + 65504) / 15, has to be a number of the type: four times that is.  (32 x 64/8 heads x 4096 keys, bf16, 37.5 us with 2, 35.6 with 8.)
+// its scale, which may be (65504 + 65504) / 15, has to be a number of the type: four times that is.  (32 x 64/8 heads x 4096 keys, bf16: 37.5 us with 2, 37.0 with 8.)
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
 template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; static constexpr float kSlack = 2.f; };
 template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; static constexpr float kSlack = 8.f; };
