@@ -23,14 +23,26 @@ struct PageLds {
     int start[kWindow];         // first token of a request, at most max_tokens
     int offset[kWindow];        // pages taken before it; -1: not served
     int cached[kWindow];
-    long long tokens[kThreads / 64], pages[kThreads / 64];
-    long long taken[kThreads / 64];
+    unsigned tokens[kThreads / 64], pages[kThreads / 64];
+    int taken[kThreads / 64];
 };
 
-__device__ __forceinline__ long long shift_up(long long x, int d, int lane)
+// Sums of tokens and of pages end at kMany, which is more than there may be of either (max_tokens <= 2^30, fewer pages): sums that end somewhere add in any order as sums do.
+constexpr unsigned kMany = (1u << 30) + 1;
+__device__ __forceinline__ unsigned add(unsigned a, unsigned b) { return min(a + b, kMany); }
+template <int kControl, int kRows> __device__ __forceinline__ unsigned add_dpp(unsigned x)
 {
-    const long long y = __shfl_up(x, d);
-    return lane >= d ? y : 0;
+    return add(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xf, false));
+}
+// sum of x over the lanes up to this one
+__device__ __forceinline__ unsigned prefix(unsigned x)
+{
+    x = add_dpp<0x111, 0xf>(x);                                             // from 1, 2, 4 and 8 lanes before, within a row of 16
+    x = add_dpp<0x112, 0xf>(x);
+    x = add_dpp<0x114, 0xf>(x);
+    x = add_dpp<0x118, 0xf>(x);
+    x = add_dpp<0x142, 0xa>(x);                                             // the sum of row 0 to row 1 and of 2 to 3
+    return add_dpp<0x143, 0xc>(x);                                          // of rows 0 and 1 to 2 and 3
 }
 
 __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
@@ -38,10 +50,12 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
     __shared__ PageLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int P = 1 << p.page_shift;
-    const long long room = (long long)p.width << p.page_shift;
+    const int room = p.width << p.page_shift;
+    auto pages = [&](unsigned len) { return (int)((len + P - 1) >> p.page_shift); };
     const int n_free = min(max(*p.n_free, 0), p.n_pages);
     const int t0 = blockIdx.x * (kThreads * kTokens) + tid;                 // this thread's tokens: t0 + i kThreads
-    long long tokens_before = 0, pages_before = 0, taken = 0;               // of the windows before this one
+    unsigned tokens_before = 0, pages_before = 0;                           // of the windows before this one
+    int taken = 0;
     int slot[kTokens];
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) slot[i] = -1;
@@ -54,70 +68,75 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             const int b = w0 + tid * kItems + i;
             c[i] = n[i] = 0;
             if (b < p.batch) {
-                c[i] = (int)min((long long)max(p.cached[b], 0), room);
+                c[i] = min(max(p.cached[b], 0), room);
                 n[i] = max(p.fresh[b], 0);
             }
         }
-        long long tok = 0;
+        unsigned tok = 0;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) tok += n[i];
-        long long run = tok;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) run += shift_up(run, d, lane);
+        for (int i = 0; i < kItems; ++i) tok = add(tok, n[i]);
+        const unsigned run = prefix(tok), before = (unsigned)__builtin_amdgcn_update_dpp(0, (int)run, 0x138, 0xf, 0xf, false);      // (without this lane's)
         if (lane == 63) lds.tokens[wave] = run;
         __syncthreads();
-        long long start = tokens_before + run - tok, all = tokens_before;
+        unsigned start = tokens_before, all = tokens_before;
         for (int w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) start += lds.tokens[w];
-            all += lds.tokens[w];
+            if (w < wave) start = add(start, lds.tokens[w]);
+            all = add(all, lds.tokens[w]);
         }
+        start = add(start, before);
         // what a request needs, where it has room for its tokens in the table and in the slot map
         int need[kItems];
-        long long pg = 0, at = start;
+        unsigned pg = 0, at = start;
         bool fits[kItems];
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            at += n[i];
-            fits[i] = c[i] + (long long)n[i] <= room && at <= p.max_tokens;
-            need[i] = fits[i] ? (int)((c[i] + (long long)n[i] + P - 1) >> p.page_shift) - (int)(((long long)c[i] + P - 1) >> p.page_shift) : 0;
-            pg += need[i];
+            at = add(at, n[i]);
+            const unsigned len = (unsigned)c[i] + (unsigned)n[i];
+            fits[i] = len <= (unsigned)room && at <= (unsigned)p.max_tokens;
+            need[i] = fits[i] ? pages(len) - pages(c[i]) : 0;
+            pg = add(pg, need[i]);
         }
-        long long prun = pg;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) prun += shift_up(prun, d, lane);
+        const unsigned prun = prefix(pg), pbefore = (unsigned)__builtin_amdgcn_update_dpp(0, (int)prun, 0x138, 0xf, 0xf, false);
         if (lane == 63) lds.pages[wave] = prun;
         __syncthreads();
-        long long off = pages_before + prun - pg, pages_all = pages_before;
+        unsigned off = pages_before, pages_all = pages_before;
         for (int w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) off += lds.pages[w];
-            pages_all += lds.pages[w];
+            if (w < wave) off = add(off, lds.pages[w]);
+            pages_all = add(pages_all, lds.pages[w]);
         }
+        off = add(off, pbefore);
         at = start;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int r = tid * kItems + i, b = w0 + r;
-            const bool served = fits[i] && (need[i] == 0 || off + need[i] <= n_free);
-            if (off + need[i] <= n_free) taken = off + need[i];             // (grows along the requests of a thread, and from window to window)
+            const unsigned upto = add(off, need[i]);
+            const bool listed = upto <= (unsigned)n_free, served = fits[i] && (need[i] == 0 || listed);
+            if (listed) taken = (int)upto;                                  // (grows along the requests of a thread, and from window to window)
             if (b < p.batch) {
-                const int s = (int)min(at, (long long)p.max_tokens);
+                const int s = (int)min(at, (unsigned)p.max_tokens);
                 lds.start[r] = s;
                 lds.cached[r] = c[i];
-                lds.offset[r] = served ? (int)min(off, (long long)n_free) : -1;     // (beyond the list only where nothing is needed)
+                lds.offset[r] = served ? (int)min(off, (unsigned)n_free) : -1;      // (beyond the list only where nothing is needed)
                 if ((b / kWindow + r / 64) % gridDim.x == blockIdx.x) {     // the workgroups share these out by 64 requests
                     p.starts[b] = s;
                     p.seq_lens[b] = served ? c[i] + n[i] : c[i];
                 }
             }
-            at += n[i];
-            off += need[i];
+            at = add(at, n[i]);
+            off = upto;
         }
         __syncthreads();
         // tokens of this window's requests
-        const long long end = min(all, (long long)p.max_tokens);
+        const int end = (int)min(all, (unsigned)p.max_tokens), first = (int)min(tokens_before, (unsigned)p.max_tokens);
+        const int32_t *from[kTokens];                                       // where the token's page stands; null: no slot from this window
+        int32_t *to[kTokens];                                               // the table's entry, of a fresh page's first token
+        int in_page[kTokens], page[kTokens];
 #pragma unroll
         for (int i = 0; i < kTokens; ++i) {
             const int t = t0 + i * kThreads;
-            if (t < tokens_before || t >= end) continue;
+            from[i] = nullptr;
+            to[i] = nullptr;
+            if (t < first || t >= end) continue;
             int lo = 0, hi = count;                                         // the last request that starts at or before t
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
@@ -127,15 +146,20 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             const int b = w0 + lo;
             const int cached = lds.cached[lo];
             const int pos = cached + t - lds.start[lo];
-            const int held = (int)(((long long)cached + P - 1) >> p.page_shift), j = pos >> p.page_shift;
+            const int held = pages(cached), j = pos >> p.page_shift;
             int32_t *entry = p.table + (size_t)b * p.width + j;
-            int page;
-            if (j < held) page = *entry;
-            else {
-                page = p.free_pages[n_free - 1 - (lds.offset[lo] + j - held)];
-                if ((pos & (P - 1)) == 0) *entry = page;
-            }
-            if ((unsigned)page < (unsigned)p.n_pages) slot[i] = (page << p.page_shift) + (pos & (P - 1));
+            in_page[i] = pos & (P - 1);
+            from[i] = j < held ? entry : p.free_pages + (n_free - 1 - (lds.offset[lo] + j - held));
+            if (j >= held && in_page[i] == 0) to[i] = entry;
+        }
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i)                                   // (all before the first store, which they might otherwise have to wait for)
+            if (from[i]) page[i] = *from[i];
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i) {
+            if (!from[i]) continue;
+            if (to[i]) *to[i] = page[i];
+            if ((unsigned)page[i] < (unsigned)p.n_pages) slot[i] = (page[i] << p.page_shift) + in_page[i];
         }
         tokens_before = all;
         pages_before = pages_all;
@@ -149,13 +173,13 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
     if (blockIdx.x == 0) {
         // pages taken: the largest running need that the list could serve
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) taken = max(taken, (long long)__shfl_xor(taken, d));
+        for (int d = 1; d < 64; d *= 2) taken = max(taken, __shfl_xor(taken, d));
         if (lane == 0) lds.taken[wave] = taken;
         __syncthreads();
         if (tid == 0) {
             for (int w = 1; w < kThreads / 64; ++w) taken = max(taken, lds.taken[w]);
-            *p.n_left = n_free - (int)taken;
-            p.starts[p.batch] = (int)min(tokens_before, (long long)p.max_tokens);
+            *p.n_left = n_free - taken;
+            p.starts[p.batch] = (int)min(tokens_before, (unsigned)p.max_tokens);
         }
     }
 }
