@@ -6,6 +6,7 @@
 //   scores   S^T[key][query] = K . Q^T: A = 16 keys of the tile in LDS, B = Q^T in registers.  Row 4 g + r of key block t is key 8 g + 4 t + r of the 32 of a step, so
 //            that lane (n, g) holds keys 8 g .. 8 g + 7 of query n: the B operand of
 //   output   O^T[d][query] = V^T . P^T: A = V^T by the transposing LDS read.
+// Where a launch has few workgroups, a workgroup is two such halves that take every other step and join their sums at the end (kHalves).
 // Softmax with a running maximum per query; the weights are of the type (one rounding, as large as the output's own), their sum is that of the
 // rounded ones, in fp32.
 #include <utility>
@@ -62,10 +63,12 @@ __device__ __forceinline__ u32x4_t window(const void *base, long long bytes)
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
 }
 
-template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kernel(LatentPromptProblem p)
+template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) void latent_prefill_kernel(LatentPromptProblem p)
 {
-    __shared__ PromptLds lds;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    __shared__ union { PromptLds ring[kHalves]; f32x4_t sums[4][18][64]; } both;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, n = lane & 15, g = lane >> 4;
+    const int half = kHalves == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);      // takes the steps half, half + kHalves, ...
+    PromptLds &lds = both.ring[half];
     // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads, all tiles of a head on one: its keys and values are read into one L2 only.  (Heads
     // dealt out to the XCDs in turn measured the same.)
     const int pairs = p.B * p.H, per = (pairs + 7) / 8, tiles = (p.Smax + kTileQ - 1) / kTileQ;
@@ -77,12 +80,13 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
     uint16_t *out = p.out + ((size_t)b * p.Smax * p.H + h) * kNope;
     const size_t out_stride = (size_t)p.H * kNope;
     if (i0 >= S) {                                             // rows past the prompt: zeros
-        for (int i = i0 + (tid >> 4); i < min(i0 + kTileQ, p.Smax); i += 16)
+        for (int i = i0 + (tid >> 4); i < min(i0 + kTileQ, p.Smax); i += 16 * kHalves)
             *reinterpret_cast<u32x4_t *>(out + i * out_stride + 8 * (tid & 15)) = u32x4_t{0u, 0u, 0u, 0u};
         return;
     }
-    const int steps = (min(i0 + kTileQ, S) - 1) / kStep + 1;
-    const int mine = w0 < S ? (min(w0 + 32, S) - 1) / kStep + 1 : 0;
+    // this half's steps, of the workgroup (the first half has as many or one more) and of the wavefront, whose last step of all is the one with masks
+    const int steps = ((min(i0 + kTileQ, S) - 1) / kStep + kHalves) / kHalves;
+    const int all = w0 < S ? (min(w0 + 32, S) - 1) / kStep + 1 : 0, mine = (all - half + kHalves - 1) / kHalves;
 
     const unsigned lds_k = lds_address(lds.k[0]), lds_r = lds_address(lds.r[0]), lds_v = lds_address(lds.v[0]);
     u32x4_t q[2][6];
@@ -112,25 +116,26 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
     // The fetches walk along the rows: a place in memory, the rows left from there, a place in the ring.  Rows without keys arrive as zeros.
     struct Walk { const unsigned char *from; int left; unsigned to; };
     const unsigned char *kv = reinterpret_cast<const unsigned char *>(p.kv) + ((size_t)b * p.Smax * p.H + h) * (2 * kNope * 2);
-    Walk wk = {kv, S, 0u}, wv = {kv + kNope * 2, S, 0u};
-    const unsigned char *rope_from = reinterpret_cast<const unsigned char *>(p.rope) + (size_t)b * p.Smax * rope_bytes;
+    const int skip = half * kStep;
+    Walk wk = {kv + (size_t)skip * row_bytes, S - skip, 0u}, wv = {kv + (size_t)skip * row_bytes + kNope * 2, S - skip, 0u};
+    const unsigned char *rope_from = reinterpret_cast<const unsigned char *>(p.rope) + ((size_t)b * p.Smax + skip) * rope_bytes;
     auto bytes_of = [&](int left, int stride, int row) { const int rows = min(left, kStep); return rows > 0 ? (rows - 1) * stride + row : 0; };
     auto fetch_k = [&] {
         const u32x4_t rk = window(wk.from, bytes_of(wk.left, row_bytes, kNope * 2)), rr = window(rope_from, bytes_of(wk.left, rope_bytes, kRope * 2));
 #pragma unroll
         for (int k = 0; k < 2; ++k) load_to_lds(rk, koff, 4 * k * row_bytes, lds_k + wk.to * (kStep * kNope * 2) + (2 * wave + k) * 1024);
         load_to_lds(rr, roff, 0, lds_r + wk.to * (kStep * kRope * 2) + wave * 1024);
-        wk.from += (size_t)kStep * row_bytes;
-        rope_from += (size_t)kStep * rope_bytes;
-        wk.left -= kStep;
+        wk.from += (size_t)kHalves * kStep * row_bytes;
+        rope_from += (size_t)kHalves * kStep * rope_bytes;
+        wk.left -= kHalves * kStep;
         wk.to = wk.to == kRingK - 1 ? 0 : wk.to + 1;
     };
     auto fetch_v = [&] {
         const u32x4_t rv = window(wv.from, bytes_of(wv.left, row_bytes, kNope * 2));
 #pragma unroll
         for (int k = 0; k < 2; ++k) load_to_lds(rv, voff, 4 * k * row_bytes, lds_v + wv.to * (kStep * kNope * 2) + (2 * wave + k) * 1024);
-        wv.from += (size_t)kStep * row_bytes;
-        wv.left -= kStep;
+        wv.from += (size_t)kHalves * kStep * row_bytes;
+        wv.left -= kHalves * kStep;
         wv.to = wv.to == kRingV - 1 ? 0 : wv.to + 1;
     };
     // Entering step s, K of s + 2 and V of s have landed; the step fetches K of s + 4 and V of s + 2, whose places were last read in step s - 1 or before.
@@ -183,7 +188,7 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
         unsigned k2 = lds_k + k_next * (kStep * kNope * 2) + k_at;
         asm("" : "+v"(kk), "+v"(rr), "+v"(vv), "+v"(k2));      // (or addresses of every place are kept in registers of their own)
         // key 8 g + j of the step is visible to query 16 qb + n of the wavefront where j - 16 qb <= own
-        const int own = n - 8 * g;
+        const int own = kHalves == 1 || (all - 1) % kHalves == half ? n - 8 * g : kStep;
         float z[2][8], top[2];
         f32x4_t scn[2][2];
         u32x4_t a[12], av[8], w[2];
@@ -310,6 +315,32 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
     }
     for (; s < steps; ++s) enter();                           // the steps that only later wavefronts have
     wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
+    if constexpr (kHalves == 2) {                              // the second half's sums to the first, in the rings' place
+        tile_barrier();
+        if (half == 1) {
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) both.sums[wave][8 * qb + dt][lane] = acc[dt][qb];
+                both.sums[wave][16 + qb][lane] = f32x4_t{sum[qb][0], ref[qb], 0.f, 0.f};
+            }
+        }
+        tile_barrier();
+        if (half == 1) return;
+        if (all > 1)                                           // (of one step the second half has none)
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                const f32x4_t x = both.sums[wave][16 + qb][lane];
+                const float top = fmaxf(ref[qb], x[1]), f0 = __builtin_amdgcn_exp2f(ref[qb] - top), f1 = __builtin_amdgcn_exp2f(x[1] - top);
+                sum[qb][0] = sum[qb][0] * f0 + x[0] * f1;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const f32x4_t y = both.sums[wave][8 * qb + dt][lane];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[dt][qb][r] = acc[dt][qb][r] * f0 + y[r] * f1;
+                }
+            }
+    }
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int row = w0 + 16 * qb + n;
@@ -324,12 +355,18 @@ template <class T> __global__ __launch_bounds__(256, 2) void latent_prefill_kern
     }
 }
 
+template <class T> hipError_t prefill(const LatentPromptProblem &p, hipStream_t s)
+{
+    const long long workgroups = ((long long)p.B * p.H + 7) / 8 * 8 * ((p.Smax + kTileQ - 1) / kTileQ);
+    const dim3 grid((unsigned)workgroups);
+    // A wavefront alone on its SIMD takes 0.75 us a step, two 1.05 together: launches that leave the second place empty give it to a second half of the workgroup, unless they are
+    // so short that joining the halves costs as much (with halves / without, us: 1 x 16 heads x 2000 tokens 42.6 / 54.0, 1 x 8 x 4000 75.2 / 100.0, 1 x 32 x 500 18.3 / 19.6, 3 x 16 x
+    // 150 .. 1000 31.3 / 32.9, 4 x 16 x 200 .. 400 17.0 / 17.2, 1 x 16 x 128 11.2 / 10.0, 32 x 16 x 100 22.5 / 16.3, 1 x 64 x 2000 117 / 107).
+    return workgroups <= kComputeUnits * 3 / 2 && p.Smax > 2 * kTileQ ? launch(latent_prefill_kernel<T, 2>, grid, dim3(512), s, p) : launch(latent_prefill_kernel<T, 1>, grid, dim3(256), s, p);
+}
+
 }  // namespace
 
-hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s)
-{
-    const dim3 grid((unsigned)(((long long)p.B * p.H + 7) / 8 * 8 * ((p.Smax + kTileQ - 1) / kTileQ)));
-    return p.dtype == kF16 ? launch(latent_prefill_kernel<F16>, grid, dim3(256), s, p) : launch(latent_prefill_kernel<BF16>, grid, dim3(256), s, p);
-}
+hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s) { return p.dtype == kF16 ? prefill<F16>(p, s) : prefill<BF16>(p, s); }
 
 }  // namespace fd

@@ -278,6 +278,18 @@ def test_prompts(dtype, lens, heads, max_seq, rope_stride):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["fp16", "bf16"])
+@pytest.mark.parametrize("size", [1.0, 20.0])
+def test_prompts_of_many_workgroups(dtype, size):
+    """Of the launches above each workgroup of prompts beyond 256 tokens is split in halves; here it is not."""
+    lens, heads, max_seq = [400, 0, 333], 70, 400
+    q, kv, rope = prompt(dtype, lens, heads, max_seq, 64, 7, size)
+    got = prefill(q, kv, rope, torch.tensor(lens, dtype=torch.int32, device=DEV), 0.0722)
+    torch.cuda.synchronize()
+    few = [0, 33, 69]
+    check_prompt(got[:3, :, few], q[:, :, few], kv[:, :, few], rope, lens, 0.0722)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["fp16", "bf16"])
 def test_prompts_with_large_logits(dtype):
     q, kv, rope = prompt(dtype, [400, 257], 2, 416, 576, 3, 20.0)
     got = prefill(q, kv, rope, torch.tensor([400, 257], dtype=torch.int32, device=DEV), 0.0722)
