@@ -121,11 +121,14 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     const unsigned char *rope_from = reinterpret_cast<const unsigned char *>(p.rope) + ((size_t)b * p.Smax + skip) * rope_bytes;
     auto bytes_of = [&](int left, int stride, int row) { const int rows = min(left, kStep); return rows > 0 ? (rows - 1) * stride + row : 0; };
     auto fetch_k = [&] {
-        const u32x4_t rk = window(wk.from, bytes_of(wk.left, row_bytes, kNope * 2)), rr = window(rope_from, bytes_of(wk.left, rope_bytes, kRope * 2));
+        const u32x4_t rk = window(wk.from, bytes_of(wk.left, row_bytes, kNope * 2));
 #pragma unroll
         for (int k = 0; k < 2; ++k) load_to_lds(rk, koff, 4 * k * row_bytes, lds_k + wk.to * (kStep * kNope * 2) + (2 * wave + k) * 1024);
-        load_to_lds(rr, roff, 0, lds_r + wk.to * (kStep * kRope * 2) + wave * 1024);
         wk.from += (size_t)kHalves * kStep * row_bytes;
+    };
+    auto fetch_r = [&] {                                       // behind fetch_k
+        const u32x4_t rr = window(rope_from, bytes_of(wk.left, rope_bytes, kRope * 2));
+        load_to_lds(rr, roff, 0, lds_r + wk.to * (kStep * kRope * 2) + wave * 1024);
         rope_from += (size_t)kHalves * kStep * rope_bytes;
         wk.left -= kHalves * kStep;
         wk.to = wk.to == kRingK - 1 ? 0 : wk.to + 1;
@@ -139,10 +142,11 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         wv.to = wv.to == kRingV - 1 ? 0 : wv.to + 1;
     };
     // Entering step s, K of s + 2 and V of s have landed; the step fetches K of s + 4 and V of s + 2, whose places were last read in step s - 1 or before.
-    fetch_k();
-    fetch_k();
-    fetch_k(); fetch_v();
-    fetch_k(); fetch_v();
+    for (int i = 0; i < kRingK; ++i) {
+        fetch_k();
+        fetch_r();
+        if (i >= kRingK - 2) fetch_v();
+    }
 
     f32x4_t acc[8][2], sum[2];                                 // sum: of the rounded weights, in every element (V^T of ones)
     float ref[2] = {0.f, 0.f};                                 // of the weights, in units of log2
@@ -203,6 +207,9 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         slots(std::make_integer_sequence<int, 12>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
             if constexpr (!kLast) score_slot(mi);
+            if constexpr (mm == 1) fetch_k();
+            if constexpr (mm == 3) fetch_r();
+            if constexpr (mm == 5) fetch_v();
             if constexpr (mm < 8) {                            // two logits a slot, against the reference so far
                 constexpr int qb = mm >> 2, j = 2 * (mm & 3);
 #pragma unroll
@@ -299,8 +306,6 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     auto enter = [&] {
         wait_fetches<5>();                                     // K of s + 2 and V of s; what step s - 1 fetched is under way
         tile_barrier();
-        fetch_k();
-        fetch_v();
     };
     int s = 0;
 #pragma unroll 1
@@ -313,7 +318,12 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         step(std::true_type{}, s, scA);
         ++s;
     }
-    for (; s < steps; ++s) enter();                           // the steps that only later wavefronts have
+    for (; s < steps; ++s) {                                   // the steps that only later wavefronts have
+        enter();
+        fetch_k();
+        fetch_r();
+        fetch_v();
+    }
     wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
     if constexpr (kHalves == 2) {                              // the second half's sums to the first, in the rings' place
         tile_barrier();
