@@ -14,9 +14,9 @@ namespace fd {
 namespace {
 
 // ---- rows in and out ----
-// A row is read, coded and written within eight lanes, 16 elements to a lane (read back: 16 lanes, eight elements to a lane).  The arithmetic is in fp32: the
-// differences and the division are rounded once each.  What bounds the coding is its vector instructions, some 15 an element; with eight elements
-// to a lane the places and the two divisions of a group cost as much again (16001 tokens x 8 heads, fp16: 26.8 us so, 20.3 with 16).  Reading back is bound by memory.
+// A row is read, coded and written within eight lanes, 16 elements to a lane; with eight elements to a lane the places and the two divisions of a group cost as much as the codes
+// (16001 tokens x 8 heads, fp16: 26.8 us so, 18.6 with 16).  The arithmetic is in fp32: the differences and the division are rounded once each.  What bounds the coding is its
+// vector instructions, some 16 an element with all else, next to memory (84 MB).  Reading back is bound by memory (84 MB): the rows leave past the caches (18.8 us without, 17.5 so).
 
 template <class F> __device__ __forceinline__ float group_reduce(float x, int lanes, F f)
 {
@@ -63,23 +63,21 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
         f[2 * i] = T::lo(w);
         f[2 * i + 1] = T::hi(w);
     }
-    float lo = f[0], hi = f[0], odd = 0.f;                                  // odd: NaN where an element is infinite or NaN ...
+    float lo = f[0], hi = f[0];                                             // NaN where an element is
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        lo = fminf(lo, f[i]);
-        hi = fmaxf(hi, f[i]);
-        odd = __builtin_fmaf(f[i], 0.f, odd);
+    for (int i = 1; i < 16; ++i) {
+        lo = __builtin_elementwise_minimum(lo, f[i]);
+        hi = __builtin_elementwise_maximum(hi, f[i]);
     }
     const int lanes = 8 / pool.NG;
-    lo = group_reduce(lo, lanes, [](float a, float b) { return fminf(a, b); });
-    hi = group_reduce(hi, lanes, [](float a, float b) { return fmaxf(a, b); });
-    odd = group_reduce(odd, lanes, [](float a, float b) { return a + b; });
+    lo = group_reduce(lo, lanes, [](float a, float b) { return __builtin_elementwise_minimum(a, b); });
+    hi = group_reduce(hi, lanes, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
     // The scale as it is stored is the one that the codes are taken against.  Quotients are those of fp32 division: with r = 1 / s rounded, q = t r and one correction, q +
     // r (t - q s), give the correctly rounded t / s (Markstein) where nothing leaves the range of normal numbers; where it might, divisions do.  (With a division for
-    // each element the call was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)
+    // each element the call was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)  A scale that is a normal number is off by 2^-8 of itself at
+    // most, so that no quotient passes 15.5 and has to be limited.
     const float span = hi - lo;
-    odd = __builtin_fmaf(span, 0.f, odd);                                   // (or where the group's range is)
-    const bool ordinary = (span > 0x1p-80f && span < 0x1p100f) || span == 0.f;
+    const bool ordinary = (span >= 15.5f * T::kSmallest && span < 0x1p100f) || span == 0.f;
     constexpr float kFifteenth = 1.f / 15.f;
     float fifteenth = span * kFifteenth;
     fifteenth = __builtin_fmaf(__builtin_fmaf(-fifteenth, 15.f, span), kFifteenth, fifteenth);
@@ -87,24 +85,25 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
     unsigned short s_bits = T::bits(fifteenth), l_bits = T::bits(lo);
     const float s = T::lo(s_bits), inv = 1.f / s;
     float quarter[4] = {0.f, 0.f, 0.f, 0.f};                                // four codes each: whole numbers below 2^16
-    auto put = [&](int i, float q) { quarter[i >> 2] = __builtin_fmaf(quarter[i >> 2], 16.f, fminf(__builtin_rintf(q), 15.f)); };       // (t is not negative)
+    auto put = [&](int i, float c) { quarter[i >> 2] = __builtin_fmaf(quarter[i >> 2], 16.f, c); };
     if (__all(ordinary)) {
 #pragma unroll
         for (int i = 15; i >= 0; --i) {
             const float t = f[i] - lo, q = t * inv;
-            put(i, __builtin_fmaf(__builtin_fmaf(-q, s, t), inv, q));
+            put(i, __builtin_rintf(__builtin_fmaf(__builtin_fmaf(-q, s, t), inv, q)));
         }
     } else {
 #pragma unroll
-        for (int i = 15; i >= 0; --i) put(i, (f[i] - lo) / s);
+        for (int i = 15; i >= 0; --i) put(i, fminf(__builtin_rintf((f[i] - lo) / s), 15.f));       // (t is not negative)
     }
+    const bool odd = !(span < INFINITY);                                    // an infinite element, a NaN or such a range
     unsigned word[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         word[i] = (unsigned)quarter[2 * i] | ((unsigned)quarter[2 * i + 1] << 16);
-        if (odd != 0.f || !(s > 0.f)) word[i] = 0;                          // (what was put together is NaN, then)
+        if (odd || !(s > 0.f)) word[i] = 0;                                 // (what was put together is NaN, then)
     }
-    if (odd != 0.f) s_bits = l_bits = 0x7fff;                               // NaN in both types: the group reads as NaN
+    if (odd) s_bits = l_bits = 0x7fff;                               // NaN in both types: the group reads as NaN
     unsigned *codes = reinterpret_cast<unsigned *>((at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64);
     const int place = at.is_v ? 2 * j : 8 * (j & 1) + (j >> 1), apart = at.is_v ? 1 : 4;
     codes[place] = word[0];
@@ -117,21 +116,26 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
 
 template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(NibblePool pool, NibbleRows rows)
 {
-    const unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int j = threadIdx.x & 15;
-    const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, r);
+    const unsigned row = blockIdx.x * 32 + (threadIdx.x >> 3);
+    const int j = threadIdx.x & 7;                                          // elements from 8 j and from 64 + 8 j: stores of eight lanes lie side by side
+    const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, row);
     if (!at.live) return;
-    const unsigned char *codes = (at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64;
-    const unsigned word = *reinterpret_cast<const unsigned *>(codes + 4 * (at.is_v ? j : 4 * (j & 3) + (j >> 2)));
+    const unsigned *codes = reinterpret_cast<const unsigned *>((at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64);
+    const int place = at.is_v ? j : 4 * (j & 3) + (j >> 2), apart = at.is_v ? 8 : 2;
+    const unsigned word[2] = {codes[place], codes[place + apart]};
     const uint16_t *scales = (at.is_v ? pool.v_scales : pool.k_scales) + at.row * (2 * pool.NG);
-    const int g = j / (16 / pool.NG);
-    const float s = T::lo(scales[g]), l = T::lo(scales[pool.NG + g]);
-    u32x4_t x;
+    u32x4_t *dst = reinterpret_cast<u32x4_t *>((at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim) + j;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)                                             // s c is exact in fp32: one rounding there, one to the type
-        x[i] = T::pack(__builtin_fmaf(s, (float)((word >> (8 * i)) & 15), l), __builtin_fmaf(s, (float)((word >> (8 * i + 4)) & 15), l));
-    uint16_t *dst = (at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim + 8 * j;
-    *reinterpret_cast<u32x4_t *>(dst) = x;
+    for (int w = 0; w < 2; ++w) {
+        const int g = (j + 8 * w) * pool.NG >> 4;
+        const float s = T::lo(scales[g]), l = T::lo(scales[pool.NG + g]);
+        const unsigned even = word[w] & 0x0f0f0f0fu, odd = (word[w] >> 4) & 0x0f0f0f0fu;       // bytes, of which a conversion takes any
+        u32x4_t x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)                                         // s c is exact in fp32: one rounding there, one to the type
+            x[i] = T::pack(__builtin_fmaf(s, (float)((even >> (8 * i)) & 255), l), __builtin_fmaf(s, (float)((odd >> (8 * i)) & 255), l));
+        __builtin_nontemporal_store(x, dst + 8 * w);
+    }
 }
 
 // ---- attention ----
@@ -674,7 +678,7 @@ hipError_t launch_nibble_write(const NibblePool &pool, const NibbleRows &rows, h
 }
 hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
 {
-    const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 15) / 16));
+    const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
     return pool.dtype == kF16 ? launch(nibble_read_kernel<F16>, grid, dim3(256), s, pool, rows) : launch(nibble_read_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
 template <class T, int DIM> static hipError_t join(const JoinProblem &p, hipStream_t s)
