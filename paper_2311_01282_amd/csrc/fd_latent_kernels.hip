@@ -80,6 +80,8 @@ typedef __attribute__((address_space(4))) const int32_t *scalar_i32;      // rea
 
 template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW, 2) void latent_decode_kernel(LatentProblem p)
 {
+    // (a step's tiles are taken together: their weights wait for one maximum, their reads run ahead over both -- 256 sequences of 1024 keys, 128 heads: 101 us one by one, 97 so,
+    // 92 with the scaling in the exponents' multiply-adds and the sum of weights on the matrix cores)
     constexpr int NH = NW / DS, kDt = 32 / DS;                 // groups of 16 heads; tiles of 16 elements of a wavefront
     constexpr bool kTwoParts = NW < 8;                         // of a weight
     constexpr int kKeys = TPW * kTile, kRows = kKeys / NW;     // keys of a step; rows that a wavefront fetches
@@ -151,12 +153,15 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
             const int kb = kParts * i + odd;
             q[i] = *reinterpret_cast<const u32x4_t *>(kParts * i < 16 ? p.q_latent + row * kLatent + 32 * kb + 8 * g : p.q_rope + row * kRope + 32 * (kb - 16) + 8 * g);
         }
+        q[i] ^= p.scale < 0.f ? 0x80008000u : 0u;               // (the largest product is then the largest logit)
     }
     f32x4_t acc[kDt];
 #pragma unroll
     for (int dt = 0; dt < kDt; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    const float c1 = p.scale * kLog2e;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};                        // of rounded weights, in every element (C^T of ones); else of this lane's, in l
+    const unsigned one2 = T::pack(1.f, 1.f);
+    const float c1 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);   // (not 0: of a masked score it has to leave -inf)
     // this lane's operand reads: piece 4 kb + g of row k_row; 32 bytes from element 16 dt of row v_row.  Pieces within 256 bytes differ by an exclusive or.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
     const int k_first = k_row + (DS == 1 ? 0 : 4 * (part & 1));
@@ -172,111 +177,123 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
         tile_barrier();                                        // ... for every wavefront, all of which are through with step s - 1
         fetch(s + kSteps - 1);
         if (heads <= 0) continue;
-#pragma unroll 1
-        for (int i = 0; i < TPW; ++i) {
-            const unsigned tile_c = lds_c + (s % kSteps * TPW + i) * (kTile * kCBytes), tile_r = lds_r + (s % kSteps * TPW + i) * (kTile * kRBytes);
-            f32x4_t sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            {
-                const unsigned kc = tile_c + k_at, kr = tile_r + kr_at;
-                auto read = [&](int i, int t) {
-                    const int kb = kParts * i;
-                    const unsigned x = kb < 16 ? (kc ^ ((kb & 3) << 6)) + ((kb >> 2) << 8) + t * 4 * kCBytes : (kr ^ ((kb & 1) << 6)) + t * 4 * kRBytes;
-                    return *(lds_u32x4)(uintptr_t)x;
-                };
-                // reads run kAhead operands ahead of the instructions that use them
-                constexpr int kAhead = 3;
-                u32x4_t a[kAhead + 1][kBlocks];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-                    for (int t = 0; t < kBlocks; ++t) a[i][t] = read(i, t);
-#pragma unroll
-                for (int i = 0; i < kOperands; ++i) {
-                    if (i + kAhead < kOperands)
-#pragma unroll
-                        for (int t = 0; t < kBlocks; ++t) a[(i + kAhead) % (kAhead + 1)][t] = read(i + kAhead, t);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int t = 0; t < kBlocks; ++t) {
-                        const int to = kBlocks == 1 ? i & 1 : t;             // (of one block: two chains)
-                        sc[to] = T::mfma(a[i % (kAhead + 1)][t], q[i], sc[to]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if constexpr (DS > 1) {                            // the wavefronts of 16 heads exchange their parts
-                lds.x[wave % NH][part][lane] = sc[0] + sc[1];
-                tile_barrier();
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    sc[t] = lds.x[wave % NH][t][lane];
-                    if constexpr (DS == 4) sc[t] += lds.x[wave % NH][t + 2][lane];
-                }
-            }
-            const unsigned vc = tile_c + v_at + 2 * d0;
-            auto read = [&](int dt) {
-                const unsigned x = (vc ^ ((dt & 7) << 5)) + ((dt >> 3) << 8);
-                const s16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)x);
-                const s16x4_t w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(x + 4 * kCBytes));
-                return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
+        const unsigned tile_c = lds_c + s % kSteps * (kKeys * kCBytes), tile_r = lds_r + s % kSteps * (kKeys * kRBytes);
+        f32x4_t sc[TPW][2];
+        {
+            const unsigned kc = tile_c + k_at, kr = tile_r + kr_at;
+            auto read = [&](int op) {                          // of tile op / kOperands / kBlocks
+                const int i = op / (kOperands * kBlocks), t = op % kBlocks, kb = op / kBlocks % kOperands * kParts;
+                const unsigned x = kb < 16 ? (kc ^ ((kb & 3) << 6)) + ((kb >> 2) << 8) + t * 4 * kCBytes + i * (kTile * kCBytes) : (kr ^ ((kb & 1) << 6)) + t * 4 * kRBytes + i * (kTile * kRBytes);
+                return *(lds_u32x4)(uintptr_t)x;
             };
-            constexpr int kAhead = 4;
+            // reads run kAhead operands ahead of the instructions that use them
+            constexpr int kOps = TPW * kOperands * kBlocks, kAhead = 3 + (TPW == 1);
             u32x4_t a[kAhead + 2];
 #pragma unroll
-            for (int d = 0; d < kAhead; ++d) a[d] = read(d);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < TPW; ++i) sc[i][0] = sc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int op = 0; op < kAhead; ++op) a[op] = read(op);
+#pragma unroll
+            for (int op = 0; op < kOps; op += kBlocks) {
+#pragma unroll
+                for (int t = 0; t < kBlocks; ++t)
+                    if (op + t + kAhead < kOps) a[(op + t + kAhead) % (kAhead + 2)] = read(op + t + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < kBlocks; ++t) {
+                    const int i = op / (kOperands * kBlocks), at = op / kBlocks % kOperands, to = kBlocks == 1 ? at & 1 : t;             // (of one block: two chains)
+                    sc[i][to] = T::mfma(a[(op + t) % (kAhead + 2)], q[at], sc[i][to]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (DS > 1) {                                // the wavefronts of 16 heads exchange their parts
+            static_assert(TPW == 1);
+            lds.x[wave % NH][part][lane] = sc[0][0] + sc[0][1];
+            tile_barrier();
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                sc[0][t] = lds.x[wave % NH][t][lane];
+                if constexpr (DS == 4) sc[0][t] += lds.x[wave % NH][t + 2][lane];
+            }
+        }
+        const unsigned vc = tile_c + v_at + 2 * d0;
+        // the output's operands: two tiles of elements, each of all tiles of keys, and on
+        auto read = [&](int op) {
+            const int dt = op / (2 * TPW) * 2 + op % 2, i = op / 2 % TPW;
+            const unsigned x = (vc ^ ((dt & 7) << 5)) + ((dt >> 3) << 8) + i * (kTile * kCBytes);
+            const s16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)x);
+            const s16x4_t w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(x + 4 * kCBytes));
+            return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        constexpr int kOps = TPW * kDt, kAhead = 4;
+        u32x4_t a[kAhead + 2];
+#pragma unroll
+        for (int op = 0; op < kAhead; ++op) a[op] = read(op);
+        __builtin_amdgcn_sched_barrier(0);
 
-            const int left = end - (start + s * kKeys + i * kTile);         // keys from the tile's first
+        const int left = end - (start + s * kKeys);            // keys from the step's first
+        float top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] *= c1;
-            if (left < kTile) {
+        for (int i = 0; i < TPW; ++i) {
+            if (left < kKeys) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sc[j >> 2][j & 3] = 8 * g + j < left ? sc[j >> 2][j & 3] : -INFINITY;
+                for (int j = 0; j < 8; ++j) sc[i][j >> 2][j & 3] = kTile * i + 8 * g + j < left ? sc[i][j >> 2][j & 3] : -INFINITY;
             }
-            float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-            top = columns_max(top);
-            if (__any(top > m + kSlack)) {                     // (also where there is no reference yet)
-                const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-                l *= f;
+            top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3])), fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3]))));
+        }
+        top = columns_max(top) * c1;
+        if (__any(top > m + kSlack)) {                         // (also where there is no reference yet)
+            const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            l *= f;
 #pragma unroll
-                for (int dt = 0; dt < kDt; ++dt)
+            for (int r = 0; r < 4; ++r) sum[r] *= f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[dt][r] *= f;
-                m = to;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-            u32x4_t hi, lo;
+            for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[dt][r] *= f;
+            m = to;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        u32x4_t hi[TPW], lo[TPW];
+#pragma unroll
+        for (int i = 0; i < TPW; ++i)
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(sc[j >> 2][j & 3] - ref), e1 = __builtin_amdgcn_exp2f(sc[j >> 2][(j & 3) + 1] - ref);
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][j >> 2][j & 3], c1, -ref)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][j >> 2][(j & 3) + 1], c1, -ref));
                 const unsigned h = T::pack(e0, e1);
-                hi[j >> 1] = h;
+                hi[i][j >> 1] = h;
                 if constexpr (kTwoParts) {
                     l += e0 + e1;
-                    lo[j >> 1] = T::pack(e0 - T::lo(h), e1 - T::hi(h));
-                } else {
-                    l += T::lo(h) + T::hi(h);
+                    lo[i][j >> 1] = T::pack(e0 - T::lo(h), e1 - T::hi(h));
                 }
             }
+        if constexpr (!kTwoParts)
 #pragma unroll
-            for (int dt = 0; dt < kDt; dt += 2) {
+            for (int i = 0; i < TPW; ++i) sum = T::mfma(u32x4_t{one2, one2, one2, one2}, hi[i], sum);
 #pragma unroll
-                for (int d = 0; d < 2; ++d)
-                    if (dt + d + kAhead < kDt) a[(dt + d + kAhead) % (kAhead + 2)] = read(dt + d + kAhead);
-                __builtin_amdgcn_sched_barrier(0);
+        for (int op = 0; op < kOps; op += 2) {
+            const int dt = op / (2 * TPW) * 2, i = op / 2 % TPW;
 #pragma unroll
-                for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(dt + d) % (kAhead + 2)], hi, acc[dt + d]);
-                if constexpr (kTwoParts)
+            for (int d = 0; d < 2; ++d)
+                if (op + d + kAhead < kOps) a[(op + d + kAhead) % (kAhead + 2)] = read(op + d + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(dt + d) % (kAhead + 2)], lo, acc[dt + d]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(op + d) % (kAhead + 2)], hi[i], acc[dt + d]);
+            if constexpr (kTwoParts)
+#pragma unroll
+                for (int d = 0; d < 2; ++d) acc[dt + d] = T::mfma(a[(op + d) % (kAhead + 2)], lo[i], acc[dt + d]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     wait_fetches<0>();                                         // (nothing may land in LDS after the workgroup's end)
     if (n >= heads) return;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    if constexpr (kTwoParts) {
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+    } else {
+        l = sum[0];
+    }
     const size_t row = (size_t)b * p.H + head0 + n;
     if (len <= p.C) {                                          // the only chunk with keys
         const float inv = 1.f / l;
