@@ -187,7 +187,7 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
                 return *(lds_u32x4)(uintptr_t)x;
             };
             // reads run kAhead operands ahead of the instructions that use them
-            constexpr int kOps = TPW * kOperands * kBlocks, kAhead = 3 + (TPW == 1);
+            constexpr int kOps = TPW * kOperands * kBlocks, kAhead = 3;
             u32x4_t a[kAhead + 2];
 #pragma unroll
             for (int i = 0; i < TPW; ++i) sc[i][0] = sc[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -240,7 +240,8 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sc[i][j >> 2][j & 3] = kTile * i + 8 * g + j < left ? sc[i][j >> 2][j & 3] : -INFINITY;
             }
-            top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][0][2], sc[i][0][3])), fmaxf(fmaxf(sc[i][1][0], sc[i][1][1]), fmaxf(sc[i][1][2], sc[i][1][3]))));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = __builtin_elementwise_maximum(top, sc[i][j >> 2][j & 3]);        // (of a NaN or not: of one the output is NaN anyway)
         }
         top = columns_max(top) * c1;
         if (__any(top > m + kSlack)) {                         // (also where there is no reference yet)
