@@ -1,7 +1,7 @@
 // Latent attention over a paged cache: one row of 576 elements a token -- 512 that stand for the keys and values of all heads, 64 rotary ones
 // that all heads share -- and queries that the caller has taken into the latent space (the absorbed form):
 //     x_j = scale (q_latent . c_j + q_rope . r_j),   out = sum_j softmax(x)_j c_j.
-// Every head reads the same rows, as keys and as values: a row is fetched once for 64 heads.
+// Every head reads the same rows, as keys and as values: a row is fetched once for up to 128 heads.
 #include "fd_chunk.h"
 #include "fd_cache.h"
 #include "fd_types.h"
@@ -34,7 +34,8 @@ __global__ __launch_bounds__(kPieces * kWriteTokens) void latent_write_kernel(La
 // ones (64 x 128 heads x 4096 keys: 106 us with two, 93 with one).
 // A wavefront owns 16 heads: 72 registers of queries and 128 of sums.  A workgroup of NW wavefronts takes 16 NH heads of a sequence and a chunk of its keys,
 // TPW tiles of 32 at a time, which all its wavefronts fetch straight into LDS while they work on those before.  Where there are fewer heads than wavefronts, DS = NW / NH
-// of them share 16 heads: all form the weights, each adds up its part of the elements.
+// of them share 16 heads: of the scores each forms a part (one of the two key blocks, of four wavefronts every other operand of one) and finds the others' in LDS, then all form the
+// weights, and each adds up its part of the elements (all scores by each: 1 x 16 heads x 2048 keys 10.9 us, 8.9 so).
 constexpr int kTile = 32;
 // The reference of a head's weights follows its maximum only where that has grown by more than this (in units of log2): weights are at most 2^8 then, and
 // the sums, 128 registers of a wavefront, are brought to another reference once or twice a chunk; of 16 heads some maximum grows in most tiles.

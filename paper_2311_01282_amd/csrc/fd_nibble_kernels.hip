@@ -16,7 +16,7 @@ namespace {
 // ---- rows in and out ----
 // A row is read, coded and written within eight lanes, 16 elements to a lane; with eight elements to a lane the places and the two divisions of a group cost as much as the codes
 // (16001 tokens x 8 heads, fp16: 26.8 us so, 18.6 with 16).  The arithmetic is in fp32: the differences and the division are rounded once each.  What bounds the coding is its
-// vector instructions, some 16 an element with all else, next to memory (84 MB).  Reading back is bound by memory (84 MB): the rows leave past the caches (18.8 us without, 17.5 so).
+// vector instructions, some 16 an element with all else, next to memory (91 MB).  Reading back is bound by memory (84 MB): the rows leave past the caches (18.8 us without, 17.5 so).
 
 template <class F> __device__ __forceinline__ float group_reduce(float x, int lanes, F f)
 {
