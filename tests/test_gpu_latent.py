@@ -298,11 +298,26 @@ def test_prompts_with_large_logits(dtype):
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.07])
-def test_prompts_with_scales_of_zero_and_below(scale):
-    q, kv, rope = prompt(torch.float16, [170, 33], 3, 200, 64, 5)
-    got = prefill(q, kv, rope, torch.tensor([170, 33], dtype=torch.int32, device=DEV), scale)
+@pytest.mark.parametrize("lens,max_seq", [([170, 33], 200), ([300, 64], 320)])
+def test_prompts_with_scales_of_zero_and_below(scale, lens, max_seq):
+    q, kv, rope = prompt(torch.float16, lens, 3, max_seq, 64, 5)
+    got = prefill(q, kv, rope, torch.tensor(lens, dtype=torch.int32, device=DEV), scale)
     torch.cuda.synchronize()
-    check_prompt(got, q, kv, rope, [170, 33], scale)
+    check_prompt(got, q, kv, rope, lens, scale)
+
+
+def test_a_prompt_does_not_see_later_keys():
+    """Infinite and NaN keys and rotary parts behind a query do not reach it, in either form of the launch."""
+    for max_seq in (224, 420):
+        n = max_seq - 4
+        q, kv, rope = prompt(torch.bfloat16, [n], 2, max_seq, 64, 9)
+        lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+        clean = prefill(q, kv, rope, lens, 0.07)
+        kv[0, 150, 0, 5], kv[0, 170, 0, 7], rope[0, 200, 3] = float("nan"), float("inf"), float("nan")
+        got = prefill(q, kv, rope, lens, 0.07)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0, :150, 0], clean[0, :150, 0]) and torch.equal(got[0, :200, 1], clean[0, :200, 1])
+        assert got[0, 150:n, 0].isnan().all() and got[0, 200:n, 1].isnan().all()
 
 
 def test_prompts_beyond_32_bits():
