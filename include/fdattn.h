@@ -554,8 +554,8 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
  * Decode attention over the 4-bit cache: out = softmax(scale q K^T) V with the values that the codes stand for (unrounded).
  * q, out [batch, n_q_heads, 128] of the pool's dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of
  * 64 from 64 to 16384 keys, for example fd_nibble_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
- * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of dtype each (22
- * significant bits in fp16, down to 2^-24, 16 in bf16).  A sequence of length 0 gives zero rows.  One launch for up to 16
+ * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of bf16 each, 16
+ * significant bits whatever their size (values beyond 2^100 may overflow the fp32 sums).  A sequence of length 0 gives zero rows.  One launch for up to 16
  * chunks a row and up to 512 workgroups (one for each chunk of up to 16 heads that share a KV head), else two.
  */
 size_t    fd_nibble_workspace_bytes(const fd_shape *shape);

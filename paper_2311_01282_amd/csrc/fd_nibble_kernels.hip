@@ -145,8 +145,9 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 //     sum_d q_d (l_g + s_g c_d) = sum_g s_g (sum_{d in g} q_d c_d) + l_g (sum_{d in g} q_d),
 // four matrix instructions a row, one a group of 32, and a multiply-add with s and one with l a group; the 16 is taken off in the term with l.  Of the output
 //     sum_j p_j (l_jg + s_jg c_jd) = sum_j (p_j s_jg) (16 + c_jd) + sum_j p_j (l_jg - 16 s_jg),
-// the weights p s of a group as the operand, in two parts of the type (hi + lo: 16 significant bits in bf16, 22 in fp16; one part alone
-// would add an error as large as the output's rounding), the last sum in fp32.
+// the weights p s of a group as the operand, in two numbers of bf16 whatever the cache's type (hi + lo: 16 significant bits; one alone would add an error as
+// large as the output's rounding), the last sum in fp32.  Of fp16 they would be 22 bits where p s is large, but nothing below 2^-25, and the two sums then disagree by
+// up to 31 times that a key, however small the values are (16384 keys, logits of deviation 3, values of 0.01: 2 % of the output; 4e-6 so).
 //
 // Lanes (16 x 16 x 32): n = lane % 16, c = lane / 16.  Scores of 16 query heads (rows) and 16 keys (columns): the lane of a key has its
 // scales in registers.  Query head h of a tile sits in row 4 (h % 4) + h / 4, so that R = ceil(heads / 4) of a lane's four rows are in use.
@@ -162,11 +163,12 @@ constexpr int kJoinWorkgroups = 512;             // of a launch that joins its r
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
 constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
 
-// kSlack: the reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.  In fp16 a weight times
-// its scale, which may be (65504 + 65504) / 15, has to be a number of the type: four times that is.  (32 x 64/8 heads x 4096 keys, bf16: 37.5 us with 2, 37.0 with 8.)
+// The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.
+// (32 x 64/8 heads x 4096 keys, bf16: 37.5 us with 2, 37.0 with 8.)
+constexpr float kSlack = 8.f;
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
-template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; static constexpr float kSlack = 2.f; };
-template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; static constexpr float kSlack = 8.f; };
+template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; };
+template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; };
 
 // Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).  sixteen: Magic::kSixteen in a register the compiler cannot see through, which keeps
 // "and" and "or" one instruction (of two constants only one can be other than a register).
@@ -325,8 +327,9 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     }
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    unsigned sixteen;
+    unsigned sixteen, sixteen_v;                   // of K, whose products are with queries of type T, and of V
     asm("v_mov_b32 %0, %1" : "=v"(sixteen) : "i"(Magic<T>::kSixteen));
+    asm("v_mov_b32 %0, %1" : "=v"(sixteen_v) : "i"(Magic<BF16>::kSixteen));
 
     unsigned char *w_at = lds.w[wave][0][0];
     constexpr int kLo = 4 * R * kRowStride, kTurn = 2 * kLo;               // from a hi part to its lo part, from a group to the next
@@ -406,7 +409,7 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             top[r] = row16_max(fmaxf(fmaxf(z[0][r], z[1][r]), fmaxf(z[2][r], z[3][r])));
-            grew |= top[r] > m[r] + Magic<T>::kSlack;
+            grew |= top[r] > m[r] + kSlack;
         }
         if (__any(grew)) {                                                             // (also where there is no reference yet)
 #pragma unroll
@@ -441,10 +444,10 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
                     low[r][g] = __builtin_fmaf(z[i][r], l0, low[r][g]);
                     low[r][g] = __builtin_fmaf(z[i + 1][r], l1, low[r][g]);
                     const float w0 = z[i][r] * s0, w1 = z[i + 1][r] * s1;
-                    const unsigned h = T::pack(w0, w1);
+                    const unsigned h = BF16::pack(w0, w1);
                     unsigned char *at = w_at + (g & 1) * kTurn + (R * c + r) * kRowStride + 32 * i + 4 * n;
                     *reinterpret_cast<unsigned *>(at) = h;
-                    *reinterpret_cast<unsigned *>(at + kLo) = T::pack(w0 - T::lo(h), w1 - T::hi(h));
+                    *reinterpret_cast<unsigned *>(at + kLo) = BF16::pack(w0 - BF16::lo(h), w1 - BF16::hi(h));
                 }
             }
         };
@@ -462,7 +465,7 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
         for (int d = 0; d < 2; ++d)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) e[d][u] = expand<T>((unsigned)vc[0][d][u], sixteen);
+            for (int u = 0; u < 2; ++u) e[d][u] = expand<BF16>((unsigned)vc[0][d][u], sixteen_v);
         u32x4_t ah[2], al[2];
 #pragma unroll
         for (int pr = 0; pr < 4; ++pr) {
@@ -490,15 +493,15 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
 #pragma unroll
-                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = T::mfma(ah[u], e[d][u], acc[2 * pr + d]);
+                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = BF16::mfma(ah[u], e[d][u], acc[2 * pr + d]);
 #pragma unroll
-                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = T::mfma(al[u], e[d][u], acc[2 * pr + d]);
+                for (int d = 0; d < 2; ++d) acc[2 * pr + d] = BF16::mfma(al[u], e[d][u], acc[2 * pr + d]);
             }
             if (pr < 3) {
 #pragma unroll
                 for (int d = 0; d < 2; ++d)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) en[d][u] = expand<T>((unsigned)vc[(pr + 1) & 1][d][u], sixteen);
+                    for (int u = 0; u < 2; ++u) en[d][u] = expand<BF16>((unsigned)vc[(pr + 1) & 1][d][u], sixteen_v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
