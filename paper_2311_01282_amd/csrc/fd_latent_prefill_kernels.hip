@@ -236,12 +236,14 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             if constexpr (mm == 11) top[1] = columns_max(top[1]);
             __builtin_amdgcn_sched_barrier(0);
         });
-        if (s == 0 || __any((top[0] > kSlack) | (top[1] > kSlack))) {              // relative to the reference
+        // Relative to the reference, which a query whose logits have all been -inf does not have yet: none of its weights is above 0, and any number becomes it.
+        const bool none[2] = {sum[0][0] == 0.f, sum[1][0] == 0.f};
+        if (__any((top[0] > (none[0] ? -INFINITY : kSlack)) | (top[1] > (none[1] ? -INFINITY : kSlack)))) {
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) {
-                float d = s == 0 ? top[qb] : fmaxf(top[qb], 0.f);
+                float d = none[qb] ? top[qb] : fmaxf(top[qb], 0.f);
                 d = d == -INFINITY ? 0.f : d;
-                const float f = __builtin_amdgcn_exp2f(-d);
+                const float f = none[qb] ? 1.f : __builtin_amdgcn_exp2f(-d);
                 ref[qb] += d;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[qb][j] -= d;
@@ -329,12 +331,13 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
     if constexpr (kHalves == 2) {                              // the second half's sums to the first, in the rings' place
         tile_barrier();
+        auto reference = [&](int qb) { return sum[qb][0] == 0.f ? -INFINITY : ref[qb]; };      // (-inf: none, as in step)
         if (half == 1) {
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) {
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) both.sums[wave][8 * qb + dt][lane] = acc[dt][qb];
-                both.sums[wave][16 + qb][lane] = f32x4_t{sum[qb][0], ref[qb], 0.f, 0.f};
+                both.sums[wave][16 + qb][lane] = f32x4_t{sum[qb][0], reference(qb), 0.f, 0.f};
             }
         }
         tile_barrier();
@@ -343,7 +346,7 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) {
                 const f32x4_t x = both.sums[wave][16 + qb][lane];
-                const float top = fmaxf(ref[qb], x[1]), f0 = __builtin_amdgcn_exp2f(ref[qb] - top), f1 = __builtin_amdgcn_exp2f(x[1] - top);
+                const float own = reference(qb), top = fmaxf(own, x[1]), f0 = __builtin_amdgcn_exp2f(own - top), f1 = __builtin_amdgcn_exp2f(x[1] - top);
                 sum[qb][0] = sum[qb][0] * f0 + x[0] * f1;
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
