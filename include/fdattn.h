@@ -600,8 +600,7 @@ fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *poo
  *        latent rows can be given as they are; sequences max_seq rows apart)
  *   out  [batch, max_seq, n_q_heads, 128]; tokens at and behind seq_lens[b] get zero rows
  * shape: n_kv_heads == n_q_heads (<= 65535), head_dim 192; chunk is ignored.  No workspace.  Scores and sums in fp32, the weights
- * rounded to dtype for the second product; the denominator is the sum of the rounded ones.  (A value row with an infinite element or a NaN
- * can turn that element of up to 31 outputs in front of it to NaN: weights of 0 are multiplied with it.)
+ * rounded to dtype for the second product; the denominator is the sum of the rounded ones.
  */
 fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const void *q, const void *kv, const void *rope,
                                  int64_t rope_stride, const int32_t *seq_lens, void *out, void *stream);

@@ -65,6 +65,39 @@ __device__ __forceinline__ u32x4_t window(const void *base, long long bytes)
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
 }
 
+// Values that are not finite: counted in a product of their own, in which an infinite one is 1, one of the other sign 64 and a NaN 4096 (of 32 keys the counts do not meet).
+template <class T> __device__ __forceinline__ u32x4_t not_finite(u32x4_t v)
+{
+    u32x4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float f[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const unsigned h = v[i] >> (16 * k) & 0xffffu, size = h & 0x7fffu;
+            f[k] = size < T::kInfinity ? 0.f : size > T::kInfinity ? 4096.f : h == size ? 1.f : 64.f;
+        }
+        x[i] = T::pack(f[0], f[1]);
+    }
+    return x;
+}
+template <class T> __device__ __forceinline__ u32x4_t finite(u32x4_t v)          // 0 in their place
+{
+    u32x4_t x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned low = (v[i] & 0x7fffu) < T::kInfinity ? v[i] & 0xffffu : 0u, high = (v[i] >> 16 & 0x7fffu) < T::kInfinity ? v[i] & 0xffff0000u : 0u;
+        x[i] = low | high;
+    }
+    return x;
+}
+// What counts stand for as a summand.
+__device__ __forceinline__ float summand(float counts)
+{
+    const unsigned n = (unsigned)counts;
+    return (n >= 4096 ? __builtin_nanf("") : 0.f) + (n & 63 ? INFINITY : 0.f) - (n & 4032 ? INFINITY : 0.f);
+}
+
 template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) void latent_prefill_kernel(LatentPromptProblem p)
 {
     __shared__ union { PromptLds ring[kHalves]; f32x4_t sums[4][18][64]; } both;
@@ -267,6 +300,33 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             }
             __builtin_amdgcn_sched_barrier(0);
         });
+        // In the step with masks the weights of keys behind a query are 0, and 0 times an infinite value or a NaN is NaN: such values leave the product, and the queries that see
+        // them get them as a summand.  (Whether there are any: a product with 0.  In the steps before all keys are seen.)
+        if constexpr (kLast) {
+            const u32x4_t none_of = {0u, 0u, 0u, 0u};
+            f32x4_t any[2] = {zero, zero};
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) any[dt & 1] = T::mfma(av[dt], none_of, any[dt & 1]);
+            const float all_of = (any[0][0] + any[0][1]) + (any[0][2] + any[0][3]) + (any[1][0] + any[1][1]) + (any[1][2] + any[1][3]);
+            if (__any(all_of != 0.f)) {
+                u32x4_t seen[2];
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) seen[qb][j >> 1] = T::pack(j - 16 * qb <= own ? 1.f : 0.f, j + 1 - 16 * qb <= own ? 1.f : 0.f);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const u32x4_t counted = not_finite<T>(av[dt]);
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb) {
+                        const f32x4_t counts = T::mfma(counted, seen[qb], zero);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[dt][qb][r] += summand(counts[r]);
+                    }
+                    av[dt] = finite<T>(av[dt]);
+                }
+            }
+        }
         const u32x4_t ones = {one2, one2, one2, one2};
         slots(std::make_integer_sequence<int, 9>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
