@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kPieces * kWriteTokens) void latent_write_kernel(La
 // What bounds it, of 256 sequences x 1024 keys in one chunk each: memory for 16 and 32 heads (52 and 58 us, 5.8 and 5.2 TB/s), waits within a tile for 64 and 128 (74 and 92 us; of 128
 // heads matrix instructions fill 43 % of the cycles, LDS 42 %).
 constexpr int kTile = 32;
-// The reference of a head's weights follows its maximum only where that has grown by more than this (in units of log2): weights are at most 2^8 then, and
+// The reference of a head's weights follows its maximum only where that has grown by more than this (in units of log2): weights are at most 2^8 times the reference's then, and
 // the sums, 128 registers of a wavefront, are brought to another reference once or twice a chunk; of 16 heads some maximum grows in most tiles.
 constexpr float kSlack = 8.f;
 constexpr int kRowBytes = kLatentRow * 2;                      // in the cache
@@ -258,7 +258,7 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
                 for (int r = 0; r < 4; ++r) acc[dt][r] *= f;
             m = to;
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = (m == -INFINITY ? 0.f : m) - T::kLift;
         u32x4_t hi[TPW], lo[TPW];
 #pragma unroll
         for (int i = 0; i < TPW; ++i)

@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kNope = 128, kQueryDim = kNope + kRope, kStep = 32, kTileQ = 128, kRingK = 4, kRingV = 3;
 // The reference of a query's weights follows its maximum only where that has grown by more than this (in units of log2): weights are then at
-// most 2^8, and the sums are brought to another reference a few times a row instead of at every new maximum.
+// most 2^8 times the reference's, and the sums are brought to another reference a few times a row instead of at every new maximum.
 constexpr float kSlack = 8.f;
 
 struct PromptLds {
@@ -184,7 +184,7 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     }
 
     f32x4_t acc[8][2], sum[2];                                 // sum: of the rounded weights, in every element (V^T of ones)
-    float ref[2] = {0.f, 0.f};                                 // of the weights, in units of log2
+    float ref[2] = {0.f, 0.f};                                 // of the weights, in units of log2: T::kLift below the logit it was taken from
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         sum[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -271,10 +271,11 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         });
         // Relative to the reference, which a query whose logits have all been -inf does not have yet: none of its weights is above 0, and any number becomes it.
         const bool none[2] = {sum[0][0] == 0.f, sum[1][0] == 0.f};
-        if (__any((top[0] > (none[0] ? -INFINITY : kSlack)) | (top[1] > (none[1] ? -INFINITY : kSlack)))) {
+        constexpr float kMost = kSlack + T::kLift;
+        if (__any((top[0] > (none[0] ? -INFINITY : kMost)) | (top[1] > (none[1] ? -INFINITY : kMost)))) {
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) {
-                float d = none[qb] ? top[qb] : fmaxf(top[qb], 0.f);
+                float d = none[qb] ? top[qb] - T::kLift : fmaxf(top[qb] - T::kLift, 0.f);
                 d = d == -INFINITY ? 0.f : d;
                 const float f = none[qb] ? 1.f : __builtin_amdgcn_exp2f(-d);
                 ref[qb] += d;

@@ -16,6 +16,9 @@ typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 struct F16 {
     static constexpr float kSmallest = 0x1p-14f;           // normal number
     static constexpr unsigned kInfinity = 0x7c00u;         // bits
+    // log2 of a softmax weight at its reference.  Numbers below 2^-25 round to nothing: of weights from 1 downwards that is what 16384 keys leave out 17 below the largest logit, 5e-4
+    // of their sum.  With this they are counted from 2^-32, and weights up to 2^8 times the reference's still fit.
+    static constexpr float kLift = 7.f;
     static __device__ __forceinline__ float lo(unsigned w) { return (float)__builtin_bit_cast(f16x2_t, w).x; }
     static __device__ __forceinline__ float hi(unsigned w) { return (float)__builtin_bit_cast(f16x2_t, w).y; }
     static __device__ __forceinline__ unsigned short bits(float x) { const _Float16 h = (_Float16)x; return __builtin_bit_cast(unsigned short, h); }
@@ -34,6 +37,7 @@ struct F16 {
 struct BF16 {
     static constexpr float kSmallest = 0x1p-126f;
     static constexpr unsigned kInfinity = 0x7f80u;
+    static constexpr float kLift = 0.f;
     static __device__ __forceinline__ float lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
     static __device__ __forceinline__ float hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
     static __device__ __forceinline__ unsigned short bits(float x) { const __bf16 h = (__bf16)x; return __builtin_bit_cast(unsigned short, h); }
