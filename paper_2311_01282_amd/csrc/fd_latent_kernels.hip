@@ -164,7 +164,7 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     float m = -INFINITY, l = 0.f;
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};                        // of rounded weights, in every element (C^T of ones); else of this lane's, in l
     const unsigned one2 = T::pack(1.f, 1.f);
-    const float c1 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);   // (not 0: of a masked score it has to leave -inf)
+    const float c1 = fmaxf(fabsf(p.scale) * kLog2e, 0x1p-149f);  // (not 0: of a masked score it has to leave -inf; the smallest number, of other scores nothing)
     // this lane's operand reads: piece 4 kb + g of row k_row; 32 bytes from element 16 dt of row v_row.  Pieces within 256 bytes differ by an exclusive or.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
     const int k_first = k_row + (DS == 1 ? 0 : 4 * (part & 1));

@@ -192,7 +192,7 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         for (int dt = 0; dt < 8; ++dt) acc[dt][qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     const unsigned one2 = T::pack(1.f, 1.f);
-    const float c1 = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);     // (not 0: of a masked score it has to leave -inf)
+    const float c1 = fabsf(p.scale) * kLog2e;
     // This lane's operand reads: piece 4 kb + g of row k_row (+ 4 t: the same places), 32 bytes from element 16 dt of row v_row.  Those of a row differ by an exclusive or
     // with a constant.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
