@@ -514,8 +514,8 @@ fd_status fd_cache_workspace_init(fd_workspace ws, void *stream);
  *   slot_map     [max_tokens] out: slot of each token; -1 for tokens of requests that are not served, for tokens whose
  *                page (a table entry held before) is out of range, and behind the last token
  *   n_left       [1] out: pages still in the list, free_pages[0 .. *n_left - 1]
- * free_pages has room for n_pages entries; *n_free (device) is clamped to [0, n_pages].  Outputs must not overlap inputs or one
- * another.  pages_per_seq * page_size and n_pages * page_size < 2^31, max_tokens <= 2^30.  Pointers 4-byte aligned.  One launch.
+ * free_pages has room for n_pages entries; *n_free (device) is clamped to [0, n_pages].  Outputs that overlap inputs (seq_lens
+ * and cached_lens, n_left and n_free among them) or one another are refused (FD_ERR_SHAPE).  pages_per_seq * page_size and n_pages * page_size < 2^31, max_tokens <= 2^30.  Pointers 4-byte aligned.  One launch.
  */
 fd_status fd_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int32_t pages_per_seq, int32_t max_tokens,
                          const int32_t *cached_lens, const int32_t *new_lens, const int32_t *free_pages, const int32_t *n_free,

@@ -15,6 +15,17 @@ constexpr long long kMostThreads = 1ll << 32;      // of a launch
 
 #define FD_TRY(expr) do { if ((expr) != hipSuccess) return FD_ERR_HIP; } while (0)
 
+// Device arrays of a call, to see whether two share a byte.
+struct Array {
+    const void *at;
+    long long bytes;
+};
+inline bool meet(const Array &a, const Array &b)
+{
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    return a.bytes > 0 && b.bytes > 0 && (x < y ? y - x < (uintptr_t)a.bytes : x - y < (uintptr_t)b.bytes);
+}
+
 // A pool's pages: a power of two of rows each, and slots that fit 31 bits.
 fd_status check_pages(int32_t n_pages, int32_t page_size, int *shift)
 {
@@ -147,9 +158,16 @@ fd_status fd_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int3
     if (max_tokens > (1 << 30) || batch > (1 << 30)) return FD_ERR_UNSUPPORTED;
     if (!cached_lens || !new_lens || !free_pages || !n_free || !block_table || !seq_lens || !token_starts || !slot_map || !n_left)
         return FD_ERR_NULL;
-    const void *all[] = {cached_lens, new_lens, free_pages, n_free, block_table, seq_lens, token_starts, slot_map, n_left};
-    for (const void *x : all)
-        if (off(x, 4)) return FD_ERR_SHAPE;
+    // Workgroups read the inputs and the table at any time while others write: an output that shares memory with another array would be read as such.
+    const long long one = sizeof(int32_t), b = batch * one;
+    const Array all[] = {{cached_lens, b}, {new_lens, b}, {free_pages, n_pages * one}, {n_free, one}, {block_table, b * pages_per_seq}, {seq_lens, b},
+                         {token_starts, b + one}, {slot_map, max_tokens * one}, {n_left, one}};
+    constexpr int kInputs = 4, kArrays = 9;
+    for (const Array &x : all)
+        if (off(x.at, 4)) return FD_ERR_SHAPE;
+    for (int i = kInputs; i < kArrays; ++i)
+        for (int j = 0; j < i; ++j)
+            if (meet(all[i], all[j])) return FD_ERR_SHAPE;
     p.cached = cached_lens; p.fresh = new_lens; p.free_pages = free_pages; p.n_free = n_free;
     p.table = block_table; p.seq_lens = seq_lens; p.starts = token_starts; p.slots = slot_map; p.n_left = n_left;
     p.batch = batch; p.n_pages = n_pages; p.width = pages_per_seq; p.max_tokens = max_tokens;
