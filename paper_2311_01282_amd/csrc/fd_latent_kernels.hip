@@ -67,7 +67,7 @@ __device__ __forceinline__ unsigned lds_address(const void *p)
 {
     return __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
 }
-template <int N> __device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void tile_barrier()
 {
     asm volatile("" ::: "memory");
@@ -87,9 +87,8 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     // 92 with the scaling in the exponents' multiply-adds and the sum of weights on the matrix cores)
     constexpr int NH = NW / DS, kDt = 32 / DS;                 // groups of 16 heads; tiles of 16 elements of a wavefront
     constexpr bool kTwoParts = NW < 8;                         // of a weight
-    constexpr int kKeys = TPW * kTile, kRows = kKeys / NW;     // keys of a step; rows that a wavefront fetches
-    constexpr int kHalves = (kRows + 15) / 16;                 // ... from so many places of 16 rows
-    constexpr int kLoads = kRows / 8 * 9;                      // fetches of a wavefront a step
+    constexpr int kKeys = TPW * kTile, kRows = 8;              // keys of a step; rows that a wavefront fetches, all of one page
+    static_assert(kKeys == NW * kRows && kSteps == 2);
     constexpr int kParts = DS == 4 ? 2 : 1, kBlocks = DS == 1 ? 2 : 1, kOperands = 18 / kParts;        // of the scores, of a wavefront
     __shared__ LatentLds<NW, DS, TPW> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
@@ -100,11 +99,9 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     const int chunk = unit % p.nc, b = unit / p.nc;
     const int start = chunk * p.C, shift = p.pool.page_shift, mask = (1 << shift) - 1;
     const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)b * p.width);
-    // page of the 16 rows h of this wavefront in step s (of the last entry, behind the table)
-    auto page_of = [&](int s, int h) { return table[min((start + s * kKeys + wave * kRows + 16 * h) >> shift, p.width - 1)]; };
-    int page[kHalves];
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h) page[h] = page_of(0, h);
+    // page of this wavefront's rows in step s (of the last entry, behind the table)
+    auto page_of = [&](int s) { return table[min((start + s * kKeys + wave * kRows) >> shift, p.width - 1)]; };
+    int page = page_of(0);
     const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
     const int end = min(len, start + p.C);
     const int heads = min(p.H - head0, 16);                    // of this wavefront; may be 0 or less: it only fetches
@@ -122,26 +119,18 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
         int l0 = lane;
         asm volatile("" : "+v"(l0));    // (offsets are formed anew each time: there are no registers to keep them in)
         const unsigned to_c = lds_c + s % kSteps * (kKeys * kCBytes) + wave * (kRows * kCBytes), to_r = lds_r + s % kSteps * (kKeys * kRBytes) + wave * (kRows * kRBytes);
+        const int key0 = start + s * kKeys + wave * kRows;
+        const int left = min(max(end - key0, 0), kRows);
+        const int pg = min(max(page, 0), p.pool.n_pages - 1);
+        const unsigned long long at = reinterpret_cast<unsigned long long>(p.pool.rows) + (((size_t)pg << shift) + (key0 & mask)) * kRowBytes;
+        const u32x4_t rs = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
+                            (unsigned)__builtin_amdgcn_readfirstlane(left * kRowBytes), 0x00027000u};
+        const int odd = wave & 1;                              // (bit 3 of the row, which is in the keys)
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-            const int key0 = start + s * kKeys + wave * kRows + 16 * h;
-            const int left = min(max(end - key0, 0), kRows < 16 ? kRows : 16);
-            const int pg = min(max(page[h], 0), p.pool.n_pages - 1);
-            const unsigned long long at = reinterpret_cast<unsigned long long>(p.pool.rows) + (((size_t)pg << shift) + (key0 & mask)) * kRowBytes;
-            const u32x4_t rs = {(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
-                                (unsigned)__builtin_amdgcn_readfirstlane(left * kRowBytes), 0x00027000u};
-#pragma unroll
-            for (int e = 0; e < (kRows < 16 ? 1 : 2); ++e) {                 // eight rows
-                const int odd = kRows < 16 ? wave & 1 : e;                   // (bit 3 of the row, which is in the keys)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    load_to_lds(rs, (l0 ^ c_key(i) ^ (odd << 3)) << 4, (8 * e + i) * kRowBytes, to_c + (16 * h + 8 * e + i) * kCBytes);
-                const int r = l0 >> 3;
-                load_to_lds(rs, r * kRowBytes + kCBytes + (((l0 & 7) ^ r_key(r) ^ (odd << 1)) << 4), 8 * e * kRowBytes, to_r + (16 * h + 8 * e) * kRBytes);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) page[h] = page_of(s + 1, h);
+        for (int i = 0; i < kRows; ++i) load_to_lds(rs, (l0 ^ c_key(i) ^ (odd << 3)) << 4, i * kRowBytes, to_c + i * kCBytes);
+        const int r = l0 >> 3;
+        load_to_lds(rs, r * kRowBytes + kCBytes + (((l0 & 7) ^ r_key(r) ^ (odd << 1)) << 4), 0, to_r);
+        page = page_of(s + 1);
     };
     fetch(0);
 
@@ -172,13 +161,11 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
     const unsigned v_at = v_row * kCBytes + (((n >> 1) & 1) << 4) + ((n & 1) << 3) + (c_key(v_row) << 4);
 
     __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries, and with them step 0 (the compiler, which does not count the fetches, would wait within the loop)
-#pragma unroll
-    for (int s = 1; s < kSteps - 1; ++s) fetch(s);
 
     for (int s = 0; s < steps; ++s) {
-        wait_fetches<(kSteps - 2) * kLoads>();                 // step s (those behind the last one are fetched too: nothing, that is, and the count is the same)
+        wait_fetches();                                        // step s
         tile_barrier();                                        // ... for every wavefront, all of which are through with step s - 1
-        fetch(s + kSteps - 1);
+        fetch(s + 1);                                          // (behind the last step: nothing)
         if (heads <= 0) continue;
         const unsigned tile_c = lds_c + s % kSteps * (kKeys * kCBytes), tile_r = lds_r + s % kSteps * (kKeys * kRBytes);
         f32x4_t sc[TPW][2];
@@ -290,7 +277,7 @@ template <class T, int NW, int DS, int TPW> __global__ __launch_bounds__(64 * NW
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    wait_fetches<0>();                                         // (nothing may land in LDS after the workgroup's end)
+    wait_fetches();                                            // (nothing may land in LDS after the workgroup's end)
     if (n >= heads) return;
     if constexpr (kTwoParts) {
         l += __shfl_xor(l, 16);
