@@ -486,7 +486,8 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     without a valid token are not followed, an entry in use that is out of range is the caller's error (it is
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
- *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128).
+ *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128), and there
+ *     also, batch * n_q_heads rounded up to a multiple of 8, < 2^24.
  *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
  *     its first 16 KiB, arrival counters that every completed call leaves at zero again; what lies behind them may hold anything.  After that
  *     shapes and calls may change from one use to the next.  A workspace serves one call at a time: calls that may overlap, captured

@@ -330,7 +330,9 @@ fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const voi
     const fd_status st = check_shape(shape, 128 + fd::kRope);
     if (st != FD_OK) return st;
     if (shape->n_kv_heads != shape->n_q_heads || shape->n_q_heads > 65535 || !known_type(dtype)) return FD_ERR_UNSUPPORTED;
-    if ((long long)shape->batch * shape->n_q_heads * (((long long)shape->max_seq + 127) / 128) > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
+    const long long pairs = (long long)shape->batch * shape->n_q_heads, tiles = ((long long)shape->max_seq + 127) / 128;
+    // (the launch has as many workgroups, of 256 threads, for each of the eight XCDs)
+    if (pairs * tiles > kMostThreads / 512 || (pairs + 7) / 8 * 8 * tiles >= kMostThreads / 256) return FD_ERR_UNSUPPORTED;
     if (!q || !kv || !rope || !seq_lens || !out) return FD_ERR_NULL;
     if (off(q, 16) || off(kv, 16) || off(rope, 16) || off(out, 16) || off(seq_lens, 4) || rope_stride < fd::kRope || rope_stride % 8 != 0 ||
         rope_stride > (1 << 24))
