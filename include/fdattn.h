@@ -547,7 +547,7 @@ typedef struct {
 fd_status fd_nibble_write(const fd_nibble_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
                        const int32_t *slot_map, void *stream);
 
-/* Rows out of the cache, l + s c rounded to dtype once.  Layouts and slots as fd_nibble_write; rows of padding are left as they are. */
+/* Rows out of the cache, l + s c in fp32 (s c is exact, the sum rounded) and from there rounded to dtype.  Layouts and slots as fd_nibble_write; rows of padding are left as they are. */
 fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, int32_t n_tokens, void *k, int64_t k_stride, void *v,
                       int64_t v_stride, void *stream);
 
