@@ -38,7 +38,8 @@ struct NibbleProblem {
     uint16_t *out;
     float *num;                                    // workspace: [B, Hq, nc, 128] sum e^{x-m} v
     float2 *ml;                                    // [B, Hq, nc] (m, l), m the reference of the weights times log2 e
-    int32_t *counters;                             // [B, Hkv, tiles] chunks that have arrived, zero between calls; null: the join is a launch of its own
+    // [B, Hkv, tiles] chunks that have arrived, zero between calls; null: the join is a launch of its own
+    int32_t *counters;
     int B, Hq, G, tiles, C, nc, Smax, width;       // tiles: of 16 query heads of a KV head
     float scale;
 };

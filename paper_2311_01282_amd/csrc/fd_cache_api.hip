@@ -70,8 +70,8 @@ fd_status nibble_rows(const fd_nibble_pool *pool, const void *k, int64_t k_strid
         v_stride % 8 != 0)
         return FD_ERR_SHAPE;
     if ((long long)n_tokens * 2 * P->Hkv >= kMostThreads / 16) return FD_ERR_UNSUPPORTED;
-    *R = fd::NibbleRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)), const_cast<uint16_t *>(static_cast<const uint16_t *>(v)),
-                     k_stride, v_stride, slot_map, n_tokens};
+    *R = fd::NibbleRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)),
+                        const_cast<uint16_t *>(static_cast<const uint16_t *>(v)), k_stride, v_stride, slot_map, n_tokens};
     return FD_OK;
 }
 
@@ -90,8 +90,8 @@ fd_status latent_pool(const fd_latent_pool *pool, fd::LatentPool *out)
     return FD_OK;
 }
 
-// A row is cut into chunks, one workgroup each, whose sums meet in the workspace.  It begins with arrival counters, a fixed number of them, so that
-// they stay where they are whatever the shape.
+// A row is cut into chunks, one workgroup each, whose sums meet in the workspace.  It begins with arrival counters, a fixed
+// number of them, so that they stay where they are whatever the shape.
 constexpr int kCounters = 4096;
 struct Split {
     long long rows, nc;
@@ -113,7 +113,8 @@ fd_status split(const fd_shape *sh, int head_dim, int dim, int unit, Split *S)
     if (sh->chunk % unit != 0 || sh->chunk > 16384) return FD_ERR_UNSUPPORTED;
     S->rows = (long long)sh->batch * sh->n_q_heads;
     S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
-    if (S->rows * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;     // (no more workgroups than these, of 512 threads at most)
+    // (no more workgroups than these, of 512 threads at most)
+    if (S->rows * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
     const size_t slots = (size_t)(S->rows * S->nc);
     S->num = align_up(kCounters * sizeof(int32_t));
     S->ml = align_up(S->num + (S->nc == 1 ? 0 : slots * dim * sizeof(float)));
@@ -130,7 +131,8 @@ fd_status latent_split(const fd_shape *sh, Split *S)
     return sh->n_kv_heads == 1 ? FD_OK : FD_ERR_UNSUPPORTED;
 }
 
-// Keys of a chunk, a multiple of `unit`, so that `units` rows of max_seq keys make about `want` workgroups of at least `least` keys.
+// Keys of a chunk, a multiple of `unit`, so that `units` rows of max_seq keys make about `want` workgroups of at least
+// `least` keys.
 int32_t chunk_for(int32_t max_seq, long long units, long long want, int32_t least, int32_t unit)
 {
     long long nc = units > 0 ? want / units : 1;
@@ -158,10 +160,12 @@ fd_status fd_page_tables(int32_t batch, int32_t page_size, int32_t n_pages, int3
     if (max_tokens > (1 << 30) || batch > (1 << 30)) return FD_ERR_UNSUPPORTED;
     if (!cached_lens || !new_lens || !free_pages || !n_free || !block_table || !seq_lens || !token_starts || !slot_map || !n_left)
         return FD_ERR_NULL;
-    // Workgroups read the inputs and the table at any time while others write: an output that shares memory with another array would be read as such.
+    // Workgroups read the inputs and the table at any time while others write: an output that shares memory with another
+    // array would be read as such.
     const long long one = sizeof(int32_t), b = batch * one;
-    const Array all[] = {{cached_lens, b}, {new_lens, b}, {free_pages, n_pages * one}, {n_free, one}, {block_table, b * pages_per_seq}, {seq_lens, b},
-                         {token_starts, b + one}, {slot_map, max_tokens * one}, {n_left, one}};
+    const Array all[] = {{cached_lens, b}, {new_lens, b}, {free_pages, n_pages * one}, {n_free, one},
+                         {block_table, b * pages_per_seq}, {seq_lens, b}, {token_starts, b + one}, {slot_map, max_tokens * one},
+                         {n_left, one}};
     constexpr int kInputs = 4, kArrays = 9;
     for (const Array &x : all)
         if (off(x.at, 4)) return FD_ERR_SHAPE;
@@ -216,10 +220,13 @@ int32_t fd_nibble_pick_chunk(const fd_shape *shape)
 {
     if (check_shape(shape, fd::kHeadDim) != FD_OK) return 0;
     const long long units = (long long)shape->batch * shape->n_kv_heads * ((shape->n_q_heads / shape->n_kv_heads + 15) / 16);
-    // Two workgroups fit a compute unit, and a launch of one round of them is the fastest there is, ragged or not: a workgroup's beginning and end cost as much as
-    // three blocks of its four wavefronts.  Up to there 1024 keys are the best length where they fill the chip once, otherwise what does, down to a block a wavefront.
-    // (Whole call, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 16 x 32 heads x 2000 44 / 37.7 / 33.7 / *30.2, 64 x 32/8 x 4000 95 / 72 / 64 / 60 / *56.4, 32 x 32/8
-    // x 2000 33.5 / 27.4 / *22.9 / 23.3, 1 x 32 x 8192 21.7 / 16.7 / *15.9 / 21.8 / 35.6, 8 x 32/8 x 4000 17.8 / 14.4 / *14.0 / 18.2 / 26.7, 4 x 64/8 x 2000 *11.3 / 12.9 / 17.0.)
+    // Two workgroups fit a compute unit, and a launch of one round of them is the fastest there is, ragged or not: a
+    // workgroup's beginning and end cost as much as three blocks of its four wavefronts.  Up to there 1024 keys are the
+    // best length where they fill the chip once, otherwise what does, down to a block a wavefront.
+    // (Whole call, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 16 x 32 heads x 2000 44 / 37.7 / 33.7
+    // / *30.2, 64 x 32/8 x 4000 95 / 72 / 64 / 60 / *56.4, 32 x 32/8 x 2000 33.5 / 27.4 / *22.9 / 23.3, 1 x 32 x 8192 21.7
+    // / 16.7 / *15.9 / 21.8 / 35.6, 8 x 32/8 x 4000 17.8 / 14.4 / *14.0 / 18.2 / 26.7, 4 x 64/8 x 2000 *11.3 / 12.9 /
+    // 17.0.)
     const long long chip = fd::kComputeUnits, rows = units > 0 ? units : 1;
     for (int32_t c : {1024, 512, 256}) {
         const long long w = rows * (((long long)shape->max_seq + c - 1) / c);
@@ -268,8 +275,8 @@ fd_status fd_latent_write(const fd_latent_pool *pool, const void *latent, int64_
         return FD_ERR_SHAPE;
     if (n_tokens > (1 << 25)) return FD_ERR_UNSUPPORTED;                    // (72 threads each)
     if (n_tokens == 0) return FD_OK;
-    FD_TRY(fd::launch_latent_write(P, static_cast<const uint16_t *>(latent), latent_stride, static_cast<const uint16_t *>(rope), rope_stride,
-                                   n_tokens, slot_map, static_cast<hipStream_t>(stream)));
+    FD_TRY(fd::launch_latent_write(P, static_cast<const uint16_t *>(latent), latent_stride, static_cast<const uint16_t *>(rope),
+                                   rope_stride, n_tokens, slot_map, static_cast<hipStream_t>(stream)));
     return FD_OK;
 }
 
@@ -282,11 +289,13 @@ size_t fd_latent_workspace_bytes(const fd_shape *shape)
 int32_t fd_latent_pick_chunk(const fd_shape *shape)
 {
     if (check_shape(shape, fd::kLatentRow) != FD_OK || shape->n_kv_heads != 1) return 0;
-    // A chunk of c keys takes c / 32 tiles of about 1 us (1.4 of 64 heads, 1.5 of 128), and every workgroup leaves 2 KiB of sums a head, written and read again: about
-    // 0.07 us for 128 heads.  The sum of the two is least near sqrt(k units max_seq) keys; a row of many pieces takes its join 0.07 us for each, which
-    // adds sqrt(2.2 max_seq); and more than one workgroup a compute unit gains nothing.  A row that would be cut into little goes in one piece, without the join's launch.
-    // (Whole call, chunks of 64 / 128 / 256 / 512 / 1024 keys: 8 x 128 heads x 4000 77 / 46 / 41.7 / 51 / 73 us, 1 x 16 x 30000 50 / 33 / 27.4 / 31 / 45, 64 x 64 x 4000 - / - / 124 / 99 / 89,
-    // 128 x 16 x 300 29 / 26 / 25.5 / 19.5.)
+    // A chunk of c keys takes c / 32 tiles of about 1 us (1.4 of 64 heads, 1.5 of 128), and every workgroup leaves 2 KiB of
+    // sums a head, written and read again: about 0.07 us for 128 heads.  The sum of the two is least near sqrt(k units
+    // max_seq) keys; a row of many pieces takes its join 0.07 us for each, which adds sqrt(2.2 max_seq); and more than one
+    // workgroup a compute unit gains nothing.  A row that would be cut into little goes in one piece, without the join's
+    // launch.
+    // (Whole call, chunks of 64 / 128 / 256 / 512 / 1024 keys: 8 x 128 heads x 4000 77 / 46 / 41.7 / 51 / 73 us, 1 x 16 x
+    // 30000 50 / 33 / 27.4 / 31 / 45, 64 x 64 x 4000 - / - / 124 / 99 / 89, 128 x 16 x 300 29 / 26 / 25.5 / 19.5.)
     const double units = (double)shape->batch * ((shape->n_q_heads + 127) / 128), S = shape->max_seq;
     const double k = shape->n_q_heads > 64 ? 1.5 : shape->n_q_heads / 76.0;
     const double c = std::fmax(std::fmax(units * S / fd::kComputeUnits, std::sqrt(k * units * S)), std::sqrt(2.2 * S));
@@ -334,9 +343,8 @@ fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const voi
     // (the launch has as many workgroups, of 256 threads, for each of the eight XCDs)
     if (pairs * tiles > kMostThreads / 512 || (pairs + 7) / 8 * 8 * tiles >= kMostThreads / 256) return FD_ERR_UNSUPPORTED;
     if (!q || !kv || !rope || !seq_lens || !out) return FD_ERR_NULL;
-    if (off(q, 16) || off(kv, 16) || off(rope, 16) || off(out, 16) || off(seq_lens, 4) || rope_stride < fd::kRope || rope_stride % 8 != 0 ||
-        rope_stride > (1 << 24))
-        return FD_ERR_SHAPE;
+    if (off(q, 16) || off(kv, 16) || off(rope, 16) || off(out, 16) || off(seq_lens, 4)) return FD_ERR_SHAPE;
+    if (rope_stride < fd::kRope || rope_stride % 8 != 0 || rope_stride > (1 << 24)) return FD_ERR_SHAPE;
     if (shape->batch == 0) return FD_OK;
     fd::LatentPromptProblem p{};
     p.q = static_cast<const uint16_t *>(q);

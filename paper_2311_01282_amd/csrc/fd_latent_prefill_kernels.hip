@@ -1,16 +1,18 @@
-// Prompts with latent attention in the expanded form: every head has keys of 128 elements and 64 rotary ones that all heads share, values of 128, and token
-// i attends to tokens 0 .. i.  Operands lie token by token, as projections leave them.
+// Prompts with latent attention in the expanded form: every head has keys of 128 elements and 64 rotary ones that all heads
+// share, values of 128, and token i attends to tokens 0 .. i.  Operands lie token by token, as projections leave them.
 //
-// Mapping as in the prompt kernel of the equal-sized heads (16 x 16 x 32; lane = (n, g) = (lane % 16, lane / 16)): a workgroup owns 128 queries of a head, a
-// wavefront 32 of them in two blocks of 16;
-//   scores   S^T[key][query] = K . Q^T: A = 16 keys of the tile in LDS, B = Q^T in registers.  Row 4 g + r of key block t is key 8 g + 4 t + r of the 32 of a step, so
-//            that lane (n, g) holds keys 8 g .. 8 g + 7 of query n: the B operand of
+// Mapping as in the prompt kernel of the equal-sized heads (16 x 16 x 32; lane = (n, g) = (lane % 16, lane / 16)): a
+// workgroup owns 128 queries of a head, a wavefront 32 of them in two blocks of 16;
+//   scores   S^T[key][query] = K . Q^T: A = 16 keys of the tile in LDS, B = Q^T in registers.  Row 4 g + r of key block t
+//            is key 8 g + 4 t + r of the 32 of a step, so that lane (n, g) holds keys 8 g .. 8 g + 7 of query n: the B
+//            operand of
 //   output   O^T[d][query] = V^T . P^T: A = V^T by the transposing LDS read.
-// Where a launch has few workgroups, a workgroup is two such halves that take every other step and join their sums at the end (kHalves).
-// Softmax with a running maximum per query; the weights are of the type (one rounding, as large as the output's own), their sum is that of the
-// rounded ones, in fp32.
-// The matrix cores bound long prompts, at the clock that power leaves them: 64 heads x 4001 tokens 353 .. 385 us, 0.85 .. 0.93 PFLOP/s of what the mask leaves, matrix instructions in 53 %
-// of the cycles; short ones the length of a tile's walk.
+// Where a launch has few workgroups, a workgroup is two such halves that take every other step and join their sums at the
+// end (kHalves).
+// Softmax with a running maximum per query; the weights are of the type (one rounding, as large as the output's own), their
+// sum is that of the rounded ones, in fp32.
+// The matrix cores bound long prompts, at the clock that power leaves them: 64 heads x 4001 tokens 353 .. 385 us, 0.85 ..
+// 0.93 PFLOP/s of what the mask leaves, matrix instructions in 53 % of the cycles; short ones the length of a tile's walk.
 #include <utility>
 
 #include "fd_chunk.h"
@@ -22,8 +24,9 @@ namespace fd {
 namespace {
 
 constexpr int kNope = 128, kQueryDim = kNope + kRope, kStep = 32, kTileQ = 128, kRingK = 4, kRingV = 3;
-// The reference of a query's weights follows its maximum only where that has grown by more than this (in units of log2): weights are then at
-// most 2^8 times the reference's, and the sums are brought to another reference a few times a row instead of at every new maximum.
+// The reference of a query's weights follows its maximum only where that has grown by more than this (in units of log2):
+// weights are then at most 2^8 times the reference's, and the sums are brought to another reference a few times a row
+// instead of at every new maximum.
 constexpr float kSlack = 8.f;
 
 struct PromptLds {
@@ -31,15 +34,16 @@ struct PromptLds {
     alignas(256) unsigned char r[kRingK][kStep * kRope * 2];    // ... x ^ r_place(r)
     alignas(256) unsigned char v[kRingV][kStep * kNope * 2];    // 32-byte unit x of row r in place x ^ v_unit(r)
 };
-// With these the 16-byte operand reads, whose cycles hold every n once from two neighbouring g, and the transposing reads, which take 32 bytes of
-// rows 8 g + 4 h + (0 .. 3) of two neighbouring g at a time, have no bank conflicts.
+// With these the 16-byte operand reads, whose cycles hold every n once from two neighbouring g, and the transposing reads,
+// which take 32 bytes of rows 8 g + 4 h + (0 .. 3) of two neighbouring g at a time, have no bank conflicts.
 __device__ __forceinline__ int k_place(int r) { return (r & 3) | (((r >> 3) & 3) << 2); }
 __device__ __forceinline__ int r_place(int r) { return 2 * ((r >> 3) & 1) + 4 * ((r >> 1) & 1); }
 __device__ __forceinline__ int v_unit(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
 
 __device__ __forceinline__ unsigned lds_address(const void *p)
 {
-    return __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
+    return __builtin_amdgcn_readfirstlane(
+        (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
 }
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
@@ -49,7 +53,10 @@ __device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, int soff, unsi
 {
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs), "s"(soff) : "memory");
 }
-template <class F, int... I> __device__ __forceinline__ void slots(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
+template <class F, int... I> __device__ __forceinline__ void slots(std::integer_sequence<int, I...>, F f)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
 template <int N> __device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void tile_barrier()
 {
@@ -61,11 +68,13 @@ __device__ __forceinline__ void tile_barrier()
 __device__ __forceinline__ u32x4_t window(const void *base, long long bytes)
 {
     const unsigned long long at = reinterpret_cast<unsigned long long>(base);
-    return u32x4_t{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
+    return u32x4_t{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at),
+                   (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
 }
 
-// Values that are not finite: counted in a product of their own, in which an infinite one is 1, one of the other sign 64 and a NaN 4096 (of 32 keys the counts do not meet).
+// Values that are not finite: counted in a product of their own, in which an infinite one is 1, one of the other sign 64
+// and a NaN 4096 (of 32 keys the counts do not meet).
 template <class T> __device__ __forceinline__ u32x4_t not_finite(u32x4_t v)
 {
     u32x4_t x;
@@ -86,7 +95,8 @@ template <class T> __device__ __forceinline__ u32x4_t finite(u32x4_t v)         
     u32x4_t x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned low = (v[i] & 0x7fffu) < T::kInfinity ? v[i] & 0xffffu : 0u, high = (v[i] >> 16 & 0x7fffu) < T::kInfinity ? v[i] & 0xffff0000u : 0u;
+        const unsigned low = (v[i] & 0x7fffu) < T::kInfinity ? v[i] & 0xffffu : 0u;
+        const unsigned high = (v[i] >> 16 & 0x7fffu) < T::kInfinity ? v[i] & 0xffff0000u : 0u;
         x[i] = low | high;
     }
     return x;
@@ -104,8 +114,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, n = lane & 15, g = lane >> 4;
     const int half = kHalves == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 8);      // takes the steps half, half + kHalves, ...
     PromptLds &lds = both.ring[half];
-    // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads, all tiles of a head on one: its keys and values are read into one L2 only.  (Heads
-    // dealt out to the XCDs in turn measured the same.)
+    // The longest walks first.  An XCD (index modulo 8) takes neighbouring heads, all tiles of a head on one: its keys and
+    // values are read into one L2 only.  (Heads dealt out to the XCDs in turn measured the same.)
     const int pairs = p.B * p.H, per = (pairs + 7) / 8, tiles = (p.Smax + kTileQ - 1) / kTileQ;
     const int at = blockIdx.x % (8 * per), pair = at % 8 * per + at / 8, i0 = (tiles - 1 - blockIdx.x / (8 * per)) * kTileQ;
     if (pair >= pairs) return;
@@ -119,7 +129,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             *reinterpret_cast<u32x4_t *>(out + i * out_stride + 8 * (tid & 15)) = u32x4_t{0u, 0u, 0u, 0u};
         return;
     }
-    // this half's steps, of the workgroup (the first half has as many or one more) and of the wavefront, whose last step of all is the one with masks
+    // this half's steps, of the workgroup (the first half has as many or one more) and of the wavefront, whose last step of
+    // all is the one with masks
     const int steps = ((min(i0 + kTileQ, S) - 1) / kStep + kHalves) / kHalves;
     const int all = w0 < S ? (min(w0 + 32, S) - 1) / kStep + 1 : 0, mine = (all - half + kHalves - 1) / kHalves;
 
@@ -132,13 +143,15 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
 #pragma unroll
         for (int kb = 0; kb < 6; ++kb) {
             q[qb][kb] = u32x4_t{0u, 0u, 0u, 0u};
-            if (row < S) q[qb][kb] = *reinterpret_cast<const u32x4_t *>(p.q + (((size_t)b * p.Smax + row) * p.H + h) * kQueryDim + 32 * kb + 8 * g);
+            const uint16_t *from = p.q + (((size_t)b * p.Smax + row) * p.H + h) * kQueryDim + 32 * kb + 8 * g;
+            if (row < S) q[qb][kb] = *reinterpret_cast<const u32x4_t *>(from);
             q[qb][kb] ^= p.scale < 0.f ? 0x80008000u : 0u;     // (the largest product is then the largest logit)
         }
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries have arrived: what is counted from here on are fetches
 
-    // A wavefront's five of the 20 KiB of a step: rows 8 wave .. + 7 of the keys and of the values, four rows an instruction, of the rotary parts all eight.
+    // A wavefront's five of the 20 KiB of a step: rows 8 wave .. + 7 of the keys and of the values, four rows an
+    // instruction, of the rotary parts all eight.
     // (The places of rows r and r + 4 are the same: the second instruction is the first, four rows on.)
     const int row_bytes = p.H * (2 * kNope * 2), rope_bytes = (int)(p.rope_stride * 2);
     int koff, voff, roff;
@@ -148,13 +161,17 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         voff = r * row_bytes + ((x ^ (v_unit(r) << 1)) << 4);
         roff = rr * rope_bytes + (((lane & 7) ^ r_place(rr)) << 4);
     }
-    // The fetches walk along the rows: a place in memory, the rows left from there, a place in the ring.  Rows without keys arrive as zeros.
+    // The fetches walk along the rows: a place in memory, the rows left from there, a place in the ring.  Rows without keys
+    // arrive as zeros.
     struct Walk { const unsigned char *from; int left; unsigned to; };
     const unsigned char *kv = reinterpret_cast<const unsigned char *>(p.kv) + ((size_t)b * p.Smax * p.H + h) * (2 * kNope * 2);
     const int skip = half * kStep;
     Walk wk = {kv + (size_t)skip * row_bytes, S - skip, 0u}, wv = {kv + (size_t)skip * row_bytes + kNope * 2, S - skip, 0u};
     const unsigned char *rope_from = reinterpret_cast<const unsigned char *>(p.rope) + ((size_t)b * p.Smax + skip) * rope_bytes;
-    auto bytes_of = [&](int left, int stride, int row) { const int rows = min(left, kStep); return rows > 0 ? (rows - 1) * stride + row : 0; };
+    auto bytes_of = [&](int left, int stride, int row) {
+        const int rows = min(left, kStep);
+        return rows > 0 ? (rows - 1) * stride + row : 0;
+    };
     auto fetch_k = [&] {
         const u32x4_t rk = window(wk.from, bytes_of(wk.left, row_bytes, kNope * 2));
 #pragma unroll
@@ -176,7 +193,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         wv.left -= kHalves * kStep;
         wv.to = wv.to == kRingV - 1 ? 0 : wv.to + 1;
     };
-    // Entering step s, K of s + 2 and V of s have landed; the step fetches K of s + 4 and V of s + 2, whose places were last read in step s - 1 or before.
+    // Entering step s, K of s + 2 and V of s have landed; the step fetches K of s + 4 and V of s + 2, whose places were
+    // last read in step s - 1 or before.
     for (int i = 0; i < kRingK; ++i) {
         fetch_k();
         fetch_r();
@@ -184,7 +202,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     }
 
     f32x4_t acc[8][2], sum[2];                                 // sum: of the rounded weights, in every element (V^T of ones)
-    float ref[2] = {0.f, 0.f};                                 // of the weights, in units of log2: T::kLift below the logit it was taken from
+    // of the weights, in units of log2: T::kLift below the logit it was taken from
+    float ref[2] = {0.f, 0.f};
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         sum[qb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -193,8 +212,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     }
     const unsigned one2 = T::pack(1.f, 1.f);
     const float c1 = fabsf(p.scale) * kLog2e;
-    // This lane's operand reads: piece 4 kb + g of row k_row (+ 4 t: the same places), 32 bytes from element 16 dt of row v_row.  Those of a row differ by an exclusive or
-    // with a constant.
+    // This lane's operand reads: piece 4 kb + g of row k_row (+ 4 t: the same places), 32 bytes from element 16 dt of row
+    // v_row.  Those of a row differ by an exclusive or with a constant.
     const int k_row = 8 * (n >> 2) + (n & 3), v_row = 8 * g + (n >> 2);
     const unsigned k_at = k_row * (kNope * 2) + ((g ^ k_place(k_row)) << 4), r_at = k_row * (kRope * 2) + ((g ^ r_place(k_row)) << 4);
     const unsigned v_at = v_row * (kNope * 2) + (v_unit(v_row) << 5) + ((n & 3) << 3);
@@ -212,16 +231,18 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
     };
     const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 
-    // Step s from its scores sc[key block][query block], and the scores of step s + 1, which do not depend on it, in their place.  Vector instructions of one wavefront do not
-    // run under the matrix instructions of the other of its SIMD, but within a wavefront two or three independent ones do under each: so the two are woven by
-    // hand, a matrix instruction and what runs under it to a slot.  24 slots of scores hide the logits, their maxima and the first query block's exponentials, 18 of
-    // V^T P^T the second's.
+    // Step s from its scores sc[key block][query block], and the scores of step s + 1, which do not depend on it, in their
+    // place.  Vector instructions of one wavefront do not run under the matrix instructions of the other of its SIMD, but
+    // within a wavefront two or three independent ones do under each: so the two are woven by hand, a matrix instruction
+    // and what runs under it to a slot.  24 slots of scores hide the logits, their maxima and the first query block's
+    // exponentials, 18 of V^T P^T the second's.
     unsigned k_next = 1, v_now = 0;
     u32x4_t first[4];
     auto step = [&](auto last_step, int s, f32x4_t (&sc)[2][2]) {
         constexpr bool kLast = decltype(last_step)::value;
         // places of K of s + 1 (whose first four operands are there already), of K of s + 2, of V of s
-        unsigned kk = lds_k + k_next * (kStep * kNope * 2) + k_at, rr = lds_r + k_next * (kStep * kRope * 2) + r_at, vv = lds_v + v_now * (kStep * kNope * 2) + v_at;
+        unsigned kk = lds_k + k_next * (kStep * kNope * 2) + k_at, rr = lds_r + k_next * (kStep * kRope * 2) + r_at;
+        unsigned vv = lds_v + v_now * (kStep * kNope * 2) + v_at;
         k_next = k_next == kRingK - 1 ? 0 : k_next + 1;
         v_now = v_now == kRingV - 1 ? 0 : v_now + 1;
         unsigned k2 = lds_k + k_next * (kStep * kNope * 2) + k_at;
@@ -269,7 +290,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             if constexpr (mm == 11) top[1] = columns_max(top[1]);
             __builtin_amdgcn_sched_barrier(0);
         });
-        // Relative to the reference, which a query whose logits have all been -inf does not have yet: none of its weights is above 0, and any number becomes it.
+        // Relative to the reference, which a query whose logits have all been -inf does not have yet: none of its weights
+        // is above 0, and any number becomes it.
         const bool none[2] = {sum[0][0] == 0.f, sum[1][0] == 0.f};
         constexpr float kMost = kSlack + T::kLift;
         if (__any((top[0] > (none[0] ? -INFINITY : kMost)) | (top[1] > (none[1] ? -INFINITY : kMost)))) {
@@ -301,8 +323,9 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        // In the step with masks the weights of keys behind a query are 0, and 0 times an infinite value or a NaN is NaN: such values leave the product, and the queries that see
-        // them get them as a summand.  (Whether there are any: a product with 0.  In the steps before all keys are seen.)
+        // In the step with masks the weights of keys behind a query are 0, and 0 times an infinite value or a NaN is NaN:
+        // such values leave the product, and the queries that see them get them as a summand.  (Whether there are any: a
+        // product with 0.  In the steps before all keys are seen.)
         if constexpr (kLast) {
             const u32x4_t none_of = {0u, 0u, 0u, 0u};
             f32x4_t any[2] = {zero, zero};
@@ -314,7 +337,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
 #pragma unroll
                 for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) seen[qb][j >> 1] = T::pack(j - 16 * qb <= own ? 1.f : 0.f, j + 1 - 16 * qb <= own ? 1.f : 0.f);
+                    for (int j = 0; j < 8; j += 2)
+                        seen[qb][j >> 1] = T::pack(j - 16 * qb <= own ? 1.f : 0.f, j + 1 - 16 * qb <= own ? 1.f : 0.f);
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
                     const u32x4_t counted = not_finite<T>(av[dt]);
@@ -407,7 +431,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) {
                 const f32x4_t x = both.sums[wave][16 + qb][lane];
-                const float own = reference(qb), top = fmaxf(own, x[1]), f0 = __builtin_amdgcn_exp2f(own - top), f1 = __builtin_amdgcn_exp2f(x[1] - top);
+                const float own = reference(qb), top = fmaxf(own, x[1]);
+                const float f0 = __builtin_amdgcn_exp2f(own - top), f1 = __builtin_amdgcn_exp2f(x[1] - top);
                 sum[qb][0] = sum[qb][0] * f0 + x[0] * f1;
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
@@ -435,14 +460,21 @@ template <class T> hipError_t prefill(const LatentPromptProblem &p, hipStream_t 
 {
     const long long workgroups = ((long long)p.B * p.H + 7) / 8 * 8 * ((p.Smax + kTileQ - 1) / kTileQ);
     const dim3 grid((unsigned)workgroups);
-    // A wavefront alone on its SIMD takes 0.75 us a step, two 1.05 together: launches that leave the second place empty give it to a second half of the workgroup, unless they are
-    // so short that joining the halves costs as much (with halves / without, us: 1 x 16 heads x 2000 tokens 42.6 / 54.0, 1 x 8 x 4000 75.2 / 100.0, 1 x 32 x 500 18.3 / 19.6, 3 x 16 x
-    // 150 .. 1000 31.3 / 32.9, 4 x 16 x 200 .. 400 17.0 / 17.2, 1 x 16 x 128 11.2 / 10.0, 32 x 16 x 100 22.5 / 16.3, 1 x 64 x 2000 117 / 107).
-    return workgroups <= kComputeUnits * 3 / 2 && p.Smax > 2 * kTileQ ? launch(latent_prefill_kernel<T, 2>, grid, dim3(512), s, p) : launch(latent_prefill_kernel<T, 1>, grid, dim3(256), s, p);
+    // A wavefront alone on its SIMD takes 0.75 us a step, two 1.05 together: launches that leave the second place empty
+    // give it to a second half of the workgroup, unless they are so short that joining the halves costs as much (with
+    // halves / without, us: 1 x 16 heads x 2000 tokens 42.6 / 54.0, 1 x 8 x 4000 75.2 / 100.0, 1 x 32 x 500 18.3 / 19.6, 3
+    // x 16 x 150 .. 1000 31.3 / 32.9, 4 x 16 x 200 .. 400 17.0 / 17.2, 1 x 16 x 128 11.2 / 10.0, 32 x 16 x 100 22.5 / 16.3,
+    // 1 x 64 x 2000 117 / 107).
+    if (workgroups <= kComputeUnits * 3 / 2 && p.Smax > 2 * kTileQ)
+        return launch(latent_prefill_kernel<T, 2>, grid, dim3(512), s, p);
+    return launch(latent_prefill_kernel<T, 1>, grid, dim3(256), s, p);
 }
 
 }  // namespace
 
-hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s) { return p.dtype == kF16 ? prefill<F16>(p, s) : prefill<BF16>(p, s); }
+hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s)
+{
+    return p.dtype == kF16 ? prefill<F16>(p, s) : prefill<BF16>(p, s);
+}
 
 }  // namespace fd

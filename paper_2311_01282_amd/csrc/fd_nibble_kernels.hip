@@ -1,10 +1,10 @@
 // The 4-bit cache: rows into it, rows out of it, and the decode attention over it.
 //
-// A group of 32, 64 or 128 neighbouring elements of a row (128 elements of a token and KV head) shares a scale s and a lowest value l
-// of the cache's type; an element is l + s c, c = 0 .. 15.  Codes: 64 bytes a row, lower half of a byte first, V in order, K with its
-// 16 words of eight elements transposed as a 4 x 4 matrix (elements 32 t + 8 c .. + 7 in word 4 c + t): a lane of the matrix
-// instruction that multiplies K then finds its 16 bytes, one word for each of the four steps over a row, side by side, and a step
-// covers one group of 32.  Scales: all s of a row, then all l.
+// A group of 32, 64 or 128 neighbouring elements of a row (128 elements of a token and KV head) shares a scale s and a
+// lowest value l of the cache's type; an element is l + s c, c = 0 .. 15.  Codes: 64 bytes a row, lower half of a byte
+// first, V in order, K with its 16 words of eight elements transposed as a 4 x 4 matrix (elements 32 t + 8 c .. + 7 in word
+// 4 c + t): a lane of the matrix instruction that multiplies K then finds its 16 bytes, one word for each of the four steps
+// over a row, side by side, and a step covers one group of 32.  Scales: all s of a row, then all l.
 #include "fd_chunk.h"
 #include "fd_cache.h"
 #include "fd_types.h"
@@ -14,9 +14,11 @@ namespace fd {
 namespace {
 
 // ---- rows in and out ----
-// A row is read, coded and written within eight lanes, 16 elements to a lane; with eight elements to a lane the places and the two divisions of a group cost as much as the codes
-// (16001 tokens x 8 heads, fp16: 26.8 us so, 18.6 with 16).  The arithmetic is in fp32: the differences and the division are rounded once each.  What bounds the coding is its
-// vector instructions, some 16 an element with all else, next to memory (91 MB).  Reading back is bound by memory (84 MB): the rows leave past the caches (18.8 us without, 17.5 so).
+// A row is read, coded and written within eight lanes, 16 elements to a lane; with eight elements to a lane the places and
+// the two divisions of a group cost as much as the codes (16001 tokens x 8 heads, fp16: 26.8 us so, 18.6 with 16).  The
+// arithmetic is in fp32: the differences and the division are rounded once each.  What bounds the coding is its vector
+// instructions, some 16 an element with all else, next to memory (91 MB).  Reading back is bound by memory (84 MB): the
+// rows leave past the caches (18.8 us without, 17.5 so).
 
 template <class F> __device__ __forceinline__ float group_reduce(float x, int lanes, F f)
 {
@@ -54,7 +56,8 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
     const int j = threadIdx.x & 7;                                          // 16 elements from 16 j: words 2 j and 2 j + 1
     const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, row);
     if (!at.live) return;                                                   // (whole rows of 8 lanes)
-    const u32x4_t *src = reinterpret_cast<const u32x4_t *>((at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim + 16 * j);
+    const uint16_t *token = at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride;
+    const u32x4_t *src = reinterpret_cast<const u32x4_t *>(token + at.head * kHeadDim + 16 * j);
     const u32x4_t x[2] = {src[0], src[1]};
     float f[16];
 #pragma unroll
@@ -72,10 +75,11 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
     const int lanes = 8 / pool.NG;
     lo = group_reduce(lo, lanes, [](float a, float b) { return __builtin_elementwise_minimum(a, b); });
     hi = group_reduce(hi, lanes, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
-    // The scale as it is stored is the one that the codes are taken against.  Quotients are those of fp32 division: with r = 1 / s rounded, q = t r and one correction, q +
-    // r (t - q s), give the correctly rounded t / s (Markstein) where nothing leaves the range of normal numbers; where it might, divisions do.  (With a division for
-    // each element the call was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)  A scale that is a normal number is off by 2^-8 of itself at
-    // most, so that no quotient passes 15.5 and has to be limited.
+    // The scale as it is stored is the one that the codes are taken against.  Quotients are those of fp32 division: with r
+    // = 1 / s rounded, q = t r and one correction, q + r (t - q s), give the correctly rounded t / s (Markstein) where
+    // nothing leaves the range of normal numbers; where it might, divisions do.  (With a division for each element the call
+    // was bounded by them: 16001 tokens x 8 heads 35 us, 26.8 so, eight elements to a lane.)  A scale that is a normal
+    // number is off by 2^-8 of itself at most, so that no quotient passes 15.5 and has to be limited.
     const float span = hi - lo;
     const bool ordinary = (span >= 15.5f * T::kSmallest && span < 0x1p100f) || span == 0.f;
     constexpr float kFifteenth = 1.f / 15.f;
@@ -117,22 +121,26 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
 template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(NibblePool pool, NibbleRows rows)
 {
     const unsigned row = blockIdx.x * 32 + (threadIdx.x >> 3);
-    const int j = threadIdx.x & 7;                                          // elements from 8 j and from 64 + 8 j: stores of eight lanes lie side by side
+    // elements from 8 j and from 64 + 8 j: stores of eight lanes lie side by side
+    const int j = threadIdx.x & 7;
     const RowPlace at = row_place(pool, rows.slots, rows.n_tokens, row);
     if (!at.live) return;
     const unsigned *codes = reinterpret_cast<const unsigned *>((at.is_v ? pool.v_codes : pool.k_codes) + at.row * 64);
     const int place = at.is_v ? j : 4 * (j & 3) + (j >> 2), apart = at.is_v ? 8 : 2;
     const unsigned word[2] = {codes[place], codes[place + apart]};
     const uint16_t *scales = (at.is_v ? pool.v_scales : pool.k_scales) + at.row * (2 * pool.NG);
-    u32x4_t *dst = reinterpret_cast<u32x4_t *>((at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride) + at.head * kHeadDim) + j;
+    uint16_t *token = at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride;
+    u32x4_t *dst = reinterpret_cast<u32x4_t *>(token + at.head * kHeadDim) + j;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         const int g = (j + 8 * w) * pool.NG >> 4;
         const float s = T::lo(scales[g]), l = T::lo(scales[pool.NG + g]);
-        const unsigned even = word[w] & 0x0f0f0f0fu, odd = (word[w] >> 4) & 0x0f0f0f0fu;       // bytes, of which a conversion takes any
+        // bytes, of which a conversion takes any
+        const unsigned even = word[w] & 0x0f0f0f0fu, odd = (word[w] >> 4) & 0x0f0f0f0fu;
         u32x4_t x;
+        // s c is exact in fp32: one rounding there, one to the type
 #pragma unroll
-        for (int i = 0; i < 4; ++i)                                         // s c is exact in fp32: one rounding there, one to the type
+        for (int i = 0; i < 4; ++i)
             x[i] = T::pack(__builtin_fmaf(s, (float)((even >> (8 * i)) & 255), l), __builtin_fmaf(s, (float)((odd >> (8 * i)) & 255), l));
         __builtin_nontemporal_store(x, dst + 8 * w);
     }
@@ -140,38 +148,52 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 
 // ---- attention ----
 //
-// One query token a sequence over the coded rows, synchronized softmax with a running maximum.  The codes go to the matrix cores as the
-// numbers 16 + c, exact in both types, without touching the scales: of an element l + s c the product with a query is
+// One query token a sequence over the coded rows, synchronized softmax with a running maximum.  The codes go to the matrix
+// cores as the numbers 16 + c, exact in both types, without touching the scales: of an element l + s c the product with a
+// query is
 //     sum_d q_d (l_g + s_g c_d) = sum_g s_g (sum_{d in g} q_d c_d) + l_g (sum_{d in g} q_d),
-// four matrix instructions a row, one a group of 32, and a multiply-add with s and one with l a group; the 16 is taken off in the term with l.  Of the output
+// four matrix instructions a row, one a group of 32, and a multiply-add with s and one with l a group; the 16 is taken off
+// in the term with l.  Of the output
 //     sum_j p_j (l_jg + s_jg c_jd) = sum_j (p_j s_jg) (16 + c_jd) + sum_j p_j (l_jg - 16 s_jg),
-// the weights p s of a group as the operand, in two numbers of bf16 whatever the cache's type (hi + lo: 16 significant bits; one alone would add an error as
-// large as the output's rounding), the last sum in fp32.  Of fp16 they would be 22 bits where p s is large, but nothing below 2^-25, and the two sums then disagree by
-// up to 31 times that a key, however small the values are (16384 keys, logits of deviation 3, values of 0.01: 2 % of the output; 4e-6 so).
+// the weights p s of a group as the operand, in two numbers of bf16 whatever the cache's type (hi + lo: 16 significant
+// bits; one alone would add an error as large as the output's rounding), the last sum in fp32.  Of fp16 they would be 22
+// bits where p s is large, but nothing below 2^-25, and the two sums then disagree by up to 31 times that a key, however
+// small the values are (16384 keys, logits of deviation 3, values of 0.01: 2 % of the output; 4e-6 so).
 //
-// Lanes (16 x 16 x 32): n = lane % 16, c = lane / 16.  Scores of 16 query heads (rows) and 16 keys (columns): the lane of a key has its
-// scales in registers.  Query head h of a tile sits in row 4 (h % 4) + h / 4, so that R = ceil(heads / 4) of a lane's four rows are in use.
-// The weights pass through LDS (a wavefront's own), where lane n then finds row n; V's codes pass through LDS too, and the transposing
-// read of 4-bit elements gives lane n the codes of element n of 16 keys: two operands of eight.
-// A wavefront takes 64 keys at a time, four tiles of 16, every fourth such block of its workgroup's chunk; the four are joined at the end.  (Workgroups of one wavefront, with
-// a chunk and a partial result each, did 32 x 64/8 heads x 4096 keys in 38.5 us at their best chunk, these in 35.4.)  Of the 64, operand u of
-// lanes c takes keys of two tiles, 2 (c / 2) and the next, 8 (c % 2) + 4 u .. + 3 of each: what a lane has of the two tiles then lies side by side (expand's pairs).
-// What bounds it: vector instructions, 55 % of the issue slots (16 x 32 heads x up to 4096 keys, fp16: 50 us, 4.3 TB/s; 32 x 64/8 heads x 4096, bf16: 37 us, 4.2), which do not run under
-// the other wavefront's matrix instructions (18 %).
+// Lanes (16 x 16 x 32): n = lane % 16, c = lane / 16.  Scores of 16 query heads (rows) and 16 keys (columns): the lane of a
+// key has its scales in registers.  Query head h of a tile sits in row 4 (h % 4) + h / 4, so that R = ceil(heads / 4) of a
+// lane's four rows are in use.
+// The weights pass through LDS (a wavefront's own), where lane n then finds row n; V's codes pass through LDS too, and the
+// transposing read of 4-bit elements gives lane n the codes of element n of 16 keys: two operands of eight.
+// A wavefront takes 64 keys at a time, four tiles of 16, every fourth such block of its workgroup's chunk; the four are
+// joined at the end.  (Workgroups of one wavefront, with a chunk and a partial result each, did 32 x 64/8 heads x 4096 keys
+// in 38.5 us at their best chunk, these in 35.4.)  Of the 64, operand u of lanes c takes keys of two tiles, 2 (c / 2) and
+// the next, 8 (c % 2) + 4 u .. + 3 of each: what a lane has of the two tiles then lies side by side (expand's pairs).
+// What bounds it: vector instructions, 55 % of the issue slots (16 x 32 heads x up to 4096 keys, fp16: 50 us, 4.3 TB/s; 32
+// x 64/8 heads x 4096, bf16: 37 us, 4.2), which do not run under the other wavefront's matrix instructions (18 %).
 constexpr int kBlock = 64;                       // keys of a wavefront step
 constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
-constexpr int kRowStride = 144;                  // bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
+// bytes of a row of weights: 64 of two bytes, and 16 so that rows start in different banks
+constexpr int kRowStride = 144;
 
-// The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see the latent rows' kernel.
+// The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see
+// the latent rows' kernel.
 // (32 x 64/8 heads x 4096 keys, bf16: 37.5 us with 2, 37.0 with 8.)
 constexpr float kSlack = 8.f;
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
-template <> struct Magic<F16> { static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u; static constexpr int kShift = 6; };
-template <> struct Magic<BF16> { static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u; static constexpr int kShift = 3; };
+template <> struct Magic<F16> {
+    static constexpr unsigned kSixteen = 0x4c004c00u, kMask = 0x03c003c0u;
+    static constexpr int kShift = 6;
+};
+template <> struct Magic<BF16> {
+    static constexpr unsigned kSixteen = 0x41804180u, kMask = 0x00780078u;
+    static constexpr int kShift = 3;
+};
 
-// Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).  sixteen: Magic::kSixteen in a register the compiler cannot see through, which keeps
-// "and" and "or" one instruction (of two constants only one can be other than a register).
+// Eight codes of a word as an operand: pairs (0, 4), (1, 5), (2, 6), (3, 7).  sixteen: Magic::kSixteen in a register the
+// compiler cannot see through, which keeps "and" and "or" one instruction (of two constants only one can be other than a
+// register).
 template <class T> __device__ __forceinline__ u32x4_t expand(unsigned w, unsigned sixteen)
 {
     constexpr int k = Magic<T>::kShift;
@@ -188,22 +210,27 @@ template <int R> struct NibbleLds {
     union {
         struct {
             alignas(16) unsigned char v[4][2][kBlock * 64];            // of this step and of the next
-            alignas(16) unsigned char w[4][2][2][4 * R * kRowStride];  // weights of a group, two groups in turn: hi and lo parts; row 4 c + r in place R c + r
+            // weights of a group, two groups in turn: hi and lo parts; row 4 c + r in place R c + r
+            alignas(16) unsigned char w[4][2][2][4 * R * kRowStride];
         };
         float rows[4][4 * R][kHeadDim];                                // at the end: the wavefronts' sums
     };
     float m[4][4 * R], l[4][4 * R];
     int last;
 };
-// Loads into LDS, 1 KiB at lds_1k.  In assembly: of those that the compiler knows it would wait before every transposing read.  They are older than the loads of K's codes of
-// the same step, and loads arrive in order: once K's codes are there, so are they.
+// Loads into LDS, 1 KiB at lds_1k.  In assembly: of those that the compiler knows it would wait before every transposing
+// read.  They are older than the loads of K's codes of the same step, and loads arrive in order: once K's codes are there,
+// so are they.
 __device__ __forceinline__ void load_to_lds(const unsigned char *base, int voff, unsigned lds_1k)
 {
     const unsigned long long at = reinterpret_cast<unsigned long long>(base);
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds_1k), "v"(voff), "s"(at) : "memory");
 }
 
-template <class T> __device__ __forceinline__ float scale_at(const unsigned *w, int i) { return (i & 1) ? T::hi(w[i >> 1]) : T::lo(w[i >> 1]); }
+template <class T> __device__ __forceinline__ float scale_at(const unsigned *w, int i)
+{
+    return (i & 1) ? T::hi(w[i >> 1]) : T::lo(w[i >> 1]);
+}
 
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
@@ -226,7 +253,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     if (start >= end) {
         // a sequence without keys: zero rows, by the first chunk (other chunks without keys leave nothing)
         if (chunk == 0)
-            for (int i = tid; i < heads * kHeadDim / 2; i += 256) reinterpret_cast<unsigned *>(p.out + ((size_t)b * p.Hq + head0) * kHeadDim)[i] = 0u;
+            for (int i = tid; i < heads * kHeadDim / 2; i += 256)
+                reinterpret_cast<unsigned *>(p.out + ((size_t)b * p.Hq + head0) * kHeadDim)[i] = 0u;
         return;
     }
     constexpr int SW = NG;                         // 32-bit words of a row's scales
@@ -270,7 +298,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     };
     // V's codes in LDS: row of key k of tile i at 64 (16 i + k), its 16-byte piece x in place x ^ (2 (i % 2) + (k / 4) % 2)
     const int v_lane = 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 4) & 1));
-    const unsigned v_lds = __builtin_amdgcn_readfirstlane((unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)lds.v[wave][0]));
+    const unsigned v_lds = __builtin_amdgcn_readfirstlane(
+        (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char *)lds.v[wave][0]));
     auto load_v = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -332,7 +361,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     asm("v_mov_b32 %0, %1" : "=v"(sixteen_v) : "i"(Magic<BF16>::kSixteen));
 
     unsigned char *w_at = lds.w[wave][0][0];
-    constexpr int kLo = 4 * R * kRowStride, kTurn = 2 * kLo;               // from a hi part to its lo part, from a group to the next
+    // from a hi part to its lo part, from a group to the next
+    constexpr int kLo = 4 * R * kRowStride, kTurn = 2 * kLo;
     const int w_row = (R * (n >> 2) + min(n & 3, R - 1)) * kRowStride;      // of row n (of rows that no head sits in: another's)
     // this lane's row for the transposing reads of V's codes
     const int v_tile = 2 * (c >> 1) + ((n >> 2) & 1), v_key = 8 * (c & 1) + 4 * (n >> 3) + (n & 3);
@@ -341,8 +371,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 
     for (; key0 < end; key0 += 4 * kBlock, buffer ^= 1) {
         const int next = key0 + 4 * kBlock;
-        // Scores, in units of log2.  The matrix instructions of a tile run while the codes of the next are expanded (left to itself the compiler takes one register
-        // after the other through expand, product and sum, and waits in between).
+        // Scores, in units of log2.  The matrix instructions of a tile run while the codes of the next are expanded (left
+        // to itself the compiler takes one register after the other through expand, product and sum, and waits in between).
         float z[4][R];
         {
             u32x4_t e[4];
@@ -354,7 +384,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
                 u32x4_t en[4];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) a[t * NG / 4] = T::mfma(qa[t], e[t], t % (4 / NG) == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : a[t * NG / 4]);
+                for (int t = 0; t < 4; ++t)
+                    a[t * NG / 4] = T::mfma(qa[t], e[t], t % (4 / NG) == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : a[t * NG / 4]);
                 if (i < 3)
 #pragma unroll
                     for (int t = 0; t < 4; ++t) en[t] = expand<T>(kc[i + 1][t], sixteen);
@@ -391,12 +422,14 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
                 const bool live = key0 + 16 * i + n < end;
 #pragma unroll
                 for (int r = 0; r < R; ++r) z[i][r] = live ? z[i][r] : -INFINITY;
+                // of keys that are not there: may be anything
 #pragma unroll
-                for (int k = 0; k < SW; ++k) vs[i][k] = live ? vs[i][k] : 0u;          // of keys that are not there: may be anything
+                for (int k = 0; k < SW; ++k) vs[i][k] = live ? vs[i][k] : 0u;
             }
         }
         asm volatile("" ::: "memory");                                                 // K's codes have been used: V's are there
-        __builtin_amdgcn_s_waitcnt(0xc07f);                                            // ... and what was read of the step before has arrived
+        // ... and what was read of the step before has arrived
+        __builtin_amdgcn_s_waitcnt(0xc07f);
         if (next < end) {                                                              // under way during the rest of the step
             find_rows(next);
             load_v(buffer ^ 1);
@@ -438,7 +471,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
                 const float s0 = scale_at<T>(vs[i], g), s1 = scale_at<T>(vs[i + 1], g);
-                const float l0 = __builtin_fmaf(-16.f, s0, scale_at<T>(vs[i], NG + g)), l1 = __builtin_fmaf(-16.f, s1, scale_at<T>(vs[i + 1], NG + g));
+                const float l0 = __builtin_fmaf(-16.f, s0, scale_at<T>(vs[i], NG + g));
+                const float l1 = __builtin_fmaf(-16.f, s1, scale_at<T>(vs[i + 1], NG + g));
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     low[r][g] = __builtin_fmaf(z[i][r], l0, low[r][g]);
@@ -455,7 +489,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
         typedef __attribute__((address_space(3))) i32x2 *lds_i32x2;
         // 16 elements from 16 dt of this lane's row: lane n receives element n of the 16 rows
         auto read_v = [&](int dt) {
-            return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2)(v_row + buffer * (kBlock * 64) + (((dt >> 1) ^ v_turn) << 4) + ((dt & 1) << 3)));
+            const unsigned char *at = v_row + buffer * (kBlock * 64) + (((dt >> 1) ^ v_turn) << 4) + ((dt & 1) << 3);
+            return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2)at);
         };
         i32x2 vc[2][2];                                                                // of elements 32 pr .. + 31, two in turn
         vc[0][0] = read_v(0);
@@ -557,7 +592,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
         } else {
             const size_t slot = out_row * p.nc + chunk;
             float *num = p.num + slot * kHeadDim + 2 * lane, *ml = reinterpret_cast<float *>(p.ml + slot);
-            if (p.counters) {                                              // past the caches: a workgroup on another XCD may join the row
+            // past the caches: a workgroup on another XCD may join the row
+            if (p.counters) {
                 store_coherent2(num, a0, a1);
                 if (lane == 0) store_coherent2(ml, top, sum);
             } else {
@@ -567,7 +603,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
         }
     }
     if (!p.counters || chunks == 1) return;
-    // The workgroup of the group's last chunk to arrive joins its rows: a round trip to memory for the stores, one for the counter, one for the partial results.
+    // The workgroup of the group's last chunk to arrive joins its rows: a round trip to memory for the stores, one for the
+    // counter, one for the partial results.
     wait_stores_performed();
     __syncthreads();
     if (tid == 0) {
@@ -580,7 +617,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
     for (int h = wave; h < heads; h += 4) {
         const size_t out_row = (size_t)b * p.Hq + head0 + h, slot = out_row * p.nc;
         // chunk i's reference and denominator in lane i of every 16; all partial vectors under way before the first is used
-        unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + min(n, chunks - 1))), x[kJoinInPlace];
+        unsigned long long x[kJoinInPlace];
+        const unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + min(n, chunks - 1)));
 #pragma unroll
         for (int i = 0; i < kJoinInPlace; ++i)
             x[i] = load_coherent(reinterpret_cast<const unsigned long long *>(p.num + (slot + min(i, chunks - 1)) * kHeadDim) + lane);
@@ -602,7 +640,8 @@ template <class T, int NG, int R> __global__ __launch_bounds__(256, 2) void nibb
 }
 
 // ---- the join of rows that several workgroups share ----
-// A workgroup a row, of several slices that take every kSlices-th eight of the partial vectors.  Its length is that of its loads, so as many as can be are asked for together:
+// A workgroup a row, of several slices that take every kSlices-th eight of the partial vectors.  Its length is that of its
+// loads, so as many as can be are asked for together:
 // first the references and denominators of 64 chunks, then, with their factors in LDS, eight vectors of a slice at a time.
 constexpr int kJoinWindow = 64;
 template <class T, int DIM, int kSlices> __global__ __launch_bounds__(DIM / 2 * kSlices) void join_kernel(JoinProblem p)
@@ -679,18 +718,19 @@ template <class T> hipError_t attn_groups(const NibbleProblem &p, hipStream_t s)
 hipError_t launch_nibble_write(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
-    return pool.dtype == kF16 ? launch(nibble_write_kernel<F16>, grid, dim3(256), s, pool, rows) : launch(nibble_write_kernel<BF16>, grid, dim3(256), s, pool, rows);
+    return launch(pool.dtype == kF16 ? nibble_write_kernel<F16> : nibble_write_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
 hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
-    return pool.dtype == kF16 ? launch(nibble_read_kernel<F16>, grid, dim3(256), s, pool, rows) : launch(nibble_read_kernel<BF16>, grid, dim3(256), s, pool, rows);
+    return launch(pool.dtype == kF16 ? nibble_read_kernel<F16> : nibble_read_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
 template <class T, int DIM> static hipError_t join(const JoinProblem &p, hipStream_t s)
 {
     const dim3 grid((unsigned)p.rows);
     // (of up to eight vectors a row every slice but one would be idle: 128 x 128 latent rows of two 83 us, with two slices 97)
-    return p.nc > 8 ? launch(join_kernel<T, DIM, 1024 / DIM>, grid, dim3(512), s, p) : launch(join_kernel<T, DIM, 1>, grid, dim3(DIM / 2), s, p);
+    if (p.nc > 8) return launch(join_kernel<T, DIM, 1024 / DIM>, grid, dim3(512), s, p);
+    return launch(join_kernel<T, DIM, 1>, grid, dim3(DIM / 2), s, p);
 }
 hipError_t launch_join(const JoinProblem &p, hipStream_t s)
 {
@@ -700,7 +740,8 @@ hipError_t launch_join(const JoinProblem &p, hipStream_t s)
 hipError_t launch_nibble_attn(const NibbleProblem &p_, hipStream_t s)
 {
     NibbleProblem p = p_;
-    // A workgroup that joins a unit's rows keeps the others of its compute unit waiting less than a second launch costs while there are few.
+    // A workgroup that joins a unit's rows keeps the others of its compute unit waiting less than a second launch costs
+    // while there are few.
     if (p.nc > kJoinInPlace || (long long)p.B * p.pool.Hkv * p.tiles * p.nc > kJoinWorkgroups) p.counters = nullptr;
     const hipError_t e = p.pool.dtype == kF16 ? attn_groups<F16>(p, s) : attn_groups<BF16>(p, s);
     if (e != hipSuccess || p.nc == 1 || p.counters) return e;

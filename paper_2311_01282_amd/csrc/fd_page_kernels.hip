@@ -1,14 +1,15 @@
 // Page tables and slot maps from request lengths, in one launch.
 //
-// Request b holds ceil(c / P) pages for its c cached tokens and needs ceil((c + n) / P) with its n new ones; the difference is
-// taken from the end of the free list, in the order of the requests, so that request b's share starts where the needs of those
-// before it add up to: a prefix sum.  A token's place follows from another prefix sum (whose token it is) and the table.
+// Request b holds ceil(c / P) pages for its c cached tokens and needs ceil((c + n) / P) with its n new ones; the difference
+// is taken from the end of the free list, in the order of the requests, so that request b's share starts where the needs of
+// those before it add up to: a prefix sum.  A token's place follows from another prefix sum (whose token it is) and the
+// table.
 //
 // Every workgroup forms both prefix sums itself, over all requests, and then serves its own 1024 tokens: a token looks its
-// request up among the starts in LDS and takes its page from the table if the request held it before, and straight from the free list
-// if it is fresh (another workgroup may be the one to write that entry).  Each fresh page has a first token, which writes the
-// table's entry.  What bounds it is latency (8 requests 3.9 us, 300 prompts of 600000
-// tokens 8.2): a scan by one workgroup followed by a launch that fills would pay a second launch.
+// request up among the starts in LDS and takes its page from the table if the request held it before, and straight from the
+// free list if it is fresh (another workgroup may be the one to write that entry).  Each fresh page has a first token,
+// which writes the table's entry.  What bounds it is latency (8 requests 3.9 us, 300 prompts of 600000 tokens 8.2): a scan
+// by one workgroup followed by a launch that fills would pay a second launch.
 #include "fd_cache.h"
 
 namespace fd {
@@ -26,7 +27,8 @@ struct PageLds {
     int taken[kThreads / 64];
 };
 
-// Sums of tokens and of pages end at kMany, which is more than there may be of either (max_tokens <= 2^30, fewer pages): sums that end somewhere add in any order as sums do.
+// Sums of tokens and of pages end at kMany, which is more than there may be of either (max_tokens <= 2^30, fewer pages):
+// sums that end somewhere add in any order as sums do.
 constexpr unsigned kMany = (1u << 30) + 1;
 __device__ __forceinline__ unsigned add(unsigned a, unsigned b) { return min(a + b, kMany); }
 template <int kControl, int kRows> __device__ __forceinline__ unsigned add_dpp(unsigned x)
@@ -74,7 +76,8 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
         unsigned tok = 0;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) tok = add(tok, n[i]);
-        const unsigned run = prefix(tok), before = (unsigned)__builtin_amdgcn_update_dpp(0, (int)run, 0x138, 0xf, 0xf, false);      // (without this lane's)
+        // (without this lane's)
+        const unsigned run = prefix(tok), before = (unsigned)__builtin_amdgcn_update_dpp(0, (int)run, 0x138, 0xf, 0xf, false);
         if (lane == 63) lds.tokens[wave] = run;
         __syncthreads();
         unsigned start = tokens_before, all = tokens_before;
@@ -110,12 +113,14 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             const int r = tid * kItems + i, b = w0 + r;
             const unsigned upto = add(off, need[i]);
             const bool listed = upto <= (unsigned)n_free, served = fits[i] && (need[i] == 0 || listed);
-            if (listed) taken = (int)upto;                                  // (grows along the requests of a thread, and from window to window)
+            // (grows along the requests of a thread, and from window to window)
+            if (listed) taken = (int)upto;
             if (b < p.batch) {
                 const int s = (int)min(at, (unsigned)p.max_tokens);
                 lds.start[r] = s;
                 lds.cached[r] = c[i];
-                lds.offset[r] = served ? (int)min(off, (unsigned)n_free) : -1;      // (beyond the list only where nothing is needed)
+                // (beyond the list only where nothing is needed)
+                lds.offset[r] = served ? (int)min(off, (unsigned)n_free) : -1;
                 if ((b / kWindow + r / 64) % gridDim.x == blockIdx.x) {     // the workgroups share these out by 64 requests
                     p.starts[b] = s;
                     p.seq_lens[b] = served ? c[i] + n[i] : c[i];
@@ -127,7 +132,8 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
         __syncthreads();
         // tokens of this window's requests
         const int end = (int)min(all, (unsigned)p.max_tokens), first = (int)min(tokens_before, (unsigned)p.max_tokens);
-        const int32_t *from[kTokens];                                       // where the token's page stands; null: no slot from this window
+        // where the token's page stands; null: no slot from this window
+        const int32_t *from[kTokens];
         int32_t *to[kTokens];                                               // the table's entry, of a fresh page's first token
         int in_page[kTokens], page[kTokens];
 #pragma unroll
@@ -151,8 +157,9 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(PageProblem p)
             from[i] = j < held ? entry : p.free_pages + (n_free - 1 - (lds.offset[lo] + j - held));
             if (j >= held && in_page[i] == 0) to[i] = entry;
         }
+        // (all before the first store, which they might otherwise have to wait for)
 #pragma unroll
-        for (int i = 0; i < kTokens; ++i)                                   // (all before the first store, which they might otherwise have to wait for)
+        for (int i = 0; i < kTokens; ++i)
             if (from[i]) page[i] = *from[i];
 #pragma unroll
         for (int i = 0; i < kTokens; ++i) {

@@ -16,12 +16,17 @@ typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 struct F16 {
     static constexpr float kSmallest = 0x1p-14f;           // normal number
     static constexpr unsigned kInfinity = 0x7c00u;         // bits
-    // log2 of a softmax weight at its reference.  Numbers below 2^-25 round to nothing: of weights from 1 downwards that is what 16384 keys leave out 17 below the largest logit, 5e-4
-    // of their sum.  With this they are counted from 2^-32, and weights up to 2^8 times the reference's still fit.
+    // log2 of a softmax weight at its reference.  Numbers below 2^-25 round to 0.  With a reference of 1 that loses the
+    // weights of keys 17.4 and more below the largest logit: of 16384 such keys 5e-4 of the sum.  With 2^7 it loses those
+    // below 2^-32 of it, and weights of 2^8 times the reference's are still numbers.
     static constexpr float kLift = 7.f;
     static __device__ __forceinline__ float lo(unsigned w) { return (float)__builtin_bit_cast(f16x2_t, w).x; }
     static __device__ __forceinline__ float hi(unsigned w) { return (float)__builtin_bit_cast(f16x2_t, w).y; }
-    static __device__ __forceinline__ unsigned short bits(float x) { const _Float16 h = (_Float16)x; return __builtin_bit_cast(unsigned short, h); }
+    static __device__ __forceinline__ unsigned short bits(float x)
+    {
+        const _Float16 h = (_Float16)x;
+        return __builtin_bit_cast(unsigned short, h);
+    }
     static __device__ __forceinline__ unsigned pack(float a, float b)
     {
         f16x2_t h;
@@ -40,7 +45,11 @@ struct BF16 {
     static constexpr float kLift = 0.f;
     static __device__ __forceinline__ float lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
     static __device__ __forceinline__ float hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
-    static __device__ __forceinline__ unsigned short bits(float x) { const __bf16 h = (__bf16)x; return __builtin_bit_cast(unsigned short, h); }
+    static __device__ __forceinline__ unsigned short bits(float x)
+    {
+        const __bf16 h = (__bf16)x;
+        return __builtin_bit_cast(unsigned short, h);
+    }
     static __device__ __forceinline__ unsigned pack(float a, float b)
     {
         bf16x2_t h;
