@@ -252,6 +252,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         float z[2][8], top[2];
         f32x4_t scn[2][2];
         u32x4_t a[12], av[8], w[2];
+        const u32x4_t none_of = {0u, 0u, 0u, 0u};
+        f32x4_t any[2] = {zero, zero};                         // V^T times 0: NaN where a value is not finite
 #pragma unroll
         for (int op = 0; op < 4; ++op) a[op] = first[op];
         auto score_slot = [&](auto mi) {
@@ -263,6 +265,7 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         slots(std::make_integer_sequence<int, 12>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
             if constexpr (!kLast) score_slot(mi);
+            if constexpr (kLast && mm < 8) av[mm] = read_v(vv, mm);      // (early: see `any`)
             if constexpr (mm == 1) fetch_k();
             if constexpr (mm == 3) fetch_r();
             if constexpr (mm == 5) fetch_v();
@@ -316,7 +319,8 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
         slots(std::make_integer_sequence<int, 12>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
             if constexpr (!kLast) score_slot(std::integral_constant<int, mm + 12>{});
-            if constexpr (mm >= 2 && mm < 10) av[mm - 2] = read_v(vv, mm - 2);
+            if constexpr (!kLast && mm >= 2 && mm < 10) av[mm - 2] = read_v(vv, mm - 2);
+            if constexpr (kLast && mm < 8) any[mm & 1] = T::mfma(av[mm], none_of, any[mm & 1]);
             if constexpr (mm < 8) {
                 z[0][mm] = __builtin_amdgcn_exp2f(z[0][mm]);
                 if constexpr (mm & 1) w[0][mm >> 1] = T::pack(z[0][mm - 1], z[0][mm]);
@@ -324,13 +328,9 @@ template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) v
             __builtin_amdgcn_sched_barrier(0);
         });
         // In the step with masks the weights of keys behind a query are 0, and 0 times an infinite value or a NaN is NaN:
-        // such values leave the product, and the queries that see them get them as a summand.  (Whether there are any: a
-        // product with 0.  In the steps before all keys are seen.)
+        // such values leave the product, and the queries that see them get them as a summand.  (In the steps before all
+        // keys are seen.)
         if constexpr (kLast) {
-            const u32x4_t none_of = {0u, 0u, 0u, 0u};
-            f32x4_t any[2] = {zero, zero};
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) any[dt & 1] = T::mfma(av[dt], none_of, any[dt & 1]);
             const float all_of = (any[0][0] + any[0][1]) + (any[0][2] + any[0][3]) + (any[1][0] + any[1][1]) + (any[1][2] + any[1][3]);
             if (__any(all_of != 0.f)) {
                 u32x4_t seen[2];
