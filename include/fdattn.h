@@ -486,6 +486,8 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     without a valid token are not followed, an entry in use that is out of range is the caller's error (it is
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
+ *   Numbers.  Scores and outputs are summed in fp32 before they are scaled: bf16 numbers beyond 2^59 in queries and keys, or
+ *     2^100 in values, may overflow there.
  *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128), and there
  *     also, batch * n_q_heads rounded up to a multiple of 8, < 2^24.
  *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
@@ -556,7 +558,7 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
  * q, out [batch, n_q_heads, 128] of the pool's dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of
  * 64 from 64 to 16384 keys, for example fd_nibble_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
  * Scores are accumulated in fp32; the weights times V's scales enter the second product as two numbers of bf16 each, 16
- * significant bits whatever their size (values beyond 2^100 may overflow the fp32 sums).  A sequence of length 0 gives zero rows.  One launch for up to 16
+ * significant bits whatever their size.  A sequence of length 0 gives zero rows.  One launch for up to 16
  * chunks a row and up to 512 workgroups (one for each chunk of up to 16 heads that share a KV head), else two.
  */
 size_t    fd_nibble_workspace_bytes(const fd_shape *shape);

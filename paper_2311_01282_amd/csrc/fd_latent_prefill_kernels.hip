@@ -11,8 +11,8 @@
 // end (kHalves).
 // Softmax with a running maximum per query; the weights are of the type (one rounding, as large as the output's own), their
 // sum is that of the rounded ones, in fp32.
-// The matrix cores bound long prompts, at the clock that power leaves them: 64 heads x 4001 tokens 353 .. 385 us, 0.85 ..
-// 0.93 PFLOP/s of what the mask leaves, matrix instructions in 53 % of the cycles; short ones the length of a tile's walk.
+// The matrix cores bound long prompts, at the clock that power leaves them: 64 heads x 4001 tokens 331 .. 373 us, 0.88 ..
+// 0.99 PFLOP/s of what the mask leaves, matrix instructions in 53 % of the cycles; short ones the length of a tile's walk.
 #include <utility>
 
 #include "fd_chunk.h"

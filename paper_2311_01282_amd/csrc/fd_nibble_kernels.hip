@@ -167,10 +167,10 @@ template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(Nib
 // transposing read of 4-bit elements gives lane n the codes of element n of 16 keys: two operands of eight.
 // A wavefront takes 64 keys at a time, four tiles of 16, every fourth such block of its workgroup's chunk; the four are
 // joined at the end.  (Workgroups of one wavefront, with a chunk and a partial result each, did 32 x 64/8 heads x 4096 keys
-// in 38.5 us at their best chunk, these in 35.4.)  Of the 64, operand u of lanes c takes keys of two tiles, 2 (c / 2) and
+// in 38.5 us at their best chunk, these then 35.4.)  Of the 64, operand u of lanes c takes keys of two tiles, 2 (c / 2) and
 // the next, 8 (c % 2) + 4 u .. + 3 of each: what a lane has of the two tiles then lies side by side (expand's pairs).
-// What bounds it: vector instructions, 55 % of the issue slots (16 x 32 heads x up to 4096 keys, fp16: 50 us, 4.3 TB/s; 32
-// x 64/8 heads x 4096, bf16: 37 us, 4.2), which do not run under the other wavefront's matrix instructions (18 %).
+// What bounds it: vector instructions, 60 % of the issue slots (16 x 32 heads x up to 4096 keys, fp16: 50 us, 4.3 TB/s; 32
+// x 64/8 heads x 4096, bf16: 34 us, 4.5), which do not run under the other wavefront's matrix instructions (18 %).
 constexpr int kBlock = 64;                       // keys of a wavefront step
 constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
@@ -179,7 +179,7 @@ constexpr int kRowStride = 144;
 
 // The reference of a row's weights follows its maximum only where that has grown by more than this (in units of log2): see
 // the latent rows' kernel.
-// (32 x 64/8 heads x 4096 keys, bf16: 37.5 us with 2, 37.0 with 8.)
+// (32 x 64/8 heads x 4096 keys, bf16: 1 % less than with 2.)
 constexpr float kSlack = 8.f;
 template <class T> struct Magic;                 // 16 + c: c in the low bits above the last ones of the mantissa of 16
 template <> struct Magic<F16> {

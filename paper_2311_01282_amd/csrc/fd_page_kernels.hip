@@ -8,7 +8,7 @@
 // Every workgroup forms both prefix sums itself, over all requests, and then serves its own 1024 tokens: a token looks its
 // request up among the starts in LDS and takes its page from the table if the request held it before, and straight from the
 // free list if it is fresh (another workgroup may be the one to write that entry).  Each fresh page has a first token,
-// which writes the table's entry.  What bounds it is latency (8 requests 3.9 us, 300 prompts of 600000 tokens 8.2): a scan
+// which writes the table's entry.  What bounds it is latency (8 requests 4.0 us, 300 prompts of 600000 tokens 8.2): a scan
 // by one workgroup followed by a launch that fills would pay a second launch.
 #include "fd_cache.h"
 
