@@ -487,7 +487,7 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
  *   Numbers.  Scores and outputs are summed in fp32 before they are scaled: bf16 numbers beyond 2^59 in queries and keys, or
- *     2^100 in values, may overflow there.
+ *     2^100 in values, may overflow there.  In latent attention fp16 weights below 2^-32 of a row's largest count as nothing.
  *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128), and there
  *     also, batch * n_q_heads rounded up to a multiple of 8, < 2^24.
  *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
