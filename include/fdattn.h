@@ -473,12 +473,12 @@ fd_status fd_prefill_attn(const fd_shape *shape, const void *q, const void *k_ca
  * the guard fired for a logit of those 64 queries (the tile they are in was recomputed). */
 fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uint8_t **tile_flags);
 
-/* ---- Smaller paged caches: page tables, a 4-bit cache, latent attention ----
+/* ---- Smaller paged caches: page tables, a 4-bit cache, latent attention, a cache of 16 or 8 bits ----
  *
  * What a serving step over a paged cache needs besides fp16 attention: pages and slots for the step's
  * tokens (fd_page_tables), a cache in 4 bits with the calls that fill, read and attend over it (fd_nibble_*,
- * fd_decode_attn_nibble), and a cache of latent rows with its attention (fd_latent_*).  All of them take
- * fp16 or bf16.  The softmax is the synchronized one (a running maximum): no phi, no bounds, no flags.
+ * fd_decode_attn_nibble), a cache of latent rows with its attention (fd_latent_*), and a cache of 16-bit or e4m3 rows with the
+ * attention of a whole step, prompts and single tokens in one call (fd_kv_*).  All of them take fp16 or bf16.  The softmax is the synchronized one (a running maximum): no phi, no bounds, no flags.
  *   Slots.  Slot s of a pool is row s % page_size of page s / page_size; page_size is a power of two >= 16
  *     and n_pages * page_size < 2^31.  A slot outside [0, n_pages * page_size), -1 for example, is padding: its
  *     token is skipped.  The slots of one call that are no padding have to differ from each other.
@@ -490,15 +490,15 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     2^100 in values, may overflow there.  In latent attention fp16 weights below 2^-32 of a row's largest count as nothing.
  *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128), and there
  *     also, batch * n_q_heads rounded up to a multiple of 8, < 2^24.
- *   Workspaces (of the two decode calls).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
+ *   Workspaces (of the decode calls and of fd_kv_prefill_attn).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
  *     its first 16 KiB, arrival counters that every completed call leaves at zero again; what lies behind them may hold anything.  After that
  *     shapes and calls may change from one use to the next.  A workspace serves one call at a time: calls that may overlap, captured
  *     graphs that are replayed at the same time among them, need one each; so do these calls and the others of this
  *     header.  After a call that did not complete prepare it again (a left-over count keeps rows from being written).
  * Memory, stream, errors and threads: as stated at the top.                                                     */
-typedef enum { FD_F16 = 0, FD_BF16 = 1 } fd_dtype;
+typedef enum { FD_F16 = 0, FD_BF16 = 1, FD_E4M3 = 2 /* what fd_kv_pool keeps, no type of rows or queries */ } fd_dtype;
 
-/* Zeroes the arrival counters of a workspace for fd_decode_attn_nibble and fd_latent_decode_attn. */
+/* Zeroes the arrival counters of a workspace for fd_decode_attn_nibble, fd_latent_decode_attn and the fd_kv_* calls. */
 fd_status fd_cache_workspace_init(fd_workspace ws, void *stream);
 
 /*
@@ -607,6 +607,67 @@ fd_status fd_latent_decode_attn(const fd_shape *shape, const fd_latent_pool *poo
  */
 fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const void *q, const void *kv, const void *rope,
                                  int64_t rope_stride, const int32_t *seq_lens, void *out, void *stream);
+
+/*
+ * A cache of rows in 16 or in 8 bits.
+ *   k, v [n_pages, n_kv_heads, page_size, 128] of type `store`, 16-byte aligned: with store FD_F16 the pools of fd_decode_attn_paged.
+ *   k_scales, v_scales  store FD_E4M3: [n_pages, n_kv_heads, page_size] bytes, 16-byte aligned; else not used.
+ * store is dtype, or FD_E4M3 (one sign, four exponent and three mantissa bits, bias 7, no infinities).  A row of 8 bits stands for
+ * c_d 2^(byte - 127) with its codes' numbers c_d.  head_dim == 128.
+ */
+typedef struct {
+    void   *k, *v, *k_scales, *v_scales;
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+    int32_t store;             /* fd_dtype of the cache                            */
+    int32_t dtype;             /* fd_dtype of the rows, queries and outputs        */
+} fd_kv_pool;
+
+/*
+ * Rows into the cache.  k, v [n_tokens, n_kv_heads, 128] with strides of their own, slots and limits as fd_nibble_write.  16 bits: as they
+ * are.  8 bits, per row: e the smallest whole number with max |x| <= 448 2^e, not below -117; c = x 2^-e rounded to e4m3 (ties to
+ * even), its size limited to 240 where 256 2^e is beyond dtype; the byte e + 127.  A row with an infinite element or a NaN reads as
+ * NaN, all of it (byte 255, codes NaN).
+ */
+fd_status fd_kv_write(const fd_kv_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
+                      const int32_t *slot_map, void *stream);
+
+/* Rows out of the cache, as the numbers of dtype that they stand for (of rows that fd_kv_write wrote exactly).  Layouts and slots as
+ * fd_kv_write; rows of padding are left as they are. */
+fd_status fd_kv_read(const fd_kv_pool *pool, const int32_t *slot_map, int32_t n_tokens, void *k, int64_t k_stride, void *v,
+                     int64_t v_stride, void *stream);
+
+/*
+ * Decode attention: out = softmax(scale q K^T) V, one query token a sequence, with the numbers that the rows stand for.
+ * q, out [batch, n_q_heads, 128] of dtype.  shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple
+ * of 64 from 64 to 16384 keys, for example fd_kv_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
+ * Scores and sums in fp32; the weights enter the second product as two numbers of dtype each.  A sequence of length 0 gives zero
+ * rows.  One launch for up to 16 chunks a row and up to 512 workgroups (one for each chunk of up to 16 heads that share a KV head), else two.
+ */
+size_t    fd_kv_workspace_bytes(const fd_shape *shape);
+int32_t   fd_kv_pick_chunk(const fd_shape *shape);
+fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, const int32_t *block_table,
+                            const int32_t *seq_lens, void *out, fd_workspace ws, void *stream);
+
+/*
+ * Attention of a step's new tokens, packed: whole prompts, further pieces of long ones and single tokens in any mixture.
+ *   q    [n_tokens, n_q_heads, 128] of dtype, q_stride elements from a token to the next (a multiple of 8, at least n_q_heads * 128)
+ *   token_starts [batch + 1]: sequence b's new tokens are token_starts[b] .. token_starts[b + 1] - 1 (as fd_page_tables gives them; clamped
+ *        to [0, n_tokens], fewer than none count as none)
+ *   seq_lens [batch]: keys of the sequence in the cache, the new tokens' own among them: they have been written before (fd_kv_write)
+ *   out  [n_tokens, n_q_heads, 128]; rows of no sequence are left as they are
+ * New token i of n in a sequence of L keys stands at position L - n + i and attends to the keys up to there; at a position
+ * below 0 (more new tokens than keys) its rows are zero.  Of a request that fd_page_tables did not serve, L is what was cached: its rows mean
+ * nothing, and neither fault nor touch other rows.
+ * shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of 64, for example
+ * fd_kv_prefill_pick_chunk(shape, n_tokens): keys that a workgroup takes at most; from max_seq on rows are not split.
+ * (n_tokens * n_q_heads / n_kv_heads / 128 + batch) * n_kv_heads * ceil(max_seq / chunk) <= 2^23.
+ * Scores and sums in fp32; the weights enter the second product as numbers of dtype.
+ */
+size_t    fd_kv_prefill_workspace_bytes(const fd_shape *shape, int32_t n_tokens);
+int32_t   fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens);
+fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, int64_t q_stride, int32_t n_tokens,
+                             const int32_t *token_starts, const int32_t *block_table, const int32_t *seq_lens, void *out,
+                             fd_workspace ws, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *fd_status_str(fd_status status);

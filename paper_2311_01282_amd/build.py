@@ -16,7 +16,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfdattn.so")
 SOURCES = ["fd_api.hip", "fd_row_kernels.hip", "fd_reduce_kernels.hip", "fd_gqa_kernels.hip",
            "fd_stats_kernels.hip", "fd_prefill_kernels.hip", "fd_cache_api.hip", "fd_page_kernels.hip",
-           "fd_nibble_kernels.hip", "fd_latent_kernels.hip", "fd_latent_prefill_kernels.hip"]
+           "fd_nibble_kernels.hip", "fd_latent_kernels.hip", "fd_latent_prefill_kernels.hip",
+           "fd_kv_kernels.hip", "fd_kv_prefill_kernels.hip"]
 # the benchmark's streaming-read probe: a library of its own, not part of libfdattn
 PROBE_LIB = os.path.join(HERE, "libfdprobe.so")
 PROBE_SOURCES = ["fd_probe.hip"]

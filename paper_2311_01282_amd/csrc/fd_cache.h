@@ -5,7 +5,7 @@
 
 namespace fd {
 
-enum { kF16 = 0, kBf16 = 1 };                      // fd_dtype
+enum { kF16 = 0, kBf16 = 1, kE4m3 = 2 };           // fd_dtype
 
 // fd_page_kernels.hip
 struct PageProblem {
@@ -22,14 +22,14 @@ struct NibblePool {
     uint16_t *k_scales, *v_scales;                 // [n_pages, Hkv, page, 2, NG]
     int n_pages, page_shift, Hkv, NG, dtype;       // NG groups to a row: 4, 2 or 1
 };
-struct NibbleRows {
+struct TokenRows {
     uint16_t *k, *v;                               // [n_tokens, Hkv, 128], token strides of their own
     long long k_stride, v_stride;                  // elements
     const int32_t *slots;
     int n_tokens;
 };
-hipError_t launch_nibble_write(const NibblePool &pool, const NibbleRows &rows, hipStream_t s);
-hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hipStream_t s);
+hipError_t launch_nibble_write(const NibblePool &pool, const TokenRows &rows, hipStream_t s);
+hipError_t launch_nibble_read(const NibblePool &pool, const TokenRows &rows, hipStream_t s);
 
 struct NibbleProblem {
     NibblePool pool;
@@ -77,6 +77,41 @@ struct LatentPromptProblem {
     float scale;
 };
 hipError_t launch_latent_prefill(const LatentPromptProblem &p, hipStream_t s);
+
+// fd_kv_kernels.hip
+struct KvPool {
+    unsigned char *k, *v;                          // [n_pages, Hkv, page, 128] of 16 or 8 bits
+    uint8_t *k_scales, *v_scales;                  // [n_pages, Hkv, page], of 8 bits: exponent + 127
+    int n_pages, page_shift, Hkv, store, dtype;
+};
+constexpr int kLowestExponent = -117;              // of a row: the smallest code, 2^-9, then stands for a normal number of bf16
+hipError_t launch_kv_write(const KvPool &pool, const TokenRows &rows, hipStream_t s);
+hipError_t launch_kv_read(const KvPool &pool, const TokenRows &rows, hipStream_t s);
+
+struct KvProblem {
+    KvPool pool;
+    const uint16_t *q;                             // [B, Hq, 128]
+    const int32_t *seq_lens, *table;
+    uint16_t *out;
+    float *num;                                    // workspace, as NibbleProblem's
+    float2 *ml;
+    int32_t *counters;
+    int B, Hq, G, tiles, C, nc, Smax, width;
+    float scale;
+};
+hipError_t launch_kv_decode(const KvProblem &p, hipStream_t s);
+
+// fd_kv_prefill_kernels.hip
+struct KvPromptProblem {
+    KvPool pool;
+    const uint16_t *q;                             // [n_tokens, Hq, 128], token stride of its own
+    long long q_stride;
+    const int32_t *starts, *seq_lens, *table;      // starts [B + 1]
+    uint16_t *out;                                 // [n_tokens, Hq, 128]
+    int B, Hq, G, n_tokens, Smax, width;
+    float scale;
+};
+hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s);
 
 // Splits of a row between workgroups, joined by a launch of its own: out = sum_c 2^{m_c - M} num_c / sum_c 2^{m_c - M} l_c over the
 // chunks that hold a key, of rows with two or more of them.  rows: [B, H] output rows of `dim` elements.

@@ -59,20 +59,26 @@ fd_status nibble_pool(const fd_nibble_pool *pool, fd::NibblePool *out)
     return FD_OK;
 }
 
-fd_status nibble_rows(const fd_nibble_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
-                   const int32_t *slot_map, fd::NibblePool *P, fd::NibbleRows *R)
+// K and V rows of a call's tokens, as the caller has them.
+fd_status token_rows(int Hkv, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens, const int32_t *slot_map,
+                     fd::TokenRows *R)
 {
-    const fd_status st = nibble_pool(pool, P);
-    if (st != FD_OK) return st;
     if (!k || !v || !slot_map) return FD_ERR_NULL;
-    const long long width = (long long)P->Hkv * fd::kHeadDim;
+    const long long width = (long long)Hkv * fd::kHeadDim;
     if (n_tokens < 0 || off(k, 16) || off(v, 16) || off(slot_map, 4) || k_stride < width || v_stride < width || k_stride % 8 != 0 ||
         v_stride % 8 != 0)
         return FD_ERR_SHAPE;
-    if ((long long)n_tokens * 2 * P->Hkv >= kMostThreads / 16) return FD_ERR_UNSUPPORTED;
-    *R = fd::NibbleRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)),
+    if ((long long)n_tokens * 2 * Hkv >= kMostThreads / 16) return FD_ERR_UNSUPPORTED;
+    *R = fd::TokenRows{const_cast<uint16_t *>(static_cast<const uint16_t *>(k)),
                         const_cast<uint16_t *>(static_cast<const uint16_t *>(v)), k_stride, v_stride, slot_map, n_tokens};
     return FD_OK;
+}
+fd_status nibble_rows(const fd_nibble_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
+                   const int32_t *slot_map, fd::NibblePool *P, fd::TokenRows *R)
+{
+    const fd_status st = nibble_pool(pool, P);
+    if (st != FD_OK) return st;
+    return token_rows(P->Hkv, k, k_stride, v, v_stride, n_tokens, slot_map, R);
 }
 
 fd_status latent_pool(const fd_latent_pool *pool, fd::LatentPool *out)
@@ -88,6 +94,37 @@ fd_status latent_pool(const fd_latent_pool *pool, fd::LatentPool *out)
     o.dtype = pool->dtype;
     *out = o;
     return FD_OK;
+}
+
+fd_status kv_pool(const fd_kv_pool *pool, fd::KvPool *out)
+{
+    if (!pool || !pool->k || !pool->v) return FD_ERR_NULL;
+    const bool coded = pool->store == FD_E4M3;
+    if (coded && (!pool->k_scales || !pool->v_scales)) return FD_ERR_NULL;
+    fd::KvPool o{};
+    const fd_status st = check_pages(pool->n_pages, pool->page_size, &o.page_shift);
+    if (st != FD_OK) return st;
+    if (pool->n_kv_heads < 1 || pool->head_dim < 1) return FD_ERR_SHAPE;
+    if (off(pool->k, 16) || off(pool->v, 16) || (coded && (off(pool->k_scales, 16) || off(pool->v_scales, 16)))) return FD_ERR_SHAPE;
+    if (pool->head_dim != fd::kHeadDim || pool->n_kv_heads > 65535 || !known_type(pool->dtype) || (!coded && pool->store != pool->dtype))
+        return FD_ERR_UNSUPPORTED;
+    o.k = static_cast<unsigned char *>(pool->k);
+    o.v = static_cast<unsigned char *>(pool->v);
+    o.k_scales = static_cast<uint8_t *>(pool->k_scales);
+    o.v_scales = static_cast<uint8_t *>(pool->v_scales);
+    o.n_pages = pool->n_pages;
+    o.Hkv = pool->n_kv_heads;
+    o.store = pool->store;
+    o.dtype = pool->dtype;
+    *out = o;
+    return FD_OK;
+}
+fd_status kv_rows(const fd_kv_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
+                  const int32_t *slot_map, fd::KvPool *P, fd::TokenRows *R)
+{
+    const fd_status st = kv_pool(pool, P);
+    if (st != FD_OK) return st;
+    return token_rows(P->Hkv, k, k_stride, v, v_stride, n_tokens, slot_map, R);
 }
 
 // A row is cut into chunks, one workgroup each, whose sums meet in the workspace.  It begins with arrival counters, a fixed
@@ -129,6 +166,26 @@ fd_status latent_split(const fd_shape *sh, Split *S)
     const fd_status st = split(sh, fd::kLatentRow, fd::kLatent, 64, S);
     if (st != FD_OK) return st;
     return sh->n_kv_heads == 1 ? FD_OK : FD_ERR_UNSUPPORTED;
+}
+
+fd_status kv_split(const fd_shape *sh, Split *S) { return split(sh, fd::kHeadDim, fd::kHeadDim, 64, S); }
+
+// The packed prompts: tiles of 128 (token, query head) rows of a KV head, of which no sequence leaves more than one unfilled.
+fd_status prompt_split(const fd_shape *sh, int32_t n_tokens, Split *S)
+{
+    const fd_status st = check_shape(sh, fd::kHeadDim);
+    if (st != FD_OK) return st;
+    if (sh->chunk <= 0 || n_tokens < 0) return FD_ERR_SHAPE;
+    if (sh->chunk % 64 != 0) return FD_ERR_UNSUPPORTED;
+    const long long units = ((long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch) * sh->n_kv_heads;
+    S->rows = (long long)n_tokens * sh->n_q_heads;
+    S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
+    if (units > kMostThreads / 512 || units * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
+    const size_t slots = S->nc == 1 ? 0 : (size_t)(S->rows * S->nc);
+    S->num = align_up(kCounters * sizeof(int32_t));
+    S->ml = align_up(S->num + slots * fd::kHeadDim * sizeof(float));
+    S->total = align_up(S->ml + slots * sizeof(float2));
+    return FD_OK;
 }
 
 // Keys of a chunk, a multiple of `unit`, so that `units` rows of max_seq keys make about `want` workgroups of at least
@@ -183,7 +240,7 @@ fd_status fd_nibble_write(const fd_nibble_pool *pool, const void *k, int64_t k_s
                        const int32_t *slot_map, void *stream)
 {
     fd::NibblePool P;
-    fd::NibbleRows R;
+    fd::TokenRows R;
     const fd_status st = nibble_rows(pool, k, k_stride, v, v_stride, n_tokens, slot_map, &P, &R);
     if (st != FD_OK) return st;
     if (n_tokens == 0) return FD_OK;
@@ -195,7 +252,7 @@ fd_status fd_nibble_read(const fd_nibble_pool *pool, const int32_t *slot_map, in
                       int64_t v_stride, void *stream)
 {
     fd::NibblePool P;
-    fd::NibbleRows R;
+    fd::TokenRows R;
     const fd_status st = nibble_rows(pool, k, k_stride, v, v_stride, n_tokens, slot_map, &P, &R);
     if (st != FD_OK) return st;
     if (n_tokens == 0) return FD_OK;
@@ -356,6 +413,110 @@ fd_status fd_latent_prefill_attn(const fd_shape *shape, int32_t dtype, const voi
     p.B = shape->batch; p.H = shape->n_q_heads; p.Smax = shape->max_seq; p.dtype = dtype;
     p.scale = shape->scale;
     FD_TRY(fd::launch_latent_prefill(p, static_cast<hipStream_t>(stream)));
+    return FD_OK;
+}
+
+fd_status fd_kv_write(const fd_kv_pool *pool, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t n_tokens,
+                      const int32_t *slot_map, void *stream)
+{
+    fd::KvPool P;
+    fd::TokenRows R;
+    const fd_status st = kv_rows(pool, k, k_stride, v, v_stride, n_tokens, slot_map, &P, &R);
+    if (st != FD_OK) return st;
+    if (n_tokens == 0) return FD_OK;
+    FD_TRY(fd::launch_kv_write(P, R, static_cast<hipStream_t>(stream)));
+    return FD_OK;
+}
+
+fd_status fd_kv_read(const fd_kv_pool *pool, const int32_t *slot_map, int32_t n_tokens, void *k, int64_t k_stride, void *v,
+                     int64_t v_stride, void *stream)
+{
+    fd::KvPool P;
+    fd::TokenRows R;
+    const fd_status st = kv_rows(pool, k, k_stride, v, v_stride, n_tokens, slot_map, &P, &R);
+    if (st != FD_OK) return st;
+    if (n_tokens == 0) return FD_OK;
+    FD_TRY(fd::launch_kv_read(P, R, static_cast<hipStream_t>(stream)));
+    return FD_OK;
+}
+
+size_t fd_kv_workspace_bytes(const fd_shape *shape)
+{
+    Split S;
+    return kv_split(shape, &S) == FD_OK ? S.total : 0;
+}
+
+int32_t fd_kv_pick_chunk(const fd_shape *shape)
+{
+    return fd_nibble_pick_chunk(shape);
+}
+
+fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, const int32_t *block_table, const int32_t *seq_lens,
+                            void *out, fd_workspace ws, void *stream)
+{
+    Split S;
+    fd_status st = kv_split(shape, &S);
+    if (st != FD_OK) return st;
+    fd::KvProblem p{};
+    st = kv_pool(pool, &p.pool);
+    if (st != FD_OK) return st;
+    if (!q || !block_table || !seq_lens || !out) return FD_ERR_NULL;
+    if (off(q, 16) || off(out, 16) || off(block_table, 4) || off(seq_lens, 4)) return FD_ERR_SHAPE;
+    if (pool->n_kv_heads != shape->n_kv_heads || shape->max_seq % pool->page_size != 0) return FD_ERR_SHAPE;
+    if (bad_ws(ws, S)) return FD_ERR_WORKSPACE;
+    if (shape->batch == 0) return FD_OK;
+    p.q = static_cast<const uint16_t *>(q);
+    p.seq_lens = seq_lens;
+    p.table = block_table;
+    p.out = static_cast<uint16_t *>(out);
+    p.num = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + S.num);
+    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.ml);
+    p.B = shape->batch; p.Hq = shape->n_q_heads; p.G = shape->n_q_heads / shape->n_kv_heads; p.tiles = (p.G + 15) / 16;
+    if ((long long)p.B * shape->n_kv_heads * p.tiles <= kCounters) p.counters = static_cast<int32_t *>(ws.ptr);
+    p.C = shape->chunk; p.nc = (int)S.nc; p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
+    p.scale = shape->scale;
+    FD_TRY(fd::launch_kv_decode(p, static_cast<hipStream_t>(stream)));
+    return FD_OK;
+}
+
+size_t fd_kv_prefill_workspace_bytes(const fd_shape *shape, int32_t n_tokens)
+{
+    Split S;
+    return prompt_split(shape, n_tokens, &S) == FD_OK ? S.total : 0;
+}
+
+int32_t fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens)
+{
+    if (check_shape(shape, fd::kHeadDim) != FD_OK || n_tokens < 0) return 0;
+    return (shape->max_seq + 63) / 64 * 64;
+}
+
+fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, int64_t q_stride, int32_t n_tokens,
+                             const int32_t *token_starts, const int32_t *block_table, const int32_t *seq_lens, void *out, fd_workspace ws,
+                             void *stream)
+{
+    Split S;
+    fd_status st = prompt_split(shape, n_tokens, &S);
+    if (st != FD_OK) return st;
+    fd::KvPromptProblem p{};
+    st = kv_pool(pool, &p.pool);
+    if (st != FD_OK) return st;
+    if (!q || !token_starts || !block_table || !seq_lens || !out) return FD_ERR_NULL;
+    if (off(q, 16) || off(out, 16) || off(token_starts, 4) || off(block_table, 4) || off(seq_lens, 4)) return FD_ERR_SHAPE;
+    if (q_stride < (int64_t)shape->n_q_heads * fd::kHeadDim || q_stride % 8 != 0) return FD_ERR_SHAPE;
+    if (pool->n_kv_heads != shape->n_kv_heads || shape->max_seq % pool->page_size != 0) return FD_ERR_SHAPE;
+    if (bad_ws(ws, S)) return FD_ERR_WORKSPACE;
+    if (shape->batch == 0 || n_tokens == 0) return FD_OK;
+    p.q = static_cast<const uint16_t *>(q);
+    p.q_stride = q_stride;
+    p.starts = token_starts;
+    p.seq_lens = seq_lens;
+    p.table = block_table;
+    p.out = static_cast<uint16_t *>(out);
+    p.B = shape->batch; p.Hq = shape->n_q_heads; p.G = shape->n_q_heads / shape->n_kv_heads; p.n_tokens = n_tokens;
+    p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
+    p.scale = shape->scale;
+    FD_TRY(fd::launch_kv_prefill(p, static_cast<hipStream_t>(stream)));
     return FD_OK;
 }
 

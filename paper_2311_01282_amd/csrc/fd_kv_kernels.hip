@@ -1,0 +1,332 @@
+// The paged cache of 16 or 8 bits: rows into it, rows out of it, and decode attention over it.
+//
+// In 8 bits a row (128 elements of a token and KV head) is c_d 2^e: e the smallest whole number with max |x| <= 448 2^e, c_d
+// e4m3.  The scale is a power of two, so that a value is a number of the type (four significant bits) and needs no rounding
+// on the way back; what an arbitrary scale could gain, less than a factor of two of the range, is not precision: e4m3 has that down
+// to 2^-6 of its 448.
+#include "fd_kv.h"
+
+namespace fd {
+
+namespace {
+
+// ---- rows in and out ----
+// A row is read, coded and written within eight lanes: 16 elements a lane, from 8 j and from 64 + 8 j, so that eight lanes' loads
+// and stores lie side by side.
+
+struct KvPlace {
+    size_t row;                 // of the pool: (page, head, token in page)
+    int token, head;
+    bool is_v, live;
+};
+
+// Row r of the call: K and V rows of a token's heads, one after the other.  (32 bits: a division of 64 is a hundred instructions.)
+__device__ __forceinline__ KvPlace kv_place(const KvPool &pool, const TokenRows &rows, unsigned r)
+{
+    KvPlace at;
+    const unsigned per = 2 * pool.Hkv, token = r / per, rest = r - token * per;
+    at.is_v = rest >= (unsigned)pool.Hkv;
+    at.head = at.is_v ? rest - pool.Hkv : rest;
+    at.token = (int)token;
+    at.live = token < (unsigned)rows.n_tokens;
+    const int slot = at.live ? rows.slots[token] : -1;
+    at.live = slot >= 0 && (slot >> pool.page_shift) < pool.n_pages;         // anything else: padding, left alone
+    const int page = at.live ? slot >> pool.page_shift : 0;
+    at.row = (((size_t)page * pool.Hkv + at.head) << pool.page_shift) + (at.live ? slot & ((1 << pool.page_shift) - 1) : 0);
+    return at;
+}
+
+__device__ __forceinline__ unsigned lanes8_max(unsigned x)
+{
+    auto swap = [](unsigned y, auto control) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)y, decltype(control)::value, 0xf, 0xf, true); };
+    x = max(x, swap(x, std::integral_constant<int, 0xB1>{}));
+    x = max(x, swap(x, std::integral_constant<int, 0x4E>{}));
+    return max(x, swap(x, std::integral_constant<int, 0x141>{}));
+}
+
+template <class T, bool k8> __global__ __launch_bounds__(256) void kv_write_kernel(KvPool pool, TokenRows rows)
+{
+    const KvPlace at = kv_place(pool, rows, blockIdx.x * 32 + (threadIdx.x >> 3));
+    const int j = threadIdx.x & 7;
+    if (!at.live) return;                                                   // (whole rows of 8 lanes)
+    const uint16_t *token = at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride;
+    const u32x4_t *src = reinterpret_cast<const u32x4_t *>(token + at.head * kHeadDim) + j;
+    const u32x4_t x[2] = {src[0], src[8]};
+    unsigned char *to = at.is_v ? pool.v : pool.k;
+    if constexpr (!k8) {
+        u32x4_t *dst = reinterpret_cast<u32x4_t *>(to + at.row * (2 * kHeadDim)) + j;
+        dst[0] = x[0];
+        dst[8] = x[1];
+    } else {
+        // The largest magnitude, as bits of the type: infinity and NaN are the largest of all.
+        unsigned top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned w = x[i >> 2][i & 3] & 0x7fff7fffu;
+            top = max(top, max(w & 0xffffu, w >> 16));
+        }
+        top = lanes8_max(top);
+        const bool odd = top >= T::kInfinity;
+        // max <= 1.75 2^8 2^e: the exponent of max, less 8, one more where its mantissa is above 1.75
+        const int e = max((int)((__builtin_bit_cast(unsigned, T::lo(top)) + 0x1fffffu) >> 23) - 127 - 8, kLowestExponent);
+        const float by = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+        // (exact, or below what any code stands for)  Where 256 2^e is beyond the type the largest code is 240.
+        const float most = e >= T::kLastExponent ? 240.f : 448.f;
+        unsigned *codes = reinterpret_cast<unsigned *>(to + at.row * kHeadDim) + 2 * j;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            unsigned c[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned w0 = x[h][2 * i], w1 = x[h][2 * i + 1];
+                auto in = [&](float f) { return __builtin_amdgcn_fmed3f(f * by, -most, most); };
+                int y = __builtin_amdgcn_cvt_pk_fp8_f32(in(T::lo(w0)), in(T::hi(w0)), 0, false);
+                y = __builtin_amdgcn_cvt_pk_fp8_f32(in(T::lo(w1)), in(T::hi(w1)), y, true);
+                c[i] = odd ? 0x7f7f7f7fu : (unsigned)y;                     // NaN
+            }
+            *reinterpret_cast<u32x2_t *>(codes + 16 * h) = u32x2_t{c[0], c[1]};
+        }
+        if (j == 0) (at.is_v ? pool.v_scales : pool.k_scales)[at.row] = odd ? 255 : (uint8_t)(e + 127);
+    }
+}
+
+template <class T, bool k8> __global__ __launch_bounds__(256) void kv_read_kernel(KvPool pool, TokenRows rows)
+{
+    const KvPlace at = kv_place(pool, rows, blockIdx.x * 32 + (threadIdx.x >> 3));
+    const int j = threadIdx.x & 7;
+    if (!at.live) return;
+    const unsigned char *from = at.is_v ? pool.v : pool.k;
+    uint16_t *token = at.is_v ? rows.v + at.token * rows.v_stride : rows.k + at.token * rows.k_stride;
+    u32x4_t *dst = reinterpret_cast<u32x4_t *>(token + at.head * kHeadDim) + j;
+    u32x4_t x[2];
+    if constexpr (k8) {
+        const float s = scale_of((at.is_v ? pool.v_scales : pool.k_scales)[at.row]);
+        const u32x2_t *codes = reinterpret_cast<const u32x2_t *>(from + at.row * kHeadDim) + j;
+        const u32x2_t c[2] = {codes[0], codes[8]};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[h] = from_codes<T>(c[h][0], c[h][1], s);
+    } else {
+        const u32x4_t *src = reinterpret_cast<const u32x4_t *>(from + at.row * (2 * kHeadDim)) + j;
+        x[0] = src[0];
+        x[1] = src[8];
+    }
+    __builtin_nontemporal_store(x[0], dst);
+    __builtin_nontemporal_store(x[1], dst + 8);
+}
+
+// ---- decode attention ----
+// A workgroup takes a chunk of a sequence's keys for up to 16 query heads that share a KV head, a wavefront every fourth block of
+// it; nothing of the cache passes through LDS.  The wavefronts' sums are joined at the end, those of chunks by the
+// workgroup that arrives last or by a launch of its own.
+constexpr int kBlock = 32;
+constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
+constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
+constexpr int kSumRow = kHeadDim + 4;            // (rows start in different banks)
+
+struct DecodeLds {
+    alignas(16) float rows[4][16][kSumRow];
+    float m[4][16], l[4][16];
+    int last;
+};
+
+template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_kernel(KvProblem p)
+{
+    __shared__ DecodeLds lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const int chunk = blockIdx.x % p.nc, group = blockIdx.x / p.nc;
+    int unit = group;
+    const int tile = unit % p.tiles;
+    unit /= p.tiles;
+    const int hkv = unit % p.pool.Hkv, b = unit / p.pool.Hkv;
+    const int start = chunk * p.C;
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)b * p.width);
+    const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
+    const int end = min(len, start + p.C);
+    const int heads = min(p.G - 16 * tile, 16), head0 = hkv * p.G + 16 * tile;      // query heads of this tile
+    if (start >= end) {
+        // a sequence without keys: zero rows, by the first chunk (other chunks without keys leave nothing)
+        if (chunk == 0)
+            for (int i = tid; i < heads * kHeadDim / 2; i += 256)
+                reinterpret_cast<unsigned *>(p.out + ((size_t)b * p.Hq + head0) * kHeadDim)[i] = 0u;
+        return;
+    }
+    const int last = end - 1;
+    Keys<T, k8> keys;
+    Values<T, k8> values;
+    BlockPages pages;
+    int key0 = start + kBlock * wave;
+    if (key0 < end) {
+        pages = block_pages(table, p.pool.page_shift, key0, last);
+        const BlockRows at = block_rows(p.pool, hkv, pages, key0, last);
+        keys.load(p.pool, at, lane);
+        values.load(p.pool, at, lane);
+        pages = block_pages(table, p.pool.page_shift, key0 + 4 * kBlock, last);
+    }
+    u32x4_t q[4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+        q[kb] = u32x4_t{0u, 0u, 0u, 0u};
+        if (n < heads)
+            q[kb] = *reinterpret_cast<const u32x4_t *>(p.q + ((size_t)b * p.Hq + head0 + n) * kHeadDim + Keys<T, k8>::element(kb, g));
+    }
+    const float c1 = p.scale * kLog2e;
+    Softmax<T> state;
+    state.clear();
+    for (; key0 < end; key0 += 4 * kBlock) {
+        const int next = key0 + 4 * kBlock;
+        f32x4_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) s[t] = T::mfma(keys.operand(t, kb, lane), q[kb], s[t]);
+        }
+        BlockRows at;
+        if (next < end) {
+            at = block_rows(p.pool, hkv, pages, next, last);
+            keys.load(p.pool, at, lane);
+        }
+        float z[8];
+        const int live = end - key0 - 8 * g;                   // keys from 8 g on
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3] * c1;
+        if (key0 + kBlock > end) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = j < live ? z[j] : -INFINITY;
+            values.keep(live);
+        }
+        u32x4_t a[8];
+        values.operands(a);
+        if (next < end) {
+            values.load(p.pool, at, lane);
+            pages = block_pages(table, p.pool.page_shift, next + 4 * kBlock, last);
+        }
+        // (no code of 8 bits is infinite, and NaN stay what they are)
+        state.block(z, a, !k8 && any_not_finite<T>(a));
+    }
+
+    // the four wavefronts' sums
+    {
+        float l = rows_sum(state.sum, state.sum);
+        l = halves_sum(l, l);
+        if (n < heads) {
+            if (g == 0) {
+                lds.m[wave][n] = state.ref;
+                lds.l[wave][n] = l;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<f32x4_t *>(&lds.rows[wave][n][32 * g + 8 * r + 4 * h]) =
+                        f32x4_t{state.acc[4 * h][r], state.acc[4 * h + 1][r], state.acc[4 * h + 2][r], state.acc[4 * h + 3][r]};
+        }
+    }
+    __syncthreads();
+    const int chunks = (len + p.C - 1) / p.C;                              // of this sequence
+    for (int h = wave; h < heads; h += 4) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.m[w][h]);
+        float a0 = 0.f, a1 = 0.f, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = lds.m[w][h];
+            // a wavefront without keys has m = -inf and zeros; one whose logits are all -inf or NaN has NaN, and keeps it
+            const float f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top);
+            const float2 x = *reinterpret_cast<const float2 *>(&lds.rows[w][h][2 * lane]);
+            a0 = __builtin_fmaf(x.x, f, a0);
+            a1 = __builtin_fmaf(x.y, f, a1);
+            sum = __builtin_fmaf(lds.l[w][h], f, sum);
+        }
+        const size_t out_row = (size_t)b * p.Hq + head0 + h;
+        if (chunks == 1) {
+            const float inv = 1.f / sum;
+            reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
+        } else {
+            const size_t slot = out_row * p.nc + chunk;
+            float *num = p.num + slot * kHeadDim + 2 * lane, *ml = reinterpret_cast<float *>(p.ml + slot);
+            // past the caches: a workgroup on another XCD may join the row
+            if (p.counters) {
+                store_coherent2(num, a0, a1);
+                if (lane == 0) store_coherent2(ml, top, sum);
+            } else {
+                *reinterpret_cast<float2 *>(num) = float2{a0, a1};
+                if (lane == 0) *reinterpret_cast<float2 *>(ml) = float2{top, sum};
+            }
+        }
+    }
+    if (!p.counters || chunks == 1) return;
+    // The workgroup of the group's last chunk to arrive joins its rows: a round trip to memory for the stores, one for the
+    // counter, one for the partial results.
+    wait_stores_performed();
+    __syncthreads();
+    if (tid == 0) {
+        const int arrived = __hip_atomic_fetch_add(p.counters + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lds.last = arrived == chunks - 1;
+        if (arrived == chunks - 1) store_coherent(p.counters + group, 0);          // ready for the next call
+    }
+    __syncthreads();
+    if (!lds.last) return;
+    for (int h = wave; h < heads; h += 4) {
+        const size_t out_row = (size_t)b * p.Hq + head0 + h, slot = out_row * p.nc;
+        // chunk i's reference and denominator in lane i of every 16; all partial vectors under way before the first is used
+        unsigned long long x[kJoinInPlace];
+        const unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + min(n, chunks - 1)));
+#pragma unroll
+        for (int i = 0; i < kJoinInPlace; ++i)
+            x[i] = load_coherent(reinterpret_cast<const unsigned long long *>(p.num + (slot + min(i, chunks - 1)) * kHeadDim) + lane);
+        const float mi = n < chunks ? as_f32((unsigned)s) : -INFINITY, top = row16_max(mi);
+        const float f = n >= chunks ? 0.f : mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+        const float sum = row16_sum(n < chunks ? as_f32((unsigned)(s >> 32)) * f : 0.f);
+        float a0 = 0.f, a1 = 0.f;
+        each16(std::make_integer_sequence<int, kJoinInPlace>{}, [&](auto of) {
+            constexpr int i = decltype(of)::value;
+            if (i < chunks) {
+                const float fi = row16_lane<i>(f);
+                a0 = __builtin_fmaf(as_f32((unsigned)x[i]), fi, a0);
+                a1 = __builtin_fmaf(as_f32((unsigned)(x[i] >> 32)), fi, a1);
+            }
+        });
+        const float inv = 1.f / sum;
+        reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
+    }
+}
+
+template <class F> auto by_type(const KvPool &pool, F f)
+{
+    const std::true_type yes;
+    const std::false_type no;
+    if (pool.store == kE4m3) return pool.dtype == kF16 ? f(F16{}, yes) : f(BF16{}, yes);
+    return pool.dtype == kF16 ? f(F16{}, no) : f(BF16{}, no);
+}
+dim3 rows_grid(const KvPool &pool, const TokenRows &rows) { return dim3((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32)); }
+
+}  // namespace
+
+hipError_t launch_kv_write(const KvPool &pool, const TokenRows &rows, hipStream_t s)
+{
+    return by_type(pool, [&](auto type, auto k8) {
+        return launch(kv_write_kernel<decltype(type), decltype(k8)::value>, rows_grid(pool, rows), dim3(256), s, pool, rows);
+    });
+}
+hipError_t launch_kv_read(const KvPool &pool, const TokenRows &rows, hipStream_t s)
+{
+    return by_type(pool, [&](auto type, auto k8) {
+        return launch(kv_read_kernel<decltype(type), decltype(k8)::value>, rows_grid(pool, rows), dim3(256), s, pool, rows);
+    });
+}
+hipError_t launch_kv_decode(const KvProblem &p_, hipStream_t s)
+{
+    KvProblem p = p_;
+    const long long workgroups = (long long)p.B * p.pool.Hkv * p.tiles * p.nc;
+    if (p.nc > kJoinInPlace || workgroups > kJoinWorkgroups) p.counters = nullptr;
+    const hipError_t e = by_type(p.pool, [&](auto type, auto k8) {
+        return launch(kv_decode_kernel<decltype(type), decltype(k8)::value>, dim3((unsigned)workgroups), dim3(256), s, p);
+    });
+    if (e != hipSuccess || p.nc == 1 || p.counters) return e;
+    JoinProblem j{p.num, p.ml, p.seq_lens, p.out, p.B * p.Hq, p.Hq, p.C, p.nc, p.Smax, kHeadDim, p.pool.dtype};
+    return launch_join(j, s);
+}
+
+}  // namespace fd

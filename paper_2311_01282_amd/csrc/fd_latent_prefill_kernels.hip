@@ -17,7 +17,7 @@
 
 #include "fd_chunk.h"
 #include "fd_cache.h"
-#include "fd_types.h"
+#include "fd_finite.h"
 
 namespace fd {
 
@@ -71,41 +71,6 @@ __device__ __forceinline__ u32x4_t window(const void *base, long long bytes)
     return u32x4_t{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at),
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
-}
-
-// Values that are not finite: counted in a product of their own, in which an infinite one is 1, one of the other sign 64
-// and a NaN 4096 (of 32 keys the counts do not meet).
-template <class T> __device__ __forceinline__ u32x4_t not_finite(u32x4_t v)
-{
-    u32x4_t x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float f[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const unsigned h = v[i] >> (16 * k) & 0xffffu, size = h & 0x7fffu;
-            f[k] = size < T::kInfinity ? 0.f : size > T::kInfinity ? 4096.f : h == size ? 1.f : 64.f;
-        }
-        x[i] = T::pack(f[0], f[1]);
-    }
-    return x;
-}
-template <class T> __device__ __forceinline__ u32x4_t finite(u32x4_t v)          // 0 in their place
-{
-    u32x4_t x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned low = (v[i] & 0x7fffu) < T::kInfinity ? v[i] & 0xffffu : 0u;
-        const unsigned high = (v[i] >> 16 & 0x7fffu) < T::kInfinity ? v[i] & 0xffff0000u : 0u;
-        x[i] = low | high;
-    }
-    return x;
-}
-// What counts stand for as a summand.
-__device__ __forceinline__ float summand(float counts)
-{
-    const unsigned n = (unsigned)counts;
-    return (n >= 4096 ? __builtin_nanf("") : 0.f) + (n & 63 ? INFINITY : 0.f) - (n & 4032 ? INFINITY : 0.f);
 }
 
 template <class T, int kHalves> __global__ __launch_bounds__(256 * kHalves, 2) void latent_prefill_kernel(LatentPromptProblem p)

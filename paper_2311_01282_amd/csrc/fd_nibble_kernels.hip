@@ -50,7 +50,7 @@ __device__ __forceinline__ RowPlace row_place(const NibblePool &pool, const int3
     return at;
 }
 
-template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(NibblePool pool, NibbleRows rows)
+template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(NibblePool pool, TokenRows rows)
 {
     const unsigned row = blockIdx.x * 32 + (threadIdx.x >> 3);
     const int j = threadIdx.x & 7;                                          // 16 elements from 16 j: words 2 j and 2 j + 1
@@ -118,7 +118,7 @@ template <class T> __global__ __launch_bounds__(256) void nibble_write_kernel(Ni
     else if (j % lanes == 1) scales[pool.NG + g] = l_bits;
 }
 
-template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(NibblePool pool, NibbleRows rows)
+template <class T> __global__ __launch_bounds__(256) void nibble_read_kernel(NibblePool pool, TokenRows rows)
 {
     const unsigned row = blockIdx.x * 32 + (threadIdx.x >> 3);
     // elements from 8 j and from 64 + 8 j: stores of eight lanes lie side by side
@@ -730,12 +730,12 @@ template <class T> hipError_t attn_groups(const NibbleProblem &p, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_nibble_write(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
+hipError_t launch_nibble_write(const NibblePool &pool, const TokenRows &rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
     return launch(pool.dtype == kF16 ? nibble_write_kernel<F16> : nibble_write_kernel<BF16>, grid, dim3(256), s, pool, rows);
 }
-hipError_t launch_nibble_read(const NibblePool &pool, const NibbleRows &rows, hipStream_t s)
+hipError_t launch_nibble_read(const NibblePool &pool, const TokenRows &rows, hipStream_t s)
 {
     const dim3 grid((unsigned)(((long long)rows.n_tokens * 2 * pool.Hkv + 31) / 32));
     return launch(pool.dtype == kF16 ? nibble_read_kernel<F16> : nibble_read_kernel<BF16>, grid, dim3(256), s, pool, rows);

@@ -16,6 +16,7 @@ typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 struct F16 {
     static constexpr float kSmallest = 0x1p-14f;           // normal number
     static constexpr unsigned kInfinity = 0x7c00u;         // bits
+    static constexpr int kLastExponent = 8;                // e with 256 2^e beyond the type
     // log2 of a softmax weight at its reference.  Numbers below 2^-25 round to 0.  With a reference of 1 that loses the
     // weights of keys 17.4 and more below the largest logit: of 16384 such keys 5e-4 of the sum.  With 2^7 it loses those
     // below 2^-32 of it, and weights of 2^8 times the reference's are still numbers.
@@ -42,6 +43,7 @@ struct F16 {
 struct BF16 {
     static constexpr float kSmallest = 0x1p-126f;
     static constexpr unsigned kInfinity = 0x7f80u;
+    static constexpr int kLastExponent = 120;
     static constexpr float kLift = 0.f;
     static __device__ __forceinline__ float lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
     static __device__ __forceinline__ float hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }

@@ -20,7 +20,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 FD_OK, FD_ERR_NULL, FD_ERR_SHAPE, FD_ERR_BOUNDS, FD_ERR_WORKSPACE, FD_ERR_UNSUPPORTED, FD_ERR_HIP, FD_ERR_STATIC_LIMIT = range(8)
 FD_STATIC_SCRATCH_BYTES = 8 << 20
-FD_F16, FD_BF16 = range(2)
+FD_F16, FD_BF16, FD_E4M3 = range(3)
 
 
 class Shape(ctypes.Structure):
@@ -53,6 +53,13 @@ class LatentPool(ctypes.Structure):
     """fd_latent_pool"""
     _fields_ = [("rows", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class KvPool(ctypes.Structure):
+    """fd_kv_pool"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("store", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class FdError(RuntimeError):
@@ -120,11 +127,15 @@ def _bind(lib):
     lib.fd_prefill_get_flags.argtypes = [_sp, Workspace, ctypes.POINTER(_vp)]
 
     i32, i64 = ctypes.c_int32, ctypes.c_int64
-    nibble, latent = ctypes.POINTER(NibblePool), ctypes.POINTER(LatentPool)
-    for _name in ("fd_nibble_workspace_bytes", "fd_latent_workspace_bytes"):
+    nibble, latent, kv = ctypes.POINTER(NibblePool), ctypes.POINTER(LatentPool), ctypes.POINTER(KvPool)
+    lib.fd_kv_prefill_workspace_bytes.restype = ctypes.c_size_t
+    lib.fd_kv_prefill_workspace_bytes.argtypes = [_sp, i32]
+    lib.fd_kv_prefill_pick_chunk.restype = i32
+    lib.fd_kv_prefill_pick_chunk.argtypes = [_sp, i32]
+    for _name in ("fd_nibble_workspace_bytes", "fd_latent_workspace_bytes", "fd_kv_workspace_bytes"):
         getattr(lib, _name).restype = ctypes.c_size_t
         getattr(lib, _name).argtypes = [_sp]
-    for _name in ("fd_nibble_pick_chunk", "fd_latent_pick_chunk"):
+    for _name in ("fd_nibble_pick_chunk", "fd_latent_pick_chunk", "fd_kv_pick_chunk"):
         getattr(lib, _name).restype = ctypes.c_int32
         getattr(lib, _name).argtypes = [_sp]
     for _name, _args in (("fd_page_tables", [i32] * 5 + [_vp] * 10),
@@ -134,7 +145,11 @@ def _bind(lib):
                          ("fd_decode_attn_nibble", [_sp, nibble, _vp, _vp, _vp, _vp, Workspace, _vp]),
                          ("fd_latent_write", [latent, _vp, i64, _vp, i64, i32, _vp, _vp]),
                          ("fd_latent_decode_attn", [_sp, latent, _vp, _vp, _vp, _vp, _vp, Workspace, _vp]),
-                         ("fd_latent_prefill_attn", [_sp, i32, _vp, _vp, _vp, i64, _vp, _vp, _vp])):
+                         ("fd_latent_prefill_attn", [_sp, i32, _vp, _vp, _vp, i64, _vp, _vp, _vp]),
+                         ("fd_kv_write", [kv, _vp, i64, _vp, i64, i32, _vp, _vp]),
+                         ("fd_kv_read", [kv, _vp, i32, _vp, i64, _vp, i64, _vp]),
+                         ("fd_kv_decode_attn", [_sp, kv, _vp, _vp, _vp, _vp, Workspace, _vp]),
+                         ("fd_kv_prefill_attn", [_sp, kv, _vp, i64, i32, _vp, _vp, _vp, _vp, Workspace, _vp])):
         getattr(lib, _name).restype = ctypes.c_int
         getattr(lib, _name).argtypes = _args
     return lib
@@ -147,7 +162,8 @@ EXPORTS = ("fd_decode_attn_static", "fd_decode_attn_paged", "fd_decode_attn_page
            "fd_decode_attn_partial", "fd_decode_attn_gqa_partial", "fd_get_flags", "fd_get_partials",
            "fd_status_str", "fd_page_tables", "fd_nibble_write", "fd_nibble_read", "fd_nibble_workspace_bytes", "fd_nibble_pick_chunk",
            "fd_cache_workspace_init", "fd_decode_attn_nibble", "fd_latent_write", "fd_latent_workspace_bytes", "fd_latent_pick_chunk", "fd_latent_decode_attn",
-           "fd_latent_prefill_attn")
+           "fd_latent_prefill_attn", "fd_kv_write", "fd_kv_read", "fd_kv_workspace_bytes", "fd_kv_pick_chunk", "fd_kv_decode_attn",
+           "fd_kv_prefill_workspace_bytes", "fd_kv_prefill_pick_chunk", "fd_kv_prefill_attn")
 
 
 def status_str(status):
@@ -339,3 +355,41 @@ def fd_latent_decode_attn(shape, pool, q_latent, q_rope, block_table, seq_lens, 
 
 def fd_latent_prefill_attn(shape, dtype, q, kv, rope, rope_stride, seq_lens, out, stream=0):
     _check(_lib.fd_latent_prefill_attn(ctypes.byref(shape), int(dtype), q, kv, rope, int(rope_stride), seq_lens, out, stream))
+
+
+def make_kv_pool(k, v, k_scales, v_scales, n_pages, page_size, n_kv_heads, head_dim, store, dtype):
+    """k_scales, v_scales: None unless store is FD_E4M3."""
+    return KvPool(k, v, k_scales, v_scales, int(n_pages), int(page_size), int(n_kv_heads), int(head_dim), int(store), int(dtype))
+
+
+def fd_kv_write(pool, k, k_stride, v, v_stride, n_tokens, slot_map, stream=0):
+    _check(_lib.fd_kv_write(ctypes.byref(pool), k, int(k_stride), v, int(v_stride), int(n_tokens), slot_map, stream))
+
+
+def fd_kv_read(pool, slot_map, n_tokens, k, k_stride, v, v_stride, stream=0):
+    _check(_lib.fd_kv_read(ctypes.byref(pool), slot_map, int(n_tokens), k, int(k_stride), v, int(v_stride), stream))
+
+
+def fd_kv_workspace_bytes(shape):
+    return int(_lib.fd_kv_workspace_bytes(ctypes.byref(shape)))
+
+
+def fd_kv_pick_chunk(shape):
+    return int(_lib.fd_kv_pick_chunk(ctypes.byref(shape)))
+
+
+def fd_kv_decode_attn(shape, pool, q, block_table, seq_lens, out, ws_ptr, ws_bytes, stream=0):
+    _check(_lib.fd_kv_decode_attn(ctypes.byref(shape), ctypes.byref(pool), q, block_table, seq_lens, out, Workspace(ws_ptr, ws_bytes), stream))
+
+
+def fd_kv_prefill_workspace_bytes(shape, n_tokens):
+    return int(_lib.fd_kv_prefill_workspace_bytes(ctypes.byref(shape), int(n_tokens)))
+
+
+def fd_kv_prefill_pick_chunk(shape, n_tokens):
+    return int(_lib.fd_kv_prefill_pick_chunk(ctypes.byref(shape), int(n_tokens)))
+
+
+def fd_kv_prefill_attn(shape, pool, q, q_stride, n_tokens, token_starts, block_table, seq_lens, out, ws_ptr, ws_bytes, stream=0):
+    _check(_lib.fd_kv_prefill_attn(ctypes.byref(shape), ctypes.byref(pool), q, int(q_stride), int(n_tokens), token_starts, block_table, seq_lens,
+                                   out, Workspace(ws_ptr, ws_bytes), stream))

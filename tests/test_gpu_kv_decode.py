@@ -1,0 +1,157 @@
+"""Decode attention over the paged cache of 16 or 8 bits, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests.kv_pool import DEV, TYPES, check, decode, filled, lib, workspace
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / math.sqrt(128)
+BOTH = pytest.mark.parametrize("coded", [True, False], ids=["e4m3", "16"])
+TYPED = pytest.mark.parametrize("dtype", TYPES, ids=["fp16", "bf16"])
+
+
+def check_all(got, pool, lens, q, k, v, scale=SCALE):
+    share = q.shape[1] // pool.hkv
+    got, q = got.cpu(), q.cpu()
+    for b, n in enumerate(lens):
+        if n <= 0:
+            assert (got[b] == 0).all()
+            continue
+        for h in range(pool.hkv):
+            of = slice(h * share, (h + 1) * share)
+            check(got[b, of], pool.dtype, 2, q[b, of], k[b][h], v[b][h], scale, what="sequence %d, KV head %d" % (b, h))
+
+
+def queries(batch, hq, dtype, seed=1, size=1.0):
+    return (size * torch.randn(batch, hq, 128, generator=torch.Generator().manual_seed(seed))).to(dtype).to(DEV)
+
+
+def device(lens, table):
+    return table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV)
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("hq,hkv,page,chunk,max_seq", [
+    (1, 1, 16, 64, 2512), (4, 4, 16, 256, 2512), (8, 2, 32, 1024, 2528), (6, 1, 256, 4096, 2560), (9, 1, 16, 128, 2512), (16, 1, 64, 512, 2560),
+    (28, 4, 128, 0, 2560), (40, 1, 16, 320, 2512), (35, 5, 16, 16384, 2512),
+])
+def test_against_64_bits(dtype, coded, hq, hkv, page, chunk, max_seq):
+    lens = [1, 200, 0, 77, 31, 1024, 2500]
+    pool, table, k, v = filled(dtype, coded, hkv, page, lens, hq + page, max_seq // page)
+    q = queries(len(lens), hq, dtype)
+    table, dlens = device(lens, table)
+    check_all(decode(pool, table, dlens, q, chunk, max_seq, SCALE), pool, lens, q, k, v)
+
+
+@TYPED
+@BOTH
+def test_every_length_around_a_block(dtype, coded):
+    lens = list(range(0, 70)) + [127, 128, 129, 160]
+    pool, table, k, v = filled(dtype, coded, 1, 16, lens, 5, 10)
+    q = queries(len(lens), 3, dtype)
+    table, dlens = device(lens, table)
+    check_all(decode(pool, table, dlens, q, 64, 160, SCALE), pool, lens, q, k, v)
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("scale,size", [(-0.2, 1.0), (0.0, 1.0), (1.0, 3.0), (1e-30, 1.0)])
+def test_scales(dtype, coded, scale, size):
+    lens = [333, 64]
+    pool, table, k, v = filled(dtype, coded, 2, 32, lens, 9, 11, size)
+    q = queries(2, 8, dtype, size=size)
+    table, dlens = device(lens, table)
+    check_all(decode(pool, table, dlens, q, 128, 352, scale), pool, lens, q, k, v, scale)
+
+
+@TYPED
+@BOTH
+def test_first_keys_far_below_and_far_above(dtype, coded):
+    """A running maximum that grows late, one that never does, and thousands of small weights beside a large one."""
+    lens, n = [3000, 3000, 3000], 3000
+
+    def change(b, which, x):
+        if which == 0:
+            x = x * 0.05
+            x[:, n - 1 if b == 0 else 0] = 3.0 if b < 2 else -3.0
+        return x
+    pool, table, k, v = filled(dtype, coded, 1, 64, lens, 11, 47, 1.0, change)
+    q = torch.ones(3, 4, 128, dtype=dtype, device=DEV)
+    table, dlens = device(lens, table)
+    for chunk in (64, 1024, 16384):
+        check_all(decode(pool, table, dlens, q, chunk, 47 * 64, 0.05), pool, lens, q, k, v, 0.05)
+
+
+@TYPED
+@BOTH
+def test_values_that_are_not_finite(dtype, coded):
+    """What is not finite behind a sequence does not matter (the pool is garbage there); within it an infinite value (of 8 bits: the row is NaN)
+    reaches its own head's elements and no other head or sequence."""
+    lens = [100, 90, 33]
+
+    def change(b, which, x):
+        if which and b == 1:
+            x[0, 89, 5] = float("inf")
+        return x
+    pool, table, k, v = filled(dtype, coded, 2, 16, lens, 13, 7, 1.0, change)
+    q = queries(3, 4, dtype)
+    table, dlens = device(lens, table)
+    got = decode(pool, table, dlens, q, 64, 112, SCALE).cpu()
+    odd = got[1, :2].clone()
+    got[1, :2] = 0
+    assert got.isfinite().all()
+    if coded:
+        assert odd.isnan().all()
+    else:
+        assert (odd[:, 5] == float("inf")).all() and odd[:, :5].isfinite().all() and odd[:, 6:].isfinite().all()
+
+
+@TYPED
+@BOTH
+def test_rows_without_a_number_and_infinite_logits(dtype, coded):
+    """NaN in a key is NaN in the output; keys at minus infinity count as nothing."""
+    lens = [70, 130]
+
+    def change(b, which, x):
+        if not which and b == 0:
+            x[0, 40, 3] = float("nan")
+        if not which and b == 1 and not coded:
+            x[:, :100, 0] = float("-inf")
+        return x
+    pool, table, k, v = filled(dtype, coded, 1, 16, lens, 17, 9, 1.0, change)
+    q = queries(2, 2, dtype).abs()
+    table, dlens = device(lens, table)
+    got = decode(pool, table, dlens, q, 64, 144, SCALE).cpu()
+    assert got[0].isnan().all()
+    check(got[1], dtype, 2, q[1].cpu(), k[1][0][0 if coded else 100:], v[1][0][0 if coded else 100:], SCALE)
+
+
+@BOTH
+def test_lengths_beyond_the_table_and_below_zero(coded):
+    dtype, lens = torch.float16, [128, 64]
+    pool, table, k, v = filled(dtype, coded, 1, 16, lens, 19, 8)
+    q = queries(2, 2, dtype)
+    got = decode(pool, table.to(DEV), torch.tensor([1 << 30, -5], dtype=torch.int32, device=DEV), q, 64, 128, SCALE)
+    check_all(got, pool, [128, 0], q, k, v)
+
+
+@TYPED
+@BOTH
+def test_repeats_bit_for_bit_and_leaves_the_pool_alone(dtype, coded):
+    lens = [2000, 900, 1, 0]
+    pool, table, k, v = filled(dtype, coded, 4, 16, lens, 23, 125)
+    q = queries(4, 16, dtype)
+    table, dlens = device(lens, table)
+    before = [x.clone() for x in pool.rows]
+    fd = lib()
+    for chunk in (128, 64, 2048):
+        shape = fd.make_shape(4, 16, 4, 128, 2000, chunk, SCALE)
+        ws = workspace(fd.fd_kv_workspace_bytes(shape))
+        outs = [decode(pool, table, dlens, q, chunk, 2000, SCALE, ws) for _ in range(4)]
+        assert all(torch.equal(outs[0], x) for x in outs[1:])
+        assert (ws[:1 << 14] == 0).all()
+    bits = torch.uint8 if coded else torch.int16
+    assert all(torch.equal(a.view(bits), b.view(bits)) for a, b in zip(before, pool.rows))
