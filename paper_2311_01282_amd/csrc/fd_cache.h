@@ -108,7 +108,9 @@ struct KvPromptProblem {
     long long q_stride;
     const int32_t *starts, *seq_lens, *table;      // starts [B + 1]
     uint16_t *out;                                 // [n_tokens, Hq, 128]
-    int B, Hq, G, n_tokens, Smax, width;
+    float *num;                                    // workspace: [n_tokens, Hq, nc, 128]
+    float2 *ml;                                    // [n_tokens, Hq, nc]
+    int B, Hq, G, n_tokens, tiles, C, nc, Smax, width;      // tiles: of 128 rows of a KV head, at most
     float scale;
 };
 hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s);

@@ -171,13 +171,17 @@ fd_status latent_split(const fd_shape *sh, Split *S)
 fd_status kv_split(const fd_shape *sh, Split *S) { return split(sh, fd::kHeadDim, fd::kHeadDim, 64, S); }
 
 // The packed prompts: tiles of 128 (token, query head) rows of a KV head, of which no sequence leaves more than one unfilled.
+long long prompt_tiles(const fd_shape *sh, int32_t n_tokens)
+{
+    return (long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch;
+}
 fd_status prompt_split(const fd_shape *sh, int32_t n_tokens, Split *S)
 {
     const fd_status st = check_shape(sh, fd::kHeadDim);
     if (st != FD_OK) return st;
     if (sh->chunk <= 0 || n_tokens < 0) return FD_ERR_SHAPE;
-    if (sh->chunk % 64 != 0) return FD_ERR_UNSUPPORTED;
-    const long long units = ((long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch) * sh->n_kv_heads;
+    if (sh->chunk % 64 != 0 || sh->chunk > (1 << 30)) return FD_ERR_UNSUPPORTED;      // (a chunk's end fits 31 bits)
+    const long long units = prompt_tiles(sh, n_tokens) * sh->n_kv_heads;
     S->rows = (long long)n_tokens * sh->n_q_heads;
     S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
     if (units > kMostThreads / 512 || units * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
@@ -513,8 +517,11 @@ fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, cons
     p.seq_lens = seq_lens;
     p.table = block_table;
     p.out = static_cast<uint16_t *>(out);
+    p.num = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + S.num);
+    p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.ml);
     p.B = shape->batch; p.Hq = shape->n_q_heads; p.G = shape->n_q_heads / shape->n_kv_heads; p.n_tokens = n_tokens;
-    p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
+    p.tiles = (int)prompt_tiles(shape, n_tokens);
+    p.C = shape->chunk; p.nc = (int)S.nc; p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
     p.scale = shape->scale;
     FD_TRY(fd::launch_kv_prefill(p, static_cast<hipStream_t>(stream)));
     return FD_OK;

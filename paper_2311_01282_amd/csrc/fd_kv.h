@@ -151,15 +151,15 @@ template <class T, bool k8> struct Values {
 };
 
 // Whether a wavefront's operand holds an infinite value or a NaN.
-template <class T> __device__ __forceinline__ bool any_not_finite(const u32x4_t (&a)[8])
+template <class T, int N> __device__ __forceinline__ bool any_not_finite(const u32x4_t (&a)[N])
 {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     u16x2 top = {0, 0};
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
+    for (int k = 0; k < N; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const unsigned w = a[dt][i] & 0x7fff7fffu;
+            const unsigned w = a[k][i] & 0x7fff7fffu;
             top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
         }
     return __any(max((unsigned)top.x, (unsigned)top.y) >= T::kInfinity);

@@ -3,20 +3,97 @@
 //
 // A row is a (token, query head) pair; the G query heads that share a KV head go together, rows r = G i + j of head j of the
 // sequence's new token i, so that a tile of neighbouring rows reads the same keys whatever G is and however few tokens there are.
-// A wavefront owns 16 rows and walks along the keys in blocks of 32 (fd_kv.h).
+// A workgroup owns a tile of 128 rows, a wavefront 32 of them, and walks along the keys in steps of 32, which pass through LDS.
+// Lanes (32 x 32 x 16): c = lane % 32, h = lane / 32;
+//   scores   S^T[key][row] = K . Q^T: A = the 32 keys of a step in LDS, B = Q^T in registers.  Row 8 j + 4 h + i of the result
+//            is key 16 (j / 2) + 8 h + 4 (j % 2) + i, so that lane (c, h) holds of row c the keys 16 m + 8 h + 0 .. 7: the B
+//            operands m = 0, 1 of
+//   output   O^T[d][row] = V^T . P^T: A = V^T by the transposing LDS read.
+// Softmax with a running maximum per row; the weights are of the type (one rounding, as large as the output's own), their sum
+// is that of the rounded ones, in fp32.
+#include <utility>
+
 #include "fd_kv.h"
 
 namespace fd {
 
 namespace {
 
-constexpr int kTileRows = 64;                    // of a workgroup: four wavefronts
+constexpr int kTileRows = 128, kStep = 32, kRingK = 4, kRingV = 3, kRowBytes = 2 * kHeadDim, kStepBytes = kStep * kRowBytes;
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+template <class T> __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c)
+{
+    if constexpr (std::is_same<T, F16>::value)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// sum += a + b of two numbers of the type
+template <class T> __device__ __forceinline__ float add_pair(unsigned pair, float sum)
+{
+    if constexpr (std::is_same<T, F16>::value)
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pair), __builtin_bit_cast(f16x2_t, 0x3c003c00u), sum, false);
+    else
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), sum, false);
+}
+// the larger of the two halves' values, in both
+__device__ __forceinline__ float halves_max(float a)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, a);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned x = r[0], y = r[1];
+    return fmaxf(as_f32(x), as_f32(y));
+}
+
+// The places of 16-byte piece x of row r of a step's keys, x ^ k_place(r), and of its 32-byte unit x of the values, x ^ v_unit(r):
+// the 16 rows that 16 neighbouring lanes read lie in places of their own, and so do the eight units of the two neighbouring
+// groups of 16 lanes that a transposing read takes at a time, rows 4 i .. 4 i + 3 of two units.
+__device__ __forceinline__ int k_place(int r) { return (r & 3) | ((r >> 3) & 1) << 2 | ((r >> 2) & 1) << 3; }
+__device__ __forceinline__ int v_unit(int r) { return 2 * (r & 3); }
+
+struct PromptLds {
+    alignas(256) unsigned char k[kRingK][kStepBytes];
+    alignas(256) unsigned char v[kRingV][kStepBytes];
+};
+
+__device__ __forceinline__ unsigned lds_address(const void *p)
+{
+    return __builtin_amdgcn_readfirstlane(
+        (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char *)p));
+}
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4_t *lds_u32x4;
+// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+__device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, unsigned lds_1k)
+{
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs) : "memory");
+}
+template <class F, int... I> __device__ __forceinline__ void slots(std::integer_sequence<int, I...>, F f)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N> __device__ __forceinline__ void wait_fetches() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ u32x4_t window(const void *base, int bytes)
+{
+    const unsigned long long at = reinterpret_cast<unsigned long long>(base);
+    return u32x4_t{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)at),
+                   (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(at >> 32)) & 0xffffu,
+                   (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
+}
 
 // The sequence and the place of a tile of the launch: sequences in order, a sequence's tiles from its last to its first.
 struct TilePlace {
     int b, tile, first, tokens;                  // b < 0: there is none; the sequence's first token and their number
 };
-__device__ __forceinline__ int tiles_of(int tokens, int G) { return (int)(((long long)tokens * G + kTileRows - 1) / kTileRows); }
 __device__ __forceinline__ TilePlace find_tile(const KvPromptProblem &p, int at, int lane)
 {
     int before = 0;
@@ -27,7 +104,7 @@ __device__ __forceinline__ TilePlace find_tile(const KvPromptProblem &p, int at,
             first = min(max(p.starts[b], 0), p.n_tokens);
             tokens = max(min(max(p.starts[b + 1], 0), p.n_tokens) - first, 0);
         }
-        const int tiles = tiles_of(tokens, p.G), upto = before + lanes_scan(tiles);
+        const int upto = before + lanes_scan((tokens * p.G + kTileRows - 1) / kTileRows);
         const unsigned long long past = __ballot(upto > at);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -39,79 +116,401 @@ __device__ __forceinline__ TilePlace find_tile(const KvPromptProblem &p, int at,
     return TilePlace{-1, 0, 0, 0};
 }
 
+// A window of memory that loads the compiler knows of go through: 0 behind it.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, int bytes)
+{
+    const unsigned long long at = reinterpret_cast<unsigned long long>(base);
+    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)at), high = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((unsigned long long)high << 32 | low), 0,
+                                             __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
+
 template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill_kernel(KvPromptProblem p)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int hkv = blockIdx.x % p.pool.Hkv;
-    const TilePlace at = find_tile(p, blockIdx.x / p.pool.Hkv, lane);
+    __shared__ PromptLds lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
+    int unit = blockIdx.x;
+    const int hkv = unit % p.pool.Hkv;
+    unit /= p.pool.Hkv;
+    const int chunk = unit / p.tiles;
+    const TilePlace at = find_tile(p, unit % p.tiles, lane);
     if (at.b < 0) return;
-    const int rows = at.tokens * p.G, row0 = at.tile * kTileRows + 16 * wave;       // of the sequence
-    if (row0 >= rows) return;
-    const int len = min(max(p.seq_lens[at.b], 0), p.Smax);
-    const int row = row0 + n, token = row / p.G, head = hkv * p.G + row % p.G;
-    const bool live = row < rows;
-    const int position = len - at.tokens + token;              // below 0: nothing to attend to
-    const int end = min(len, len - at.tokens + (min(row0 + 15, rows - 1)) / p.G + 1);      // keys of the 16 rows
-    const int first_position = len - at.tokens + row0 / p.G;
-    const size_t q_row = (size_t)(at.first + token);
-    u32x4_t q[4];
+    const int rows = at.tokens * p.G, row0 = at.tile * kTileRows + 32 * wave;       // of the sequence
+    const int len = min(max(p.seq_lens[at.b], 0), p.Smax), ahead = len - at.tokens;      // position of new token 0
+    const int begin = chunk * p.C, limit = min(len, begin + p.C);                   // (begin + C < 2^31)
+    auto keys_upto = [&](int row) { return min(ahead + row / p.G + 1, limit) - begin; };      // of the chunk, that a row sees
+    const int tile_keys = keys_upto(min(at.tile * kTileRows + kTileRows, rows) - 1);
+    if (tile_keys <= 0 && chunk > 0) return;
+    const int row = min(row0 + c, rows - 1), token = row / p.G, head = hkv * p.G + row % p.G, position = ahead + token;
+    const bool live = row0 + c < rows;
+    const size_t out_row = (size_t)(at.first + token) * p.Hq + head;
+    uint16_t *out = p.out + out_row * kHeadDim + 4 * h;
+    if (tile_keys <= 0) {                                      // (in the first chunk only) no row of the tile sees a key
+        if (live)
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-        q[kb] = u32x4_t{0u, 0u, 0u, 0u};
-        if (live) q[kb] = *reinterpret_cast<const u32x4_t *>(p.q + q_row * p.q_stride + (size_t)head * kHeadDim + Keys<T, k8>::element(kb, g));
+            for (int i = 0; i < 16; ++i) *reinterpret_cast<u32x2_t *>(out + 8 * i) = u32x2_t{0u, 0u};
+        return;
     }
+    // steps of the workgroup, of the wavefront, and those of it in which every row sees every key
+    const int steps = (tile_keys + kStep - 1) / kStep;
+    const int mine = row0 < rows ? max(keys_upto(min(row0 + 32, rows) - 1) + kStep - 1, 0) / kStep : 0;
+    const int full = row0 < rows ? max(keys_upto(row0), 0) / kStep : 0;
+
+    u32x4_t q[8];
+    {
+        const uint16_t *from = p.q + (size_t)(at.first + token) * p.q_stride + (size_t)head * kHeadDim + 8 * h;
+#pragma unroll
+        for (int kb = 0; kb < 8; ++kb) q[kb] = *reinterpret_cast<const u32x4_t *>(from + 16 * kb);
+    }
+    const unsigned lds_k = lds_address(lds.k[0]), lds_v = lds_address(lds.v[0]);
+
+    // A wavefront fetches rows 8 wave .. + 7 of a step's keys and values, four rows an instruction: they share a page.  Rows
+    // without keys arrive as zeros.
     const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)at.b * p.width);
-    const float c1 = p.scale * kLog2e;
-    Softmax<T> state;
-    state.clear();
-    const int last = end - 1;
-    for (int key0 = 0; key0 < end; key0 += 32) {
-        Keys<T, k8> keys;
-        Values<T, k8> values;
-        const BlockRows rows_at = block_rows(p.pool, hkv, block_pages(table, p.pool.page_shift, key0, last), key0, last);
-        keys.load(p.pool, rows_at, lane);
-        values.load(p.pool, rows_at, lane);
-        f32x4_t s[2];
+    const int key_mine = begin + 8 * wave, last = begin + tile_keys - 1, shift = p.pool.page_shift;
+    auto page_entry = [&](int s) { return table[min(key_mine + kStep * s, last) >> shift]; };
+    auto row_place = [&](int entry, int s) {                   // the row of the pool
+        const int page = min(max(entry, 0), p.pool.n_pages - 1);
+        return (((size_t)page * p.pool.Hkv + hkv) << shift) + ((key_mine + kStep * s) & ((1 << shift) - 1));
+    };
+    auto rows_of = [&](int s) { return min(max(last + 1 - key_mine - kStep * s, 0), 8); };
+    unsigned k_to = 0, v_to = 0;                               // places in the rings
+    auto next_k = [&] { k_to = k_to == kRingK - 1 ? 0 : k_to + 1; };
+    auto next_v = [&] { v_to = v_to == kRingV - 1 ? 0 : v_to + 1; };
+    // 16 bits: straight into LDS, four rows an instruction
+    int koff[2], voff[2];
+    // 8 bits: through registers, 16 codes a lane, and into LDS as numbers of the type
+    u32x4_t codes_k, codes_v;
+    unsigned byte_k, byte_v;
+    if constexpr (!k8) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) s[t] = T::mfma(keys.operand(t, kb, lane), q[kb], s[t]);
+        for (int i = 0; i < 2; ++i) {
+            const int r = 8 * wave + 4 * i + (lane >> 4), x = lane & 15;
+            koff[i] = (4 * i + (lane >> 4)) * kRowBytes + ((x ^ k_place(r)) << 4);
+            voff[i] = (4 * i + (lane >> 4)) * kRowBytes + ((x ^ (v_unit(r) << 1)) << 4);
         }
-        float z[8];
+    } else {
+        const int r = 8 * wave + (lane >> 3), x = 2 * (lane & 7);
+        koff[0] = r * kRowBytes + ((x ^ k_place(r)) << 4);
+        koff[1] = r * kRowBytes + (((x + 1) ^ k_place(r)) << 4);
+        voff[0] = r * kRowBytes + ((x ^ (v_unit(r) << 1)) << 4);
+        voff[1] = voff[0] + 16;
+    }
+    auto fetch_k = [&](size_t place, int n) {
+        if constexpr (!k8) {
+            const u32x4_t r = window(p.pool.k + place * kRowBytes, n * kRowBytes);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = key0 + 8 * g + j <= position ? s[j >> 2][j & 3] * c1 : -INFINITY;
-        if (key0 + 32 > end) values.keep(end - key0 - 8 * g);
-        u32x4_t a[8];
-        values.operands(a);
-        const bool odd = any_not_finite<T>(a);
-        if (odd && key0 + 31 > first_position) {
-            // keys behind a query have the weight 0: what they hold must not reach it, be it infinite
-            u32x4_t seen;
+            for (int i = 0; i < 2; ++i) load_to_lds(r, koff[i], lds_k + k_to * kStepBytes + (2 * wave + i) * 1024);
+            next_k();
+        } else {
+            codes_k = __builtin_amdgcn_raw_buffer_load_b128(buffer(p.pool.k + place * kHeadDim, n * kHeadDim), lane * 16, 0, 0);
+            byte_k = __builtin_amdgcn_raw_buffer_load_b8(buffer(p.pool.k_scales + place, n), lane >> 3, 0, 0);
+        }
+    };
+    auto fetch_v = [&](size_t place, int n) {
+        if constexpr (!k8) {
+            const u32x4_t r = window(p.pool.v + place * kRowBytes, n * kRowBytes);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                seen[i] = T::pack(key0 + 8 * g + 2 * i <= position ? 1.f : 0.f, key0 + 8 * g + 2 * i + 1 <= position ? 1.f : 0.f);
+            for (int i = 0; i < 2; ++i) load_to_lds(r, voff[i], lds_v + v_to * kStepBytes + (2 * wave + i) * 1024);
+            next_v();
+        } else {
+            codes_v = __builtin_amdgcn_raw_buffer_load_b128(buffer(p.pool.v + place * kHeadDim, n * kHeadDim), lane * 16, 0, 0);
+            byte_v = __builtin_amdgcn_raw_buffer_load_b8(buffer(p.pool.v_scales + place, n), lane >> 3, 0, 0);
+        }
+    };
+    auto put_k = [&] {
+        const unsigned at = lds_k + k_to * kStepBytes;
+        const float by = scale_of(byte_k);
+        *(lds_u32x4)(uintptr_t)(at + koff[0]) = from_codes<T>(codes_k[0], codes_k[1], by);
+        *(lds_u32x4)(uintptr_t)(at + koff[1]) = from_codes<T>(codes_k[2], codes_k[3], by);
+        next_k();
+    };
+    auto put_v = [&] {
+        const unsigned at = lds_v + v_to * kStepBytes;
+        const float by = scale_of(byte_v);
+        *(lds_u32x4)(uintptr_t)(at + voff[0]) = from_codes<T>(codes_v[0], codes_v[1], by);
+        *(lds_u32x4)(uintptr_t)(at + voff[1]) = from_codes<T>(codes_v[2], codes_v[3], by);
+        next_v();
+    };
+    // Entering step s, K of s + 2 and V of s are in LDS.  16 bits: the step fetches K of s + 4 and V of s + 2, whose places were
+    // last read in step s - 1 or before.  8 bits: it puts those there, fetched by the step before, and fetches K of s + 5 and
+    // V of s + 3.
+    constexpr int kAhead = k8 ? 1 : 0;
+    size_t place[3];                                           // of steps s + 2 + kAhead .. s + 4 + kAhead
+    int entry;                                                 // of the last of these
+    __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries have arrived: what is counted from here on are fetches
+    {
+        size_t first[4 + kAhead];
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                const f32x4_t counts = T::mfma(not_finite<T>(a[dt]), seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
+        for (int i = 0; i < 4 + kAhead; ++i) first[i] = row_place(page_entry(i), i);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) state.acc[dt][r] += summand(counts[r]);
-                a[dt] = finite<T>(a[dt]);
+        for (int i = 0; i < 4; ++i) {
+            fetch_k(first[i], rows_of(i));
+            if constexpr (k8) put_k();
+            if (i < 2) continue;
+            fetch_v(first[i - 2], rows_of(i - 2));
+            if constexpr (k8) put_v();
+        }
+        if constexpr (k8) {
+            fetch_k(first[4], rows_of(4));
+            fetch_v(first[2], rows_of(2));
+        }
+        place[0] = first[2 + kAhead];
+        place[1] = first[3 + kAhead];
+        entry = page_entry(4 + kAhead);
+    }
+
+    f32x16_t acc[4];
+    float sum = 0.f;                                           // of this lane's rounded weights
+    // The reference of the weights, in units of log2, is T::kLift below the logit it was taken from; it follows the maximum only
+    // where that has grown by kKvSlack.  threshold: what a logit relative to it has to pass; -inf until there is one.
+    constexpr float kMost = kKvSlack + T::kLift;
+    float ref = 0.f, threshold = -INFINITY;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
+    const float c1 = p.scale * kLog2e;
+    const int k_row = (c & 19) | (c & 4) << 1 | (c & 8) >> 1;  // the key whose row of the operand is c
+    const unsigned k_at = k_row * kRowBytes + ((h ^ k_place(k_row)) << 4);
+    const int v_row = 8 * h + ((lane >> 2) & 3);
+    const unsigned v_at = v_row * kRowBytes + ((((lane >> 4) & 1) ^ v_unit(v_row)) << 5) + ((lane & 3) << 3);
+    auto read_k = [&](unsigned kk, int kb) { return *(lds_u32x4)(uintptr_t)(kk ^ (kb << 5)); };
+    auto read_v = [&](unsigned vv, int m, int dt) {
+        const unsigned from = (vv ^ (dt << 6)) + 16 * m * kRowBytes;
+        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)from);
+        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(from + 4 * kRowBytes));
+        return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    f32x16_t zero;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+
+    // Logits z[8 m + i] of keys 16 m + 8 h + i of a step, relative to the reference, and their maximum.
+    float z[16], top = 0.f;
+    unsigned k_next = 1, v_now = 0;
+    u32x4_t first[4];                                          // the first operands of the next step's keys
+    f32x16_t scn;
+    // own: of a step s, key 16 m + 8 h + i is visible to the lane's row where 16 m + i <= own
+    auto own_of = [&](int s) { return position - begin - kStep * s - 8 * h; };
+
+    auto next_places = [&](int s) {
+        place[0] = place[1];
+        place[1] = place[2];
+        entry = page_entry(s + 5 + kAhead);
+    };
+
+    // Step s from its logits, and the scores and logits of step s + 1, which do not depend on it.  Matrix instructions and what
+    // runs under them are woven by hand, 16 slots of one matrix instruction: eight of scores, eight of V^T P^T.
+    auto step = [&](auto with_masks, int s) {
+        constexpr bool kMasks = decltype(with_masks)::value;
+        unsigned kk = lds_k + k_next * kStepBytes + k_at, vv = lds_v + v_now * kStepBytes + v_at;
+        k_next = k_next == kRingK - 1 ? 0 : k_next + 1;
+        v_now = v_now == kRingV - 1 ? 0 : v_now + 1;
+        unsigned k2 = lds_k + k_next * kStepBytes + k_at;
+        asm("" : "+v"(kk), "+v"(vv), "+v"(k2));                // (or addresses of every place are kept in registers of their own)
+        // A row whose logits have all been -inf has no reference yet: any number becomes it.
+        if (__any(top > threshold)) {
+            const bool none = threshold == -INFINITY;
+            float d = none ? top - T::kLift : fmaxf(top - T::kLift, 0.f);
+            d = d == -INFINITY ? 0.f : d;
+            const float f = none ? 1.f : __builtin_amdgcn_exp2f(-d);
+            if (top > -INFINITY) threshold = kMost;
+            ref += d;
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] -= d;
+            if (s > 0)
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) acc[dt] *= f;
+        }
+        u32x4_t a[8], av[2][4], w[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = first[i];
+        auto weight = [&](auto ii) {                           // the i-th, and of every second the pair
+            constexpr int i = decltype(ii)::value;
+            z[i] = __builtin_amdgcn_exp2f(z[i]);
+            if constexpr (i & 1) {
+                w[i >> 3][(i >> 1) & 3] = T::pack(z[i - 1], z[i]);
+                sum = add_pair<T>(w[i >> 3][(i >> 1) & 3], sum);
+            }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        slots(std::make_integer_sequence<int, 8>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            scn = mfma32<T>(a[mm], q[mm], mm == 0 ? zero : scn);
+            if constexpr (mm < 4) a[mm + 4] = read_k(kk, mm + 4);
+            if constexpr (!k8 && mm == 0) fetch_k(place[2], rows_of(s + 4));
+            if constexpr (!k8 && mm == 2) fetch_v(place[0], rows_of(s + 2));
+            av[mm >> 2][mm & 3] = read_v(vv, mm >> 2, mm & 3);
+            weight(std::integral_constant<int, mm>{});
+            if constexpr (mm >= 6) weight(std::integral_constant<int, mm + 2>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // In a step with masks the weights of keys behind a row are 0, and 0 times an infinite value or a NaN is NaN: such values
+        // leave the product, and the rows that see them get them as a summand.
+        if constexpr (kMasks) {
+            if (s >= full && (any_not_finite<T>(av[0]) || any_not_finite<T>(av[1]))) {
+                const int own = own_of(s);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    u32x4_t seen;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) seen[i >> 1] = T::pack(16 * m + i <= own ? 1.f : 0.f, 16 * m + i + 1 <= own ? 1.f : 0.f);
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt) {
+                        const f32x16_t counts = mfma32<T>(not_finite<T>(av[m][dt]), seen, zero);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[dt][r] += summand(counts[r]);
+                        av[m][dt] = finite<T>(av[m][dt]);
+                    }
+                }
             }
         }
-        state.block(z, a, odd);
+        slots(std::make_integer_sequence<int, 4>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            acc[mm] = mfma32<T>(av[0][mm], w[0], acc[mm]);
+            if constexpr (mm < 3) {
+                weight(std::integral_constant<int, 10 + 2 * mm>{});
+                weight(std::integral_constant<int, 11 + 2 * mm>{});
+            }
+            if constexpr (k8 && mm == 2) put_k();
+            if constexpr (k8 && mm == 3) put_v();
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        const int own = kMasks ? own_of(s + 1) : 0;
+        slots(std::make_integer_sequence<int, 4>{}, [&](auto mi) {
+            constexpr int mm = decltype(mi)::value;
+            acc[mm] = mfma32<T>(av[1][mm], w[1], acc[mm]);
+            first[mm] = read_k(k2, mm);
+            if constexpr (k8 && mm == 0) fetch_k(place[2], rows_of(s + 5));
+            if constexpr (k8 && mm == 1) fetch_v(place[0], rows_of(s + 3));
+#pragma unroll
+            for (int i = 4 * mm; i < 4 * mm + 4; ++i) {
+                z[i] = __builtin_fmaf(scn[i], c1, -ref);
+                if constexpr (kMasks) z[i] = i + 8 * (i >> 3) <= own ? z[i] : -INFINITY;
+            }
+            if constexpr (mm == 0) top = fmaxf(fmaxf(z[0], z[1]), z[2]);
+            if constexpr (mm == 1) top = fmaxf(fmaxf(fmaxf(fmaxf(top, z[3]), z[4]), z[5]), z[6]);
+            if constexpr (mm == 2) top = fmaxf(fmaxf(fmaxf(fmaxf(top, z[7]), z[8]), z[9]), z[10]);
+            if constexpr (mm == 3) {
+                top = fmaxf(fmaxf(fmaxf(fmaxf(top, z[11]), z[12]), z[13]), z[14]);
+                top = halves_max(fmaxf(top, z[15]));
+                next_places(s);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    if constexpr (!k8) wait_fetches<8>();                      // K of steps 0 and 1
+    tile_barrier();
+    if (mine > 0) {
+        unsigned kk = lds_k + k_at, k1 = kk + kStepBytes;
+        asm("" : "+v"(kk), "+v"(k1));
+#pragma unroll
+        for (int kb = 0; kb < 8; ++kb) scn = mfma32<T>(read_k(kk, kb), q[kb], kb == 0 ? zero : scn);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) first[kb] = read_k(k1, kb);
+        const int own = own_of(0);
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            z[i] = scn[i] * c1;
+            z[i] = i + 8 * (i >> 3) <= own ? z[i] : -INFINITY;
+            top = fmaxf(top, z[i]);
+        }
+        top = halves_max(top);
     }
-    float sum = rows_sum(state.sum, state.sum);
+    auto enter = [&](int s) {
+        if constexpr (!k8) wait_fetches<4>();                  // K of s + 2 and V of s; what step s - 1 fetched is under way
+        tile_barrier();
+        place[2] = row_place(entry, s + 4 + kAhead);
+    };
+    int s = 0;
+#pragma unroll 1
+    for (; s < full - 1; ++s) {
+        enter(s);
+        step(std::false_type{}, s);
+    }
+#pragma unroll 1
+    for (; s < mine; ++s) {
+        enter(s);
+        step(std::true_type{}, s);
+    }
+    for (; s < steps; ++s) {                                   // the steps that only other wavefronts have
+        enter(s);
+        if constexpr (k8) {
+            put_k();
+            put_v();
+        }
+        fetch_k(place[2], rows_of(s + 4 + kAhead));
+        fetch_v(place[0], rows_of(s + 2 + kAhead));
+        next_places(s);
+    }
+    wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
     sum = halves_sum(sum, sum);
     if (!live) return;
-    const float inv = position >= 0 ? 1.f / sum : 0.f;
-    uint16_t *out = p.out + (q_row * p.Hq + head) * kHeadDim + 32 * g;
+    const int chunks = (position + p.C) / p.C;                 // that hold a key of the row
+    if (chunks <= 1) {
+        if (chunk > 0) return;
+        const bool some = position >= 0;
+        const float inv = 1.f / sum;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        u32x4_t x;
+        for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = position >= 0 ? T::pack(state.acc[2 * i][r] * inv, state.acc[2 * i + 1][r] * inv) : 0u;
-        *reinterpret_cast<u32x4_t *>(out + 8 * r) = x;
+            for (int j = 0; j < 4; ++j) {
+                u32x2_t x = {T::pack(acc[dt][4 * j] * inv, acc[dt][4 * j + 1] * inv), T::pack(acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv)};
+                if (!some) x = u32x2_t{0u, 0u};
+                *reinterpret_cast<u32x2_t *>(out + 32 * dt + 8 * j) = x;
+            }
+    } else if (chunk < chunks) {
+        const size_t slot = out_row * p.nc + chunk;
+        float *num = p.num + slot * kHeadDim + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<f32x4_t *>(num + 32 * dt + 8 * j) = f32x4_t{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+        if (h == 0) p.ml[slot] = float2{threshold == -INFINITY ? -INFINITY : ref, sum};
+    }
+}
+
+// Rows that several workgroups share: out = sum_c 2^{m_c - M} num_c / sum_c 2^{m_c - M} l_c.  A workgroup a token, a wavefront every
+// fourth of its heads.
+template <class T> __global__ __launch_bounds__(256) void kv_prefill_join_kernel(KvPromptProblem p)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = blockIdx.x;
+    // the sequence: the last one that starts at the token or before it and ends behind it
+    int chunks = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int b = b0 + lane;
+        int first = 0, end = 0;
+        if (b < p.B) {
+            first = min(max(p.starts[b], 0), p.n_tokens);
+            end = min(max(p.starts[b + 1], 0), p.n_tokens);
+        }
+        const unsigned long long in = __ballot(first <= token && token < end);
+        if (!in) continue;
+        const int l = 63 - __builtin_clzll(in);
+        const int len = min(max(p.seq_lens[b0 + l], 0), p.Smax);
+        chunks = (len - __builtin_amdgcn_readlane(end, l) + token + p.C) / p.C;
+    }
+    if (chunks <= 1) return;                                   // done by the launch before, or of no sequence
+    for (int head = wave; head < p.Hq; head += 4) {
+        const size_t row = (size_t)token * p.Hq + head;
+        const float2 *ml = p.ml + row * p.nc;
+        const float *num = p.num + row * p.nc * kHeadDim + 2 * lane;
+        float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
+        for (int i = 0; i < chunks; ++i) top = fmaxf(top, ml[i].x);
+        for (int i = 0; i < chunks; ++i) {
+            const float2 s = ml[i], x = *reinterpret_cast<const float2 *>(num + (size_t)i * kHeadDim);
+            const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f(s.x - top);
+            a0 = __builtin_fmaf(x.x, f, a0);
+            a1 = __builtin_fmaf(x.y, f, a1);
+            sum = __builtin_fmaf(s.y, f, sum);
+        }
+        const float inv = 1.f / sum;
+        reinterpret_cast<unsigned *>(p.out + row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
     }
 }
 
@@ -119,12 +518,12 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
 
 hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s)
 {
-    // (no sequence leaves more than one tile unfilled)
-    const long long tiles = (long long)p.n_tokens * p.G / kTileRows + p.B;
-    const dim3 grid((unsigned)(tiles * p.pool.Hkv));
-    if (p.pool.store == kE4m3)
-        return p.pool.dtype == kF16 ? launch(kv_prefill_kernel<F16, true>, grid, dim3(256), s, p) : launch(kv_prefill_kernel<BF16, true>, grid, dim3(256), s, p);
-    return p.pool.dtype == kF16 ? launch(kv_prefill_kernel<F16, false>, grid, dim3(256), s, p) : launch(kv_prefill_kernel<BF16, false>, grid, dim3(256), s, p);
+    const dim3 grid((unsigned)((long long)p.tiles * p.pool.Hkv * p.nc));
+    const bool f16 = p.pool.dtype == kF16;
+    const hipError_t e = p.pool.store == kE4m3 ? launch(f16 ? kv_prefill_kernel<F16, true> : kv_prefill_kernel<BF16, true>, grid, dim3(256), s, p)
+                                               : launch(f16 ? kv_prefill_kernel<F16, false> : kv_prefill_kernel<BF16, false>, grid, dim3(256), s, p);
+    if (e != hipSuccess || p.nc == 1) return e;
+    return launch(f16 ? kv_prefill_join_kernel<F16> : kv_prefill_join_kernel<BF16>, dim3(p.n_tokens), dim3(256), s, p);
 }
 
 }  // namespace fd
