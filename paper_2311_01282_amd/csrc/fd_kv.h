@@ -33,39 +33,37 @@ template <class T> __device__ __forceinline__ u32x4_t from_codes(unsigned w0, un
 }
 __device__ __forceinline__ float scale_of(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
 
-// Where a block's rows are: of the pool, the first of keys 0 .. 15 and of 16 .. 31 (which may lie in another page).
+// Where a block's rows are: the first of keys 0 .. 15 in the pool, and of 16 .. 31, which may lie in another page.
 struct BlockRows {
-    size_t first[2];
+    size_t low, high;
 };
 // The pages of a block of a sequence whose last key is `last`: keys behind it are read from the last 16 that hold one.
 struct BlockPages {
-    int page[2];
+    int low, high;
 };
 __device__ __forceinline__ BlockPages block_pages(scalar_i32 table, int shift, int key0, int last)
 {
-    return BlockPages{{table[min(key0, last) >> shift], table[min(key0 + 16, last) >> shift]}};
+    return BlockPages{table[min(key0, last) >> shift], table[min(key0 + 16, last) >> shift]};
+}
+__device__ __forceinline__ size_t page_row(const KvPool &pool, int hkv, int entry, int key)
+{
+    const int page = min(max(entry, 0), pool.n_pages - 1);
+    return (((size_t)page * pool.Hkv + hkv) << pool.page_shift) + (key & ((1 << pool.page_shift) - 1));
 }
 __device__ __forceinline__ BlockRows block_rows(const KvPool &pool, int hkv, const BlockPages &pages, int key0, int last)
 {
-    BlockRows at;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int page = min(max(pages.page[i], 0), pool.n_pages - 1);
-        const int row = min(key0 + 16 * i, last & ~15) & ((1 << pool.page_shift) - 1);
-        at.first[i] = (((size_t)page * pool.Hkv + hkv) << pool.page_shift) + row;
-    }
-    return at;
+    return BlockRows{page_row(pool, hkv, pages.low, min(key0, last & ~15)), page_row(pool, hkv, pages.high, min(key0 + 16, last & ~15))};
 }
 
 // The rows of a block in a wavefront's registers, as they lie in the cache; k8: of 8 bits.
 template <class T, bool k8> struct Keys {
     u32x4_t x[2][k8 ? 2 : 4];
     u32x2_t scales;                                 // of keys 8 (n / 4) .. + 7
-    __device__ __forceinline__ void load(const KvPool &pool, const BlockRows &at, int lane)
+    __device__ __forceinline__ void load(const KvPool &pool, BlockRows at, int lane)
     {
         const int n = lane & 15, g = lane >> 4;
         // key 8 (n / 4) + 4 t + n % 4 of the block
-        const size_t first = (n < 8 ? at.first[0] : at.first[1]) + 8 * ((n >> 2) & 1);
+        const size_t first = (n < 8 ? at.low : at.high) + 8 * ((n >> 2) & 1);
         constexpr int kRow = k8 ? kHeadDim : 2 * kHeadDim;
         const unsigned char *from = pool.k + first * kRow + (n & 3) * kRow + 16 * g;
 #pragma unroll
@@ -93,10 +91,10 @@ template <class T, bool k8> struct Keys {
 template <class T, bool k8> struct Values {
     u32x4_t x[k8 ? 4 : 8];                          // elements 8 n .. + 7 of key 8 g + j; of 8 bits: of two keys
     u32x2_t scales;
-    __device__ __forceinline__ void load(const KvPool &pool, const BlockRows &at, int lane)
+    __device__ __forceinline__ void load(const KvPool &pool, BlockRows at, int lane)
     {
         const int n = lane & 15, g = lane >> 4;
-        const size_t first = (g < 2 ? at.first[0] : at.first[1]) + 8 * (g & 1);
+        const size_t first = (g < 2 ? at.low : at.high) + 8 * (g & 1);
         constexpr int kRow = k8 ? kHeadDim : 2 * kHeadDim;
         const unsigned char *from = pool.v + first * kRow + (k8 ? 8 : 16) * n;
 #pragma unroll

@@ -133,16 +133,27 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
 {
     __shared__ DecodeLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    const int chunk = blockIdx.x % p.nc, group = blockIdx.x / p.nc;
+    // The first chunk of every row, then the second: rows of a length lie side by side, and every XCD (index modulo 8) has as many of
+    // a chunk, which the short rows do not have, as of another.
+    const int groups = gridDim.x / p.nc, chunk = blockIdx.x / groups, group = blockIdx.x % groups;
     int unit = group;
     const int tile = unit % p.tiles;
     unit /= p.tiles;
     const int hkv = unit % p.pool.Hkv, b = unit / p.pool.Hkv;
     const int start = chunk * p.C;
+    const int heads = min(p.G - 16 * tile, 16), head0 = hkv * p.G + 16 * tile;      // query heads of this tile
+    // Everything that does not depend on the length is under way before it: the queries (which are first in the order of arrival, so that
+    // no wait for them is one for keys) and the pages of the first block.
+    u32x4_t q[4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb)                             // (columns without a head repeat the last)
+        q[kb] = *reinterpret_cast<const u32x4_t *>(p.q + ((size_t)b * p.Hq + head0 + min(n, heads - 1)) * kHeadDim + Keys<T, k8>::element(kb, g));
+    asm volatile("" ::: "memory");
     const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)b * p.width);
+    int key0 = start + kBlock * wave;
+    BlockPages pages = block_pages(table, p.pool.page_shift, key0, p.Smax - 1);
     const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
     const int end = min(len, start + p.C);
-    const int heads = min(p.G - 16 * tile, 16), head0 = hkv * p.G + 16 * tile;      // query heads of this tile
     if (start >= end) {
         // a sequence without keys: zero rows, by the first chunk (other chunks without keys leave nothing)
         if (chunk == 0)
@@ -153,26 +164,13 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
     const int last = end - 1;
     Keys<T, k8> keys;
     Values<T, k8> values;
-    BlockPages pages;
-    int key0 = start + kBlock * wave;
-    if (key0 < end) {
-        pages = block_pages(table, p.pool.page_shift, key0, last);
-        const BlockRows at = block_rows(p.pool, hkv, pages, key0, last);
-        keys.load(p.pool, at, lane);
-        values.load(p.pool, at, lane);
-        pages = block_pages(table, p.pool.page_shift, key0 + 4 * kBlock, last);
-    }
-    u32x4_t q[4];
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-        q[kb] = u32x4_t{0u, 0u, 0u, 0u};
-        if (n < heads)
-            q[kb] = *reinterpret_cast<const u32x4_t *>(p.q + ((size_t)b * p.Hq + head0 + n) * kHeadDim + Keys<T, k8>::element(kb, g));
-    }
     const float c1 = p.scale * kLog2e;
     Softmax<T> state;
     state.clear();
-    for (; key0 < end; key0 += 4 * kBlock) {
+    // A block, and the loads of the wavefront's next where there is one.  (Loads that a branch may have left out would be waited for as
+    // if they had not been: all of them, at every wait.)
+    auto block = [&](auto has_next, auto ends_here) {
+        constexpr bool kNext = decltype(has_next)::value, kTail = decltype(ends_here)::value;
         const int next = key0 + 4 * kBlock;
         f32x4_t s[2];
 #pragma unroll
@@ -181,28 +179,46 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) s[t] = T::mfma(keys.operand(t, kb, lane), q[kb], s[t]);
         }
+        // (the next rows take the registers of those that have been used)
+        __builtin_amdgcn_sched_barrier(0);
         BlockRows at;
-        if (next < end) {
+        if constexpr (kNext) {
             at = block_rows(p.pool, hkv, pages, next, last);
             keys.load(p.pool, at, lane);
         }
+        __builtin_amdgcn_sched_barrier(0);
         float z[8];
-        const int live = end - key0 - 8 * g;                   // keys from 8 g on
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3] * c1;
-        if (key0 + kBlock > end) {
+        if constexpr (kTail) {
+            const int live = end - key0 - 8 * g;               // keys from 8 g on
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = j < live ? z[j] : -INFINITY;
             values.keep(live);
         }
         u32x4_t a[8];
         values.operands(a);
-        if (next < end) {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) asm volatile("" : "+v"(a[dt]));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kNext) {
             values.load(p.pool, at, lane);
             pages = block_pages(table, p.pool.page_shift, next + 4 * kBlock, last);
         }
         // (no code of 8 bits is infinite, and NaN stay what they are)
         state.block(z, a, !k8 && any_not_finite<T>(a));
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (key0 < end) {
+        const BlockRows at = block_rows(p.pool, hkv, pages, key0, last);
+        keys.load(p.pool, at, lane);
+        values.load(p.pool, at, lane);
+        pages = block_pages(table, p.pool.page_shift, key0 + 4 * kBlock, last);
+#pragma unroll 1
+        for (; key0 + 4 * kBlock < end; key0 += 4 * kBlock) block(yes, no);
+        block(no, yes);
     }
 
     // the four wavefronts' sums
