@@ -658,9 +658,10 @@ fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const
  * New token i of n in a sequence of L keys stands at position L - n + i and attends to the keys up to there; at a position
  * below 0 (more new tokens than keys) its rows are zero.  Of a request that fd_page_tables did not serve, L is what was cached: its rows mean
  * nothing, and neither fault nor touch other rows.
- * shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk a multiple of 64 up to 2^30, for example
- * fd_kv_prefill_pick_chunk(shape, n_tokens): keys that a workgroup takes at most; from max_seq on rows are not split.
- * (n_tokens * n_q_heads / n_kv_heads / 128 + batch) * n_kv_heads * ceil(max_seq / chunk) <= 2^23.
+ * shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk, for example fd_kv_prefill_pick_chunk(shape, n_tokens):
+ * the keys of a sequence are dealt out to workgroups in pieces of chunk (rounded up to a multiple of 64) for every 128 of its (token,
+ * query head) rows of a KV head, begun ones counted; from max_seq on none is cut.  With T = n_tokens * n_q_heads / n_kv_heads / 128 +
+ * batch, (T + (chunk < max_seq ? batch * (max_seq / chunk) : 0)) * n_kv_heads <= 2^23.
  * Scores and sums in fp32; the weights enter the second product as numbers of dtype.
  */
 size_t    fd_kv_prefill_workspace_bytes(const fd_shape *shape, int32_t n_tokens);

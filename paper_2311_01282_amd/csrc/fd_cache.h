@@ -97,6 +97,7 @@ struct KvProblem {
     float2 *ml;
     int32_t *counters;
     int B, Hq, G, tiles, C, nc, Smax, width;
+    int by_length;                                 // the longest sequences first; set at launch
     float scale;
 };
 hipError_t launch_kv_decode(const KvProblem &p, hipStream_t s);
@@ -108,9 +109,9 @@ struct KvPromptProblem {
     long long q_stride;
     const int32_t *starts, *seq_lens, *table;      // starts [B + 1]
     uint16_t *out;                                 // [n_tokens, Hq, 128]
-    float *num;                                    // workspace: [n_tokens, Hq, nc, 128]
-    float2 *ml;                                    // [n_tokens, Hq, nc]
-    int B, Hq, G, n_tokens, tiles, C, nc, Smax, width;      // tiles: of 128 rows of a KV head, at most
+    float *num;                                    // workspace: [units, Hkv, 128 rows, 128]
+    float2 *ml;                                    // [units, Hkv, 128 rows]
+    int B, Hq, G, n_tokens, units, C, Smax, width; // units: of a KV head, at most; C: keys of a piece for each tile of a sequence
     float scale;
 };
 hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s);

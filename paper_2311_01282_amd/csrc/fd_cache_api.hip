@@ -2,6 +2,7 @@
 #include "../../include/fdattn.h"
 #include "fd_cache.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace {
@@ -170,22 +171,18 @@ fd_status latent_split(const fd_shape *sh, Split *S)
 
 fd_status kv_split(const fd_shape *sh, Split *S) { return split(sh, fd::kHeadDim, fd::kHeadDim, 64, S); }
 
-// The packed prompts: tiles of 128 (token, query head) rows of a KV head, of which no sequence leaves more than one unfilled.
-long long prompt_tiles(const fd_shape *sh, int32_t n_tokens)
-{
-    return (long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch;
-}
-fd_status prompt_split(const fd_shape *sh, int32_t n_tokens, Split *S)
+// The packed tokens: tiles of 128 (token, query head) rows of a KV head, of which no sequence leaves more than one unfilled.  A sequence of
+// t tiles and L keys is cut into ceil(L / (chunk t)) pieces, so that it has at most t + L / chunk (tile, piece) units; a unit that is
+// not its rows' only one leaves their sums in the workspace.
+fd_status prompt_split(const fd_shape *sh, int32_t n_tokens, long long *units, Split *S)
 {
     const fd_status st = check_shape(sh, fd::kHeadDim);
     if (st != FD_OK) return st;
     if (sh->chunk <= 0 || n_tokens < 0) return FD_ERR_SHAPE;
-    if (sh->chunk % 64 != 0 || sh->chunk > (1 << 30)) return FD_ERR_UNSUPPORTED;      // (a chunk's end fits 31 bits)
-    const long long units = prompt_tiles(sh, n_tokens) * sh->n_kv_heads;
-    S->rows = (long long)n_tokens * sh->n_q_heads;
-    S->nc = ((long long)sh->max_seq + sh->chunk - 1) / sh->chunk;
-    if (units > kMostThreads / 512 || units * S->nc > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
-    const size_t slots = S->nc == 1 ? 0 : (size_t)(S->rows * S->nc);
+    const long long tiles = (long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch;
+    *units = tiles + (sh->chunk < sh->max_seq ? (long long)sh->batch * (sh->max_seq / sh->chunk) : 0);
+    if (*units > kMostThreads / 512 || *units * sh->n_kv_heads > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
+    const size_t slots = sh->chunk < sh->max_seq ? (size_t)(*units * sh->n_kv_heads * 128) : 0;
     S->num = align_up(kCounters * sizeof(int32_t));
     S->ml = align_up(S->num + slots * fd::kHeadDim * sizeof(float));
     S->total = align_up(S->ml + slots * sizeof(float2));
@@ -452,7 +449,19 @@ size_t fd_kv_workspace_bytes(const fd_shape *shape)
 
 int32_t fd_kv_pick_chunk(const fd_shape *shape)
 {
-    return fd_nibble_pick_chunk(shape);
+    if (check_shape(shape, fd::kHeadDim) != FD_OK) return 0;
+    const long long units = (long long)shape->batch * shape->n_kv_heads * ((shape->n_q_heads / shape->n_kv_heads + 15) / 16);
+    // A workgroup draws what its compute unit can take (four wavefronts, a block each under way), and costs three round trips to memory
+    // before its first keys arrive; a join is a launch.  So one workgroup a compute unit where that fills the chip once, in
+    // chunks of 256 keys at least, and whole rows, which the launch sorts by length, where there are more; but no chunk that alone
+    // takes longer than 50 us.
+    // (Whole call, us, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 32 x 64/8 heads x 4096, 8 bits 64 / 57 / 49 / 48 /
+    // *44, 16 x 32 x 512 .. 4096, 8 bits 65 / 63 / 65 / 67 / *56, 64 x 32/8 x 500 .. 4000, 16 bits 114 / 104 / 103 / 107 / *93, 12 x 32/8 x
+    // 5000 .. 20001, 16 bits 122 / 113 / 115 / *115 / 137, 2 x 32/8 x 30000, 16 bits 49 / 47 / 44 / *42 / 66, 1 x 32 x 8192, 8 bits 19 /
+    // 16.3 / *15.7 / 23 / 37, 4 x 64/8 x 2000, 8 bits *9.7 / 11.2 / 15.0 / 19.5.)
+    const int32_t most = units >= fd::kComputeUnits && shape->max_seq <= 4096 ? 4096 : 2048;
+    const long long nc = std::max(units > 0 ? fd::kComputeUnits / units : 1, ((long long)shape->max_seq + most - 1) / most);
+    return chunk_for(shape->max_seq, 1, nc, 256, 64);
 }
 
 fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, const int32_t *block_table, const int32_t *seq_lens,
@@ -486,13 +495,22 @@ fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const
 size_t fd_kv_prefill_workspace_bytes(const fd_shape *shape, int32_t n_tokens)
 {
     Split S;
-    return prompt_split(shape, n_tokens, &S) == FD_OK ? S.total : 0;
+    long long units;
+    return prompt_split(shape, n_tokens, &units, &S) == FD_OK ? S.total : 0;
 }
 
 int32_t fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens)
 {
     if (check_shape(shape, fd::kHeadDim) != FD_OK || n_tokens < 0) return 0;
-    return (shape->max_seq + 63) / 64 * 64;
+    if (shape->batch == 0 || n_tokens == 0) return shape->max_seq;
+    const long long B = shape->batch, Hkv = shape->n_kv_heads, S = shape->max_seq;
+    const long long tiles = (long long)n_tokens * (shape->n_q_heads / shape->n_kv_heads) / 128, whole = std::max(tiles, std::min<long long>(B, n_tokens));
+    // Two workgroups fit a compute unit.  Launches of fewer units than 512 are cut so that they have about as many, in pieces of
+    // 768 keys at least: the sums of shorter ones cost more than they save.
+    if (whole * Hkv >= 4 * fd::kComputeUnits || S <= 1024) return shape->max_seq;
+    const long long each = std::max<long long>(tiles / B, 1);
+    const long long chunk = std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), (768 + each - 1) / each);
+    return (int32_t)std::min(chunk, S);
 }
 
 fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, int64_t q_stride, int32_t n_tokens,
@@ -500,7 +518,8 @@ fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, cons
                              void *stream)
 {
     Split S;
-    fd_status st = prompt_split(shape, n_tokens, &S);
+    long long units;
+    fd_status st = prompt_split(shape, n_tokens, &units, &S);
     if (st != FD_OK) return st;
     fd::KvPromptProblem p{};
     st = kv_pool(pool, &p.pool);
@@ -520,8 +539,8 @@ fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, cons
     p.num = reinterpret_cast<float *>(static_cast<char *>(ws.ptr) + S.num);
     p.ml = reinterpret_cast<float2 *>(static_cast<char *>(ws.ptr) + S.ml);
     p.B = shape->batch; p.Hq = shape->n_q_heads; p.G = shape->n_q_heads / shape->n_kv_heads; p.n_tokens = n_tokens;
-    p.tiles = (int)prompt_tiles(shape, n_tokens);
-    p.C = shape->chunk; p.nc = (int)S.nc; p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
+    p.units = (int)units;
+    p.C = shape->chunk; p.Smax = shape->max_seq; p.width = shape->max_seq / pool->page_size;
     p.scale = shape->scale;
     FD_TRY(fd::launch_kv_prefill(p, static_cast<hipStream_t>(stream)));
     return FD_OK;

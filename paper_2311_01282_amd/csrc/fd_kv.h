@@ -211,4 +211,128 @@ template <class T> struct Softmax {
     }
 };
 
+// A wavefront's blocks of 32 keys, every fourth from key0 on and below `end`, for up to 16 rows (of query heads or of tokens, lane
+// (n, .) row n) that share a KV head.  Nothing of the cache passes through LDS.  kMasks: a row sees the keys up to `position`, where
+// positions differ by less than 16: only a wavefront's last block has keys that not all see.
+// pages: of the first block.
+template <class T, bool k8, bool kMasks>
+__device__ __forceinline__ void walk_keys(const KvPool &pool, int hkv, scalar_i32 table, BlockPages pages, int key0, int end, int position,
+                                          const u32x4_t (&q)[4], float c1, int lane, Softmax<T> &state)
+{
+    constexpr int kNext = 4 * 32;
+    const int g = lane >> 4, last = end - 1;
+    Keys<T, k8> keys;
+    Values<T, k8> values;
+    // A block, and the loads of the next where there is one.  (Loads that a branch may have left out would be waited for as if they had
+    // not been: all of them, at every wait.)
+    auto block = [&](auto has_next, auto ends_here) {
+        constexpr bool kLoads = decltype(has_next)::value, kTail = decltype(ends_here)::value;
+        const int next = key0 + kNext;
+        f32x4_t s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) s[t] = T::mfma(keys.operand(t, kb, lane), q[kb], s[t]);
+        }
+        // (the next rows take the registers of those that have been used)
+        __builtin_amdgcn_sched_barrier(0);
+        BlockRows at;
+        if constexpr (kLoads) {
+            at = block_rows(pool, hkv, pages, next, last);
+            keys.load(pool, at, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3] * c1;
+        const int live = end - key0 - 8 * g, own = kMasks ? min(position + 1 - key0 - 8 * g, live) : live;      // keys from 8 g on
+        if constexpr (kTail) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = j < own ? z[j] : -INFINITY;
+            values.keep(live);
+        }
+        u32x4_t a[8];
+        values.operands(a);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) asm volatile("" : "+v"(a[dt]));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kLoads) {
+            values.load(pool, at, lane);
+            pages = block_pages(table, pool.page_shift, next + kNext, last);
+        }
+        // (no code of 8 bits is infinite, and NaN stay what they are)
+        const bool odd = (!k8 || (kMasks && kTail)) && any_not_finite<T>(a);
+        if constexpr (kMasks && kTail)
+            if (odd) {
+                // keys behind a row have the weight 0: what they hold must not reach it, be it infinite
+                u32x4_t seen;
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) seen[j >> 1] = T::pack(j < own ? 1.f : 0.f, j + 1 < own ? 1.f : 0.f);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const f32x4_t counts = T::mfma(not_finite<T>(a[dt]), seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) state.acc[dt][r] += summand(counts[r]);
+                    a[dt] = finite<T>(a[dt]);
+                }
+            }
+        state.block(z, a, odd);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (key0 < end) {
+        const BlockRows at = block_rows(pool, hkv, pages, key0, last);
+        keys.load(pool, at, lane);
+        values.load(pool, at, lane);
+        pages = block_pages(table, pool.page_shift, key0 + kNext, last);
+#pragma unroll 1
+        for (; key0 + kNext < end; key0 += kNext) block(yes, no);
+        block(no, yes);
+    }
+}
+
+// The sums of a workgroup's four wavefronts, and one row of all of them: lane l has elements 2 l and 2 l + 1.
+constexpr int kSumRow = kHeadDim + 4;            // (rows start in different banks)
+struct WaveSums {
+    alignas(16) float rows[4][16][kSumRow];
+    float m[4][16], l[4][16];
+    // (to be followed by a barrier)
+    template <class T> __device__ __forceinline__ void put(const Softmax<T> &state, int wave, int lane, int rows_used)
+    {
+        const int n = lane & 15, g = lane >> 4;
+        float sum = rows_sum(state.sum, state.sum);
+        sum = halves_sum(sum, sum);
+        if (n >= rows_used) return;
+        if (g == 0) {
+            m[wave][n] = state.ref;
+            l[wave][n] = sum;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<f32x4_t *>(&rows[wave][n][32 * g + 8 * r + 4 * h]) =
+                    f32x4_t{state.acc[4 * h][r], state.acc[4 * h + 1][r], state.acc[4 * h + 2][r], state.acc[4 * h + 3][r]};
+    }
+    __device__ __forceinline__ void row(int n, int lane, float &a0, float &a1, float &top, float &sum) const
+    {
+        top = -INFINITY;
+        a0 = a1 = sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, m[w][n]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = m[w][n];
+            // a wavefront without keys has m = -inf and zeros; one whose logits are all -inf or NaN has NaN, and keeps it
+            const float f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top);
+            const float2 x = *reinterpret_cast<const float2 *>(&rows[w][n][2 * lane]);
+            a0 = __builtin_fmaf(x.x, f, a0);
+            a1 = __builtin_fmaf(x.y, f, a1);
+            sum = __builtin_fmaf(l[w][n], f, sum);
+        }
+    }
+};
+
 }  // namespace fd

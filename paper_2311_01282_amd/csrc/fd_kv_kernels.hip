@@ -121,21 +121,35 @@ template <class T, bool k8> __global__ __launch_bounds__(256) void kv_read_kerne
 constexpr int kBlock = 32;
 constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
-constexpr int kSumRow = kHeadDim + 4;            // (rows start in different banks)
-
 struct DecodeLds {
-    alignas(16) float rows[4][16][kSumRow];
-    float m[4][16], l[4][16];
+    WaveSums sums;
     int last;
 };
+
+// The group that takes place `at` where the longest sequences come first (of at most 64; of equal ones the first).  Of launches that
+// give a compute unit two workgroups the first 256 go in reverse: the longest of the others join the shortest of them.
+__device__ __forceinline__ int by_length(const KvProblem &p, int at, int per, int lane)
+{
+    if (at < kComputeUnits) at = min(kComputeUnits, p.B * per) - 1 - at;
+    const int len = lane < p.B ? min(max(p.seq_lens[lane], 0), p.Smax) : -1;
+    int rank = 0;
+    for (int i = 0; i < p.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        rank += (other > len) | ((other == len) & (i < lane));
+    }
+    const unsigned long long it = __ballot(lane < p.B && rank == at / per);
+    return (int)__builtin_ctzll(it) * per + at % per;
+}
 
 template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_kernel(KvProblem p)
 {
     __shared__ DecodeLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    // The first chunk of every row, then the second: rows of a length lie side by side, and every XCD (index modulo 8) has as many of
-    // a chunk, which the short rows do not have, as of another.
-    const int groups = gridDim.x / p.nc, chunk = blockIdx.x / groups, group = blockIdx.x % groups;
+    // The first chunk of every row, then the second: every XCD (index modulo 8) has as many of a chunk, which the short rows do not
+    // have, as of another.
+    const int groups = gridDim.x / p.nc, chunk = blockIdx.x / groups, per = p.pool.Hkv * p.tiles;
+    int group = blockIdx.x % groups;
+    if (p.by_length) group = __builtin_amdgcn_readfirstlane(by_length(p, group, per, lane));
     int unit = group;
     const int tile = unit % p.tiles;
     unit /= p.tiles;
@@ -161,100 +175,15 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
                 reinterpret_cast<unsigned *>(p.out + ((size_t)b * p.Hq + head0) * kHeadDim)[i] = 0u;
         return;
     }
-    const int last = end - 1;
-    Keys<T, k8> keys;
-    Values<T, k8> values;
-    const float c1 = p.scale * kLog2e;
     Softmax<T> state;
     state.clear();
-    // A block, and the loads of the wavefront's next where there is one.  (Loads that a branch may have left out would be waited for as
-    // if they had not been: all of them, at every wait.)
-    auto block = [&](auto has_next, auto ends_here) {
-        constexpr bool kNext = decltype(has_next)::value, kTail = decltype(ends_here)::value;
-        const int next = key0 + 4 * kBlock;
-        f32x4_t s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) s[t] = T::mfma(keys.operand(t, kb, lane), q[kb], s[t]);
-        }
-        // (the next rows take the registers of those that have been used)
-        __builtin_amdgcn_sched_barrier(0);
-        BlockRows at;
-        if constexpr (kNext) {
-            at = block_rows(p.pool, hkv, pages, next, last);
-            keys.load(p.pool, at, lane);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        float z[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = s[j >> 2][j & 3] * c1;
-        if constexpr (kTail) {
-            const int live = end - key0 - 8 * g;               // keys from 8 g on
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = j < live ? z[j] : -INFINITY;
-            values.keep(live);
-        }
-        u32x4_t a[8];
-        values.operands(a);
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) asm volatile("" : "+v"(a[dt]));
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kNext) {
-            values.load(p.pool, at, lane);
-            pages = block_pages(table, p.pool.page_shift, next + 4 * kBlock, last);
-        }
-        // (no code of 8 bits is infinite, and NaN stay what they are)
-        state.block(z, a, !k8 && any_not_finite<T>(a));
-    };
-    const std::true_type yes;
-    const std::false_type no;
-    if (key0 < end) {
-        const BlockRows at = block_rows(p.pool, hkv, pages, key0, last);
-        keys.load(p.pool, at, lane);
-        values.load(p.pool, at, lane);
-        pages = block_pages(table, p.pool.page_shift, key0 + 4 * kBlock, last);
-#pragma unroll 1
-        for (; key0 + 4 * kBlock < end; key0 += 4 * kBlock) block(yes, no);
-        block(no, yes);
-    }
-
-    // the four wavefronts' sums
-    {
-        float l = rows_sum(state.sum, state.sum);
-        l = halves_sum(l, l);
-        if (n < heads) {
-            if (g == 0) {
-                lds.m[wave][n] = state.ref;
-                lds.l[wave][n] = l;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<f32x4_t *>(&lds.rows[wave][n][32 * g + 8 * r + 4 * h]) =
-                        f32x4_t{state.acc[4 * h][r], state.acc[4 * h + 1][r], state.acc[4 * h + 2][r], state.acc[4 * h + 3][r]};
-        }
-    }
+    walk_keys<T, k8, false>(p.pool, hkv, table, pages, key0, end, 0, q, p.scale * kLog2e, lane, state);
+    lds.sums.put(state, wave, lane, heads);
     __syncthreads();
     const int chunks = (len + p.C - 1) / p.C;                              // of this sequence
     for (int h = wave; h < heads; h += 4) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.m[w][h]);
-        float a0 = 0.f, a1 = 0.f, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float mw = lds.m[w][h];
-            // a wavefront without keys has m = -inf and zeros; one whose logits are all -inf or NaN has NaN, and keeps it
-            const float f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - top);
-            const float2 x = *reinterpret_cast<const float2 *>(&lds.rows[w][h][2 * lane]);
-            a0 = __builtin_fmaf(x.x, f, a0);
-            a1 = __builtin_fmaf(x.y, f, a1);
-            sum = __builtin_fmaf(lds.l[w][h], f, sum);
-        }
+        float a0, a1, top, sum;
+        lds.sums.row(h, lane, a0, a1, top, sum);
         const size_t out_row = (size_t)b * p.Hq + head0 + h;
         if (chunks == 1) {
             const float inv = 1.f / sum;
@@ -337,6 +266,7 @@ hipError_t launch_kv_decode(const KvProblem &p_, hipStream_t s)
     KvProblem p = p_;
     const long long workgroups = (long long)p.B * p.pool.Hkv * p.tiles * p.nc;
     if (p.nc > kJoinInPlace || workgroups > kJoinWorkgroups) p.counters = nullptr;
+    p.by_length = p.nc == 1 && p.B > 1 && p.B <= 64 && workgroups > kComputeUnits;
     const hipError_t e = by_type(p.pool, [&](auto type, auto k8) {
         return launch(kv_decode_kernel<decltype(type), decltype(k8)::value>, dim3((unsigned)workgroups), dim3(256), s, p);
     });

@@ -90,32 +90,59 @@ __device__ __forceinline__ u32x4_t window(const void *base, int bytes)
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
 }
 
-// The sequence and the place of a tile of the launch: sequences in order, a sequence's tiles from its last to its first.
-struct TilePlace {
-    int b, tile, first, tokens;                  // b < 0: there is none; the sequence's first token and their number
+// Units of work of a KV head: a sequence of t tiles is cut into pieces of p.C t keys (rounded up to 64), as fewer tiles need more pieces
+// to fill the chip; piece by piece, a piece's tiles from the last to the first.  Sequences of up to 64 go from the longest to the
+// shortest (of equal ones the first), of more in their order.
+struct Sequence {
+    int b, first, tokens, len;                   // its first new token, their number, its keys
+    int tiles, piece, units, before;             // keys of a piece; its units, and those of the sequences in front
 };
-__device__ __forceinline__ TilePlace find_tile(const KvPromptProblem &p, int at, int lane)
+__device__ __forceinline__ Sequence lane_sequence(const Sequence &x, int lane)
+{
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+    return Sequence{of(x.b), of(x.first), of(x.tokens), of(x.len), of(x.tiles), of(x.piece), of(x.units), of(x.before)};
+}
+// The sequences of 64 lanes, in that order, behind `before` units of others.
+__device__ __forceinline__ Sequence load_sequences(const KvPromptProblem &p, int b0, int before, int lane)
+{
+    Sequence x{b0 + lane, 0, 0, -1, 0, 64, 0, 0};
+    if (x.b < p.B) {
+        x.first = min(max(p.starts[x.b], 0), p.n_tokens);
+        x.tokens = max(min(max(p.starts[x.b + 1], 0), p.n_tokens) - x.first, 0);
+        x.len = min(max(p.seq_lens[x.b], 0), p.Smax);
+    }
+    if (p.B <= 64) {
+        int rank = lane;
+        for (int i = 0; i < p.B; ++i) {
+            const int other = __builtin_amdgcn_readlane(x.len, i);
+            rank += (int)(i > lane && other > x.len) - (int)(i < lane && other < x.len);
+        }
+        // (a permutation: lanes without a sequence are the last before and after)
+        x.b = __builtin_amdgcn_ds_permute(rank << 2, x.b);
+        x.first = __builtin_amdgcn_ds_permute(rank << 2, x.first);
+        x.tokens = __builtin_amdgcn_ds_permute(rank << 2, x.tokens);
+        x.len = __builtin_amdgcn_ds_permute(rank << 2, x.len);
+    }
+    x.tiles = (x.tokens * p.G + kTileRows - 1) / kTileRows;
+    // (in 32 bits: beyond Smax, which is 2^30 at most, a piece is the whole sequence)
+    const unsigned most = (unsigned)(p.Smax + 63) & ~63u;
+    x.piece = (int)min(__umulhi((unsigned)p.C, (unsigned)x.tiles) ? most : min((unsigned)p.C * (unsigned)x.tiles, most) + 63, most) & ~63;
+    x.units = x.tokens > 0 ? x.tiles * max((x.len + x.piece - 1) / x.piece, 1) : 0;
+    x.before = before + lanes_scan(x.units) - x.units;
+    return x;
+}
+// The first sequence in that order for which `is` holds; b < 0: none.
+template <class F> __device__ __forceinline__ Sequence find_sequence(const KvPromptProblem &p, int lane, F is)
 {
     int before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + lane;
-        int first = 0, tokens = 0;
-        if (b < p.B) {
-            first = min(max(p.starts[b], 0), p.n_tokens);
-            tokens = max(min(max(p.starts[b + 1], 0), p.n_tokens) - first, 0);
-        }
-        const int upto = before + lanes_scan((tokens * p.G + kTileRows - 1) / kTileRows);
-        const unsigned long long past = __ballot(upto > at);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            const int end = __builtin_amdgcn_readlane(upto, l);
-            return TilePlace{b0 + l, end - 1 - at, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(tokens, l)};
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
+        const Sequence x = load_sequences(p, b0, before, lane);
+        const unsigned long long found = __ballot(is(x));
+        if (found) return lane_sequence(x, __builtin_ctzll(found));
+        before = __builtin_amdgcn_readlane(x.before + x.units, 63);
     }
-    return TilePlace{-1, 0, 0, 0};
+    return Sequence{-1, 0, 0, 0, 0, 64, 0, 0};
 }
-
 // A window of memory that loads the compiler knows of go through: 0 behind it.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, int bytes)
 {
@@ -125,21 +152,63 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, int b
                                              __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 
+// A piece of a sequence of up to 16 rows, single tokens among them: what bounds it is memory, and the four wavefronts share its keys,
+// which pass from the cache into registers.
+constexpr int kFewRows = 16;
+template <class T, bool k8>
+__device__ __forceinline__ void few_rows(const KvPromptProblem &p, const Sequence &at, int chunk, int hkv, WaveSums &sums, int lane, int wave)
+{
+    const int n = lane & 15, g = lane >> 4, rows = at.tokens * p.G, ahead = at.len - at.tokens, begin = chunk * at.piece;
+    const int row = min(n, rows - 1), position = ahead + row / p.G, end = min(at.len, begin + at.piece);
+    const uint16_t *from = p.q + (size_t)(at.first + row / p.G) * p.q_stride + (size_t)(hkv * p.G + row % p.G) * kHeadDim;
+    u32x4_t q[4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) q[kb] = *reinterpret_cast<const u32x4_t *>(from + Keys<T, k8>::element(kb, g));
+    asm volatile("" ::: "memory");
+    const scalar_i32 table = (scalar_i32)(uintptr_t)(p.table + (size_t)at.b * p.width);
+    const int key0 = begin + 32 * wave;
+    Softmax<T> state;
+    state.clear();
+    const BlockPages pages = block_pages(table, p.pool.page_shift, min(key0, max(end - 1, 0)), max(end - 1, 0));
+    walk_keys<T, k8, true>(p.pool, hkv, table, pages, key0, end, position, q, p.scale * kLog2e, lane, state);
+    sums.put(state, wave, lane, rows);
+    __syncthreads();
+    for (int r = wave; r < rows; r += 4) {
+        float a0, a1, top, sum;
+        sums.row(r, lane, a0, a1, top, sum);
+        const int seen = ahead + r / p.G + 1, chunks = (seen + at.piece - 1) / at.piece;     // (of rows without keys: none)
+        if (chunks <= 1) {
+            if (chunk > 0) continue;
+            const float inv = 1.f / sum;
+            const size_t out_row = (size_t)(at.first + r / p.G) * p.Hq + hkv * p.G + r % p.G;
+            reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = seen > 0 ? T::pack(a0 * inv, a1 * inv) : 0u;
+        } else if (chunk < chunks && at.before + at.units <= p.units) {
+            const size_t slot = ((size_t)(at.before + chunk) * p.pool.Hkv + hkv) * kTileRows + r;
+            *reinterpret_cast<float2 *>(p.num + slot * kHeadDim + 2 * lane) = float2{a0, a1};
+            if (lane == 0) p.ml[slot] = float2{top, sum};
+        }
+    }
+}
+
 template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill_kernel(KvPromptProblem p)
 {
-    __shared__ PromptLds lds;
+    __shared__ union { PromptLds lds; WaveSums sums; } both;
+    PromptLds &lds = both.lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
-    int unit = blockIdx.x;
-    const int hkv = unit % p.pool.Hkv;
-    unit /= p.pool.Hkv;
-    const int chunk = unit / p.tiles;
-    const TilePlace at = find_tile(p, unit % p.tiles, lane);
+    const int hkv = blockIdx.x % p.pool.Hkv, unit = blockIdx.x / p.pool.Hkv;
+    const Sequence at = find_sequence(p, lane, [&](const Sequence &x) { return unit < x.before + x.units; });
     if (at.b < 0) return;
-    const int rows = at.tokens * p.G, row0 = at.tile * kTileRows + 32 * wave;       // of the sequence
-    const int len = min(max(p.seq_lens[at.b], 0), p.Smax), ahead = len - at.tokens;      // position of new token 0
-    const int begin = chunk * p.C, limit = min(len, begin + p.C);                   // (begin + C < 2^31)
+    const int index = unit - at.before;
+    if (at.tokens * p.G <= kFewRows) {
+        few_rows<T, k8>(p, at, index, hkv, both.sums, lane, wave);
+        return;
+    }
+    const int chunk = index / at.tiles, tile = at.tiles - 1 - index % at.tiles;
+    const int rows = at.tokens * p.G, row0 = tile * kTileRows + 32 * wave;          // of the sequence
+    const int len = at.len, ahead = len - at.tokens;          // position of new token 0
+    const int begin = chunk * at.piece, limit = min(len, begin + at.piece);
     auto keys_upto = [&](int row) { return min(ahead + row / p.G + 1, limit) - begin; };      // of the chunk, that a row sees
-    const int tile_keys = keys_upto(min(at.tile * kTileRows + kTileRows, rows) - 1);
+    const int tile_keys = keys_upto(min(tile * kTileRows + kTileRows, rows) - 1);
     if (tile_keys <= 0 && chunk > 0) return;
     const int row = min(row0 + c, rows - 1), token = row / p.G, head = hkv * p.G + row % p.G, position = ahead + token;
     const bool live = row0 + c < rows;
@@ -156,12 +225,6 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
     const int mine = row0 < rows ? max(keys_upto(min(row0 + 32, rows) - 1) + kStep - 1, 0) / kStep : 0;
     const int full = row0 < rows ? max(keys_upto(row0), 0) / kStep : 0;
 
-    u32x4_t q[8];
-    {
-        const uint16_t *from = p.q + (size_t)(at.first + token) * p.q_stride + (size_t)head * kHeadDim + 8 * h;
-#pragma unroll
-        for (int kb = 0; kb < 8; ++kb) q[kb] = *reinterpret_cast<const u32x4_t *>(from + 16 * kb);
-    }
     const unsigned lds_k = lds_address(lds.k[0]), lds_v = lds_address(lds.v[0]);
 
     // A wavefront fetches rows 8 wave .. + 7 of a step's keys and values, four rows an instruction: they share a page.  Rows
@@ -238,11 +301,15 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
     constexpr int kAhead = k8 ? 1 : 0;
     size_t place[3];                                           // of steps s + 2 + kAhead .. s + 4 + kAhead
     int entry;                                                 // of the last of these
-    __builtin_amdgcn_s_waitcnt(0x0f70);                        // the queries have arrived: what is counted from here on are fetches
     {
+        // (one round trip for all of them)
+        int entries[5 + kAhead];
         size_t first[4 + kAhead];
 #pragma unroll
-        for (int i = 0; i < 4 + kAhead; ++i) first[i] = row_place(page_entry(i), i);
+        for (int i = 0; i < 5 + kAhead; ++i) entries[i] = page_entry(i);
+        asm volatile("" ::"s"(entries[0]), "s"(entries[1]), "s"(entries[2]), "s"(entries[3]), "s"(entries[4]), "s"(entries[4 + kAhead]));
+#pragma unroll
+        for (int i = 0; i < 4 + kAhead; ++i) first[i] = row_place(entries[i], i);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             fetch_k(first[i], rows_of(i));
@@ -257,7 +324,14 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
         }
         place[0] = first[2 + kAhead];
         place[1] = first[3 + kAhead];
-        entry = page_entry(4 + kAhead);
+        entry = entries[4 + kAhead];
+    }
+    // (behind the first fetches, and waited for with them)
+    u32x4_t q[8];
+    {
+        const uint16_t *from = p.q + (size_t)(at.first + token) * p.q_stride + (size_t)head * kHeadDim + 8 * h;
+#pragma unroll
+        for (int kb = 0; kb < 8; ++kb) q[kb] = *reinterpret_cast<const u32x4_t *>(from + 16 * kb);
     }
 
     f32x16_t acc[4];
@@ -294,10 +368,9 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
     // own: of a step s, key 16 m + 8 h + i is visible to the lane's row where 16 m + i <= own
     auto own_of = [&](int s) { return position - begin - kStep * s - 8 * h; };
 
-    auto next_places = [&](int s) {
+    auto next_places = [&] {
         place[0] = place[1];
         place[1] = place[2];
-        entry = page_entry(s + 5 + kAhead);
     };
 
     // Step s from its logits, and the scores and logits of step s + 1, which do not depend on it.  Matrix instructions and what
@@ -370,6 +443,8 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
         slots(std::make_integer_sequence<int, 4>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
             acc[mm] = mfma32<T>(av[0][mm], w[0], acc[mm]);
+            first[mm] = read_k(k2, mm);
+            if constexpr (mm == 0) entry = page_entry(s + 5 + kAhead);
             if constexpr (mm < 3) {
                 weight(std::integral_constant<int, 10 + 2 * mm>{});
                 weight(std::integral_constant<int, 11 + 2 * mm>{});
@@ -382,7 +457,6 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
         slots(std::make_integer_sequence<int, 4>{}, [&](auto mi) {
             constexpr int mm = decltype(mi)::value;
             acc[mm] = mfma32<T>(av[1][mm], w[1], acc[mm]);
-            first[mm] = read_k(k2, mm);
             if constexpr (k8 && mm == 0) fetch_k(place[2], rows_of(s + 5));
             if constexpr (k8 && mm == 1) fetch_v(place[0], rows_of(s + 3));
 #pragma unroll
@@ -396,19 +470,23 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
             if constexpr (mm == 3) {
                 top = fmaxf(fmaxf(fmaxf(fmaxf(top, z[11]), z[12]), z[13]), z[14]);
                 top = halves_max(fmaxf(top, z[15]));
-                next_places(s);
             }
             __builtin_amdgcn_sched_barrier(0);
         });
+        next_places();
     };
 
-    if constexpr (!k8) wait_fetches<8>();                      // K of steps 0 and 1
+    if constexpr (!k8) __builtin_amdgcn_s_waitcnt(0x0f70);     // everything: the queries are the last; from here on fetches are counted
     tile_barrier();
     if (mine > 0) {
         unsigned kk = lds_k + k_at, k1 = kk + kStepBytes;
         asm("" : "+v"(kk), "+v"(k1));
+        u32x4_t a[8];
 #pragma unroll
-        for (int kb = 0; kb < 8; ++kb) scn = mfma32<T>(read_k(kk, kb), q[kb], kb == 0 ? zero : scn);
+        for (int kb = 0; kb < 8; ++kb) a[kb] = read_k(kk, kb);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < 8; ++kb) scn = mfma32<T>(a[kb], q[kb], kb == 0 ? zero : scn);
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) first[kb] = read_k(k1, kb);
         const int own = own_of(0);
@@ -445,12 +523,13 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
         }
         fetch_k(place[2], rows_of(s + 4 + kAhead));
         fetch_v(place[0], rows_of(s + 2 + kAhead));
-        next_places(s);
+        next_places();
+        entry = page_entry(s + 5 + kAhead);
     }
     wait_fetches<0>();                                         // nothing may land in LDS after the workgroup has ended
     sum = halves_sum(sum, sum);
     if (!live) return;
-    const int chunks = (position + p.C) / p.C;                 // that hold a key of the row
+    const int chunks = (position + at.piece) / at.piece;       // that hold a key of the row
     if (chunks <= 1) {
         if (chunk > 0) return;
         const bool some = position >= 0;
@@ -463,8 +542,8 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
                 if (!some) x = u32x2_t{0u, 0u};
                 *reinterpret_cast<u32x2_t *>(out + 32 * dt + 8 * j) = x;
             }
-    } else if (chunk < chunks) {
-        const size_t slot = out_row * p.nc + chunk;
+    } else if (chunk < chunks && at.before + at.units <= p.units) {        // (sequences that overlap may have more than there is room for)
+        const size_t slot = ((size_t)(at.before + index) * p.pool.Hkv + hkv) * kTileRows + 32 * wave + c;
         float *num = p.num + slot * kHeadDim + 4 * h;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -480,37 +559,73 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
 template <class T> __global__ __launch_bounds__(256) void kv_prefill_join_kernel(KvPromptProblem p)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = blockIdx.x;
-    // the sequence: the last one that starts at the token or before it and ends behind it
-    int chunks = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + lane;
-        int first = 0, end = 0;
-        if (b < p.B) {
-            first = min(max(p.starts[b], 0), p.n_tokens);
-            end = min(max(p.starts[b + 1], 0), p.n_tokens);
+    const Sequence at = find_sequence(p, lane, [&](const Sequence &x) { return x.first <= token && token < x.first + x.tokens; });
+    // (of no sequence; or of sequences that overlap, see above)
+    if (at.b < 0 || at.before + at.units > p.units) return;
+    const int chunks = (at.len - at.tokens + token - at.first + at.piece) / at.piece;
+    if (chunks <= 1) return;                                   // done by the launch before
+    // four heads at a time, so that the loads of all are under way together; 64 chunks at a time, their factors in the lanes
+    constexpr int kRows = 4;
+    const size_t next = (size_t)at.tiles * p.pool.Hkv * kTileRows;             // slots from a piece to the next
+    for (int head = kRows * wave; head < p.Hq; head += 4 * kRows) {
+        const float2 *ml[kRows];
+        const float *num[kRows];
+        float top[kRows], a0[kRows], a1[kRows], sum[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int of = min(head + r, p.Hq - 1), hkv = of / p.G, row = (token - at.first) * p.G + of % p.G;
+            const int unit = at.before + at.tiles - 1 - row / kTileRows;       // its tile's in the first piece
+            const size_t slot = ((size_t)unit * p.pool.Hkv + hkv) * kTileRows + row % kTileRows;
+            ml[r] = p.ml + slot;
+            num[r] = p.num + slot * kHeadDim + 2 * lane;
+            top[r] = -INFINITY;
+            a0[r] = a1[r] = sum[r] = 0.f;
         }
-        const unsigned long long in = __ballot(first <= token && token < end);
-        if (!in) continue;
-        const int l = 63 - __builtin_clzll(in);
-        const int len = min(max(p.seq_lens[b0 + l], 0), p.Smax);
-        chunks = (len - __builtin_amdgcn_readlane(end, l) + token + p.C) / p.C;
-    }
-    if (chunks <= 1) return;                                   // done by the launch before, or of no sequence
-    for (int head = wave; head < p.Hq; head += 4) {
-        const size_t row = (size_t)token * p.Hq + head;
-        const float2 *ml = p.ml + row * p.nc;
-        const float *num = p.num + row * p.nc * kHeadDim + 2 * lane;
-        float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
-        for (int i = 0; i < chunks; ++i) top = fmaxf(top, ml[i].x);
-        for (int i = 0; i < chunks; ++i) {
-            const float2 s = ml[i], x = *reinterpret_cast<const float2 *>(num + (size_t)i * kHeadDim);
-            const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f(s.x - top);
-            a0 = __builtin_fmaf(x.x, f, a0);
-            a1 = __builtin_fmaf(x.y, f, a1);
-            sum = __builtin_fmaf(s.y, f, sum);
+        for (int w0 = 0; w0 < chunks; w0 += 64) {
+            const int count = min(chunks - w0, 64);
+            float2 s[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) s[r] = ml[r][(w0 + min(lane, count - 1)) * next];
+            float f[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float m = lane < count ? s[r].x : -INFINITY, t = columns_max(row16_max(m));
+                if (t > top[r]) {                              // (uniform) what the chunks before left, to the new reference
+                    const float by = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[r] - t);
+                    a0[r] *= by;
+                    a1[r] *= by;
+                    sum[r] *= by;
+                    top[r] = t;
+                }
+                f[r] = m == top[r] ? 1.f : __builtin_amdgcn_exp2f(m - top[r]);
+                float d = row16_sum(lane < count ? s[r].y * f[r] : 0.f);
+                d = rows_sum(d, d);
+                sum[r] += halves_sum(d, d);
+            }
+            for (int i = 0; i < count; i += 2) {
+                float2 x[2][kRows];
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r)
+                        x[k][r] = *reinterpret_cast<const float2 *>(num[r] + (w0 + min(i + k, count - 1)) * next * kHeadDim);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) {
+                        if (i + k >= count) continue;
+                        const float by = as_f32((unsigned)__builtin_amdgcn_readlane(__builtin_bit_cast(int, f[r]), i + k));
+                        a0[r] = __builtin_fmaf(x[k][r].x, by, a0[r]);
+                        a1[r] = __builtin_fmaf(x[k][r].y, by, a1[r]);
+                    }
+            }
         }
-        const float inv = 1.f / sum;
-        reinterpret_cast<unsigned *>(p.out + row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const float inv = 1.f / sum[r];
+            if (head + r < p.Hq)
+                reinterpret_cast<unsigned *>(p.out + ((size_t)token * p.Hq + head + r) * kHeadDim)[lane] = T::pack(a0[r] * inv, a1[r] * inv);
+        }
     }
 }
 
@@ -518,11 +633,11 @@ template <class T> __global__ __launch_bounds__(256) void kv_prefill_join_kernel
 
 hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)p.tiles * p.pool.Hkv * p.nc));
+    const dim3 grid((unsigned)((long long)p.units * p.pool.Hkv));
     const bool f16 = p.pool.dtype == kF16;
     const hipError_t e = p.pool.store == kE4m3 ? launch(f16 ? kv_prefill_kernel<F16, true> : kv_prefill_kernel<BF16, true>, grid, dim3(256), s, p)
                                                : launch(f16 ? kv_prefill_kernel<F16, false> : kv_prefill_kernel<BF16, false>, grid, dim3(256), s, p);
-    if (e != hipSuccess || p.nc == 1) return e;
+    if (e != hipSuccess || p.C >= p.Smax) return e;
     return launch(f16 ? kv_prefill_join_kernel<F16> : kv_prefill_join_kernel<BF16>, dim3(p.n_tokens), dim3(256), s, p);
 }
 
