@@ -65,10 +65,12 @@ __device__ __forceinline__ unsigned lds_address(const void *p)
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4_t *lds_u32x4;
-// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+// (In assembly: of loads into LDS that the compiler knows it would wait before every transposing read.  A scalar register that a
+// vector instruction has written is read by a load five states later at the earliest; the compiler sees to that in its own code
+// only.)
 __device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, unsigned lds_1k)
 {
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs) : "memory");
 }
 template <class F, int... I> __device__ __forceinline__ void slots(std::integer_sequence<int, I...>, F f)
 {
@@ -432,6 +434,7 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
                     for (int i = 0; i < 8; i += 2) seen[i >> 1] = T::pack(16 * m + i <= own ? 1.f : 0.f, 16 * m + i + 1 <= own ? 1.f : 0.f);
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt) {
+                        __builtin_amdgcn_sched_barrier(0);     // (one after the other: rare, and registers are scarce)
                         const f32x16_t counts = mfma32<T>(not_finite<T>(av[m][dt]), seen, zero);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[dt][r] += summand(counts[r]);

@@ -155,3 +155,52 @@ def test_repeats_bit_for_bit_and_leaves_the_pool_alone(dtype, coded):
         assert (ws[:1 << 14] == 0).all()
     bits = torch.uint8 if coded else torch.int16
     assert all(torch.equal(a.view(bits), b.view(bits)) for a, b in zip(before, pool.rows))
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("batch,hq,hkv", [(40, 8, 8), (64, 10, 5), (65, 8, 4), (33, 80, 4), (2, 130, 130), (3, 258, 86), (57, 9, 9)])
+@pytest.mark.parametrize("kind", ["random", "equal", "edges"])
+def test_whole_rows_sorted_by_length(dtype, coded, batch, hq, hkv, kind):
+    """Launches of more workgroups than compute units in one chunk a row: a row that is done twice or not at all shows."""
+    g = torch.Generator().manual_seed(batch)
+    lens = [int(x) for x in torch.randint(0, 161, (batch,), generator=g)]
+    if kind == "equal":
+        lens = [77] * batch
+    if kind == "edges":
+        lens = [[0, 160, 1, 32, 33, 160][i % 6] for i in range(batch)]
+    pool, table, k, v = filled(dtype, coded, hkv, 16, lens, batch, 10)
+    q = queries(batch, hq, dtype)
+    table, dlens = device(lens, table)
+    shape = lib().make_shape(batch, hq, hkv, 128, 160, 0, SCALE)
+    assert lib().fd_kv_pick_chunk(shape) >= 160
+    got = decode(pool, table, dlens, q, 0, 160, SCALE)
+    assert not got.isnan().any()
+    few = [b for b in range(batch) if b < 6 or b > batch - 4]           # (the others by the rows without keys and by the check for NaN)
+    got, qc, share = got.cpu(), q.cpu(), hq // hkv
+    for b in few:
+        for h in range(hkv):
+            of = slice(h * share, (h + 1) * share)
+            if lens[b]:
+                check(got[b, of], dtype, 2, qc[b, of], k[b][h], v[b][h], SCALE, what="sequence %d, KV head %d" % (b, h))
+    assert all((got[b] == 0).all() == (lens[b] == 0) for b in range(batch))
+
+
+def test_agrees_with_the_calibrated_call_over_its_pool():
+    """With fp16 rows the pool is that of fd_decode_attn_paged."""
+    dtype = torch.float16
+    from paper_2311_01282_amd import synth
+    fd, lens = lib(), [700, 33, 0]
+    pool, table, k, v = filled(dtype, False, 2, 32, lens, 41, 24)
+    q = queries(3, 8, dtype)
+    table, dlens = device(lens, table)
+    got = decode(pool, table, dlens, q, 256, 768, SCALE)
+    shape = fd.make_shape(3, 8, 2, 128, 768, 256, SCALE)
+    ws = torch.zeros(fd.fd_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    other = torch.full_like(got, float("nan"))
+    stream = torch.cuda.current_stream().cuda_stream
+    fd.fd_workspace_init(shape, ws.data_ptr(), ws.numel(), stream)
+    fd.fd_decode_attn_paged(shape, q.data_ptr(), pool.rows[0].data_ptr(), pool.rows[1].data_ptr(), table.data_ptr(), 32, pool.n_pages, dlens.data_ptr(),
+                            synth.PHI, synth.BOUNDS, other.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    check_all(got, pool, lens, q, k, v)
+    check_all(other, pool, lens, q, k, v)
