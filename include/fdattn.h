@@ -478,7 +478,8 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  * What a serving step over a paged cache needs besides fp16 attention: pages and slots for the step's
  * tokens (fd_page_tables), a cache in 4 bits with the calls that fill, read and attend over it (fd_nibble_*,
  * fd_decode_attn_nibble), a cache of latent rows with its attention (fd_latent_*), and a cache of 16-bit or e4m3 rows with the
- * attention of a whole step, prompts and single tokens in one call (fd_kv_*).  All of them take fp16 or bf16.  The softmax is the synchronized one (a running maximum): no phi, no bounds, no flags.
+ * attention of a whole step, prompts and single tokens in one call (fd_kv_*).  All of them take fp16 or bf16.  The softmax is the
+ * synchronized one (a running maximum): no phi, no bounds, no flags.
  *   Slots.  Slot s of a pool is row s % page_size of page s / page_size; page_size is a power of two >= 16
  *     and n_pages * page_size < 2^31.  A slot outside [0, n_pages * page_size), -1 for example, is padding: its
  *     token is skipped.  The slots of one call that are no padding have to differ from each other.
@@ -487,7 +488,8 @@ fd_status fd_prefill_get_flags(const fd_shape *shape, fd_workspace ws, const uin
  *     clamped and reads the wrong page).
  *   Rows of the pools at and behind a sequence's length may hold anything, NaN included.
  *   Numbers.  Scores and outputs are summed in fp32 before they are scaled: bf16 numbers beyond 2^59 in queries and keys, or
- *     2^100 in values, may overflow there.  In latent attention fp16 weights below 2^-32 of a row's largest count as nothing.
+ *     2^100 in values, may overflow there.  In latent attention and fd_kv_prefill_attn fp16 weights below 2^-32 of a row's
+ *     largest count as nothing.
  *   Shapes.  max_seq <= 2^30; batch * n_q_heads * ceil(max_seq / chunk) <= 2^23, in prompts * ceil(max_seq / 128), and there
  *     also, batch * n_q_heads rounded up to a multiple of 8, < 2^24.
  *   Workspaces (of the decode calls and of fd_kv_prefill_attn).  Prepared once after allocation by fd_cache_workspace_init or any fill with zeros of
@@ -659,10 +661,12 @@ fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const
  * below 0 (more new tokens than keys) its rows are zero.  Of a request that fd_page_tables did not serve, L is what was cached: its rows mean
  * nothing, and neither fault nor touch other rows.
  * shape: n_kv_heads and head_dim as the pool's, any n_q_heads / n_kv_heads; chunk, for example fd_kv_prefill_pick_chunk(shape, n_tokens):
- * the keys of a sequence are dealt out to workgroups in pieces of chunk (rounded up to a multiple of 64) for every 128 of its (token,
- * query head) rows of a KV head, begun ones counted; from max_seq on none is cut.  With T = n_tokens * n_q_heads / n_kv_heads / 128 +
- * batch, (T + (chunk < max_seq ? batch * (max_seq / chunk) : 0)) * n_kv_heads <= 2^23.
- * Scores and sums in fp32; the weights enter the second product as numbers of dtype.
+ * the keys of a sequence are dealt out to workgroups in as few equal pieces (multiples of 64) as leave none more than chunk keys (rounded
+ * up to a multiple of 64) for every 128 of its (token, query head) rows of a KV head, begun ones counted; from max_seq on none is cut.
+ * With T = n_tokens * n_q_heads / n_kv_heads / 128 + batch, (T + (chunk < max_seq ? batch * (max_seq / chunk) : 0)) * n_kv_heads <= 2^23,
+ * and where chunk < max_seq n_tokens <= 2^23 and n_q_heads <= 16 * 65535.
+ * Scores and sums in fp32; the weights enter the second product as numbers of dtype, and the denominator is the sum of the rounded
+ * ones; of sequences of up to 16 rows a KV head as two numbers of dtype each.
  */
 size_t    fd_kv_prefill_workspace_bytes(const fd_shape *shape, int32_t n_tokens);
 int32_t   fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens);

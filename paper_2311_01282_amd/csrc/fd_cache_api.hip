@@ -182,6 +182,8 @@ fd_status prompt_split(const fd_shape *sh, int32_t n_tokens, long long *units, S
     const long long tiles = (long long)n_tokens * (sh->n_q_heads / sh->n_kv_heads) / 128 + sh->batch;
     *units = tiles + (sh->chunk < sh->max_seq ? (long long)sh->batch * (sh->max_seq / sh->chunk) : 0);
     if (*units > kMostThreads / 512 || *units * sh->n_kv_heads > kMostThreads / 512) return FD_ERR_UNSUPPORTED;
+    // (the launch that joins pieces has a token's 16 heads a workgroup)
+    if (sh->chunk < sh->max_seq && (n_tokens > kMostThreads / 512 || sh->n_q_heads > 16 * 65535)) return FD_ERR_UNSUPPORTED;
     const size_t slots = sh->chunk < sh->max_seq ? (size_t)(*units * sh->n_kv_heads * 128) : 0;
     S->num = align_up(kCounters * sizeof(int32_t));
     S->ml = align_up(S->num + slots * fd::kHeadDim * sizeof(float));
@@ -505,12 +507,32 @@ int32_t fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens)
     if (shape->batch == 0 || n_tokens == 0) return shape->max_seq;
     const long long B = shape->batch, Hkv = shape->n_kv_heads, S = shape->max_seq;
     const long long tiles = (long long)n_tokens * (shape->n_q_heads / shape->n_kv_heads) / 128, whole = std::max(tiles, std::min<long long>(B, n_tokens));
-    // Two workgroups fit a compute unit.  Launches of fewer units than 512 are cut so that they have about as many, in pieces of
-    // 768 keys at least: the sums of shorter ones cost more than they save.
-    if (whole * Hkv >= 4 * fd::kComputeUnits || S <= 1024) return shape->max_seq;
-    const long long each = std::max<long long>(tiles / B, 1);
-    const long long chunk = std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), (768 + each - 1) / each);
-    return (int32_t)std::min(chunk, S);
+    // Two workgroups fit a compute unit, and take 1.05 us for a step of 32 keys each that one alone takes 0.62 for.  Launches that leave
+    // compute units without a unit, or with one only, are cut so that they have about 512, in pieces of 768 keys at least: the sums of
+    // pieces, 520 bytes a row written and read again, and their join cost what shorter ones save.
+    // (Uncut / as picked here / in twice as many pieces, us: 512 tokens over 30000, 64/8 heads, 8 bits 625 / 535 / 540, 256 over 30000, 32/8
+    // 499 / 143 / 157, 100 over 8000, 64/8 138 / 60 / 78, 8 x 64 over 2000 .. 4000, 32/8 72 / 53 / 67, 16 single tokens over 2000 .. 3800, 32/8
+    // 63 / 49 / 54, 4000 of 8 heads that share one 72 / 66 / -; of more units: 1600 over 3000, 32/8 113 / 113 / 124.)
+    // Sequences of few rows are bound by memory and cut as for fd_kv_decode_attn; where there are as many units without that, only
+    // walks that would outlast the others are.
+    const bool single = tiles < B;
+    if (S <= 1024) return shape->max_seq;
+    long long chunk;
+    if (whole * Hkv >= fd::kComputeUnits * 5 / 4) {
+        chunk = S <= (single ? 4096 : 8192) ? S : single ? 2048 : 4096;
+    } else {
+        const long long each = std::max<long long>(tiles / B, 1);
+        chunk = std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), (768 + each - 1) / each);
+        if (single) chunk = std::min<long long>(chunk, 2048);
+    }
+    // ... and no workspace of more than 256 MiB
+    fd_shape cut = *shape;
+    for (;; chunk *= 2) {
+        if (chunk >= S) return shape->max_seq;
+        cut.chunk = (int32_t)chunk;
+        const size_t bytes = fd_kv_prefill_workspace_bytes(&cut, n_tokens);
+        if (bytes > 0 && bytes <= (256u << 20)) return cut.chunk;
+    }
 }
 
 fd_status fd_kv_prefill_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, int64_t q_stride, int32_t n_tokens,

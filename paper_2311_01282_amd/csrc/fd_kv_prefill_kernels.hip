@@ -92,9 +92,11 @@ __device__ __forceinline__ u32x4_t window(const void *base, int bytes)
                    (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00027000u};
 }
 
+constexpr int kFewRows = 16;
 // Units of work of a KV head: a sequence of t tiles is cut into pieces of p.C t keys (rounded up to 64), as fewer tiles need more pieces
 // to fill the chip; piece by piece, a piece's tiles from the last to the first.  Sequences of up to 64 go from the longest to the
-// shortest (of equal ones the first), of more in their order.
+// shortest (of equal ones the first), of more in their order; those of few rows count half: a key takes them 16 ns, others 33 (31 single
+// tokens beside a prompt of 1492, 32/8 heads: 140 us by the number of keys alone, 127 so).
 struct Sequence {
     int b, first, tokens, len;                   // its first new token, their number, its keys
     int tiles, piece, units, before;             // keys of a piece; its units, and those of the sequences in front
@@ -114,10 +116,11 @@ __device__ __forceinline__ Sequence load_sequences(const KvPromptProblem &p, int
         x.len = min(max(p.seq_lens[x.b], 0), p.Smax);
     }
     if (p.B <= 64) {
+        const int cost = x.tokens * p.G <= kFewRows ? x.len >> 1 : x.len;      // (of lanes without a sequence -1)
         int rank = lane;
         for (int i = 0; i < p.B; ++i) {
-            const int other = __builtin_amdgcn_readlane(x.len, i);
-            rank += (int)(i > lane && other > x.len) - (int)(i < lane && other < x.len);
+            const int other = __builtin_amdgcn_readlane(cost, i);
+            rank += (int)(i > lane && other > cost) - (int)(i < lane && other < cost);
         }
         // (a permutation: lanes without a sequence are the last before and after)
         x.b = __builtin_amdgcn_ds_permute(rank << 2, x.b);
@@ -128,8 +131,14 @@ __device__ __forceinline__ Sequence load_sequences(const KvPromptProblem &p, int
     x.tiles = (x.tokens * p.G + kTileRows - 1) / kTileRows;
     // (in 32 bits: beyond Smax, which is 2^30 at most, a piece is the whole sequence)
     const unsigned most = (unsigned)(p.Smax + 63) & ~63u;
-    x.piece = (int)min(__umulhi((unsigned)p.C, (unsigned)x.tiles) ? most : min((unsigned)p.C * (unsigned)x.tiles, most) + 63, most) & ~63;
-    x.units = x.tokens > 0 ? x.tiles * max((x.len + x.piece - 1) / x.piece, 1) : 0;
+    x.piece = (int)most;
+    x.units = x.tiles;
+    if (p.C < p.Smax && x.len > 0) {             // in pieces of one length, as many as those of p.C t keys
+        const int piece = (int)min(__umulhi((unsigned)p.C, (unsigned)x.tiles) ? most : min((unsigned)p.C * (unsigned)x.tiles, most) + 63, most) & ~63;
+        const int n = (x.len + piece - 1) / max(piece, 64);
+        x.piece = ((x.len + n - 1) / max(n, 1) + 63) & ~63;
+        x.units = x.tiles * ((x.len + x.piece - 1) / x.piece);
+    }
     x.before = before + lanes_scan(x.units) - x.units;
     return x;
 }
@@ -156,7 +165,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base, int b
 
 // A piece of a sequence of up to 16 rows, single tokens among them: what bounds it is memory, and the four wavefronts share its keys,
 // which pass from the cache into registers.
-constexpr int kFewRows = 16;
 template <class T, bool k8>
 __device__ __forceinline__ void few_rows(const KvPromptProblem &p, const Sequence &at, int chunk, int hkv, WaveSums &sums, int lane, int wave)
 {
@@ -557,78 +565,83 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
     }
 }
 
-// Rows that several workgroups share: out = sum_c 2^{m_c - M} num_c / sum_c 2^{m_c - M} l_c.  A workgroup a token, a wavefront every
-// fourth of its heads.
+// Rows that several workgroups share: out = sum_c 2^{m_c - M} num_c / sum_c 2^{m_c - M} l_c.  A workgroup takes 16 heads of a token, a
+// wavefront four of them, so that the loads of all are under way together.  (By tiles of a unit instead 8 x 64 tokens over 2000 .. 4000,
+// 32/8 heads, took 60 us for 52.5.)
+constexpr int kJoinHeads = 16;
 template <class T> __global__ __launch_bounds__(256) void kv_prefill_join_kernel(KvPromptProblem p)
 {
+    constexpr int kRows = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = blockIdx.x;
+    const int head = kJoinHeads * blockIdx.y + kRows * wave;
+    if (head >= p.Hq) return;
     const Sequence at = find_sequence(p, lane, [&](const Sequence &x) { return x.first <= token && token < x.first + x.tokens; });
-    // (of no sequence; or of sequences that overlap, see above)
-    if (at.b < 0 || at.before + at.units > p.units) return;
+    // (of no sequence; not cut; or of sequences that overlap, see above)
+    if (at.b < 0 || at.units == at.tiles || at.before < 0 || at.before + at.units > p.units) return;
     const int chunks = (at.len - at.tokens + token - at.first + at.piece) / at.piece;
     if (chunks <= 1) return;                                   // done by the launch before
-    // four heads at a time, so that the loads of all are under way together; 64 chunks at a time, their factors in the lanes
-    constexpr int kRows = 4;
     const size_t next = (size_t)at.tiles * p.pool.Hkv * kTileRows;             // slots from a piece to the next
-    for (int head = kRows * wave; head < p.Hq; head += 4 * kRows) {
-        const float2 *ml[kRows];
-        const float *num[kRows];
-        float top[kRows], a0[kRows], a1[kRows], sum[kRows];
+    const float2 *ml[kRows];
+    const float *num[kRows];
+    float top[kRows], a0[kRows], a1[kRows], sum[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int of = min(head + r, p.Hq - 1), hkv = of / p.G, row = (token - at.first) * p.G + of % p.G;
+        const int unit = at.before + at.tiles - 1 - row / kTileRows;           // its tile's in the first piece
+        const size_t slot = ((size_t)unit * p.pool.Hkv + hkv) * kTileRows + row % kTileRows;
+        ml[r] = p.ml + slot;
+        num[r] = p.num + slot * kHeadDim + 2 * lane;
+        top[r] = -INFINITY;
+        a0[r] = a1[r] = sum[r] = 0.f;
+    }
+    // 64 pieces at a time, their factors in the lanes; two partial vectors of each row under way, the first before the factors
+    for (int w0 = 0; w0 < chunks; w0 += 64) {
+        const int count = min(chunks - w0, 64);
+        float2 s[kRows], x[2][kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) s[r] = ml[r][(w0 + min(lane, count - 1)) * next];
+        auto load = [&](int i) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+                    x[k][r] = *reinterpret_cast<const float2 *>(num[r] + (w0 + min(i + k, count - 1)) * next * kHeadDim);
+        };
+        load(0);
+        float f[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const int of = min(head + r, p.Hq - 1), hkv = of / p.G, row = (token - at.first) * p.G + of % p.G;
-            const int unit = at.before + at.tiles - 1 - row / kTileRows;       // its tile's in the first piece
-            const size_t slot = ((size_t)unit * p.pool.Hkv + hkv) * kTileRows + row % kTileRows;
-            ml[r] = p.ml + slot;
-            num[r] = p.num + slot * kHeadDim + 2 * lane;
-            top[r] = -INFINITY;
-            a0[r] = a1[r] = sum[r] = 0.f;
+            const float m = lane < count ? s[r].x : -INFINITY, t = columns_max(row16_max(m));
+            if (t > top[r]) {                                  // (uniform) what the pieces before left, to the new reference
+                const float by = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[r] - t);
+                a0[r] *= by;
+                a1[r] *= by;
+                sum[r] *= by;
+                top[r] = t;
+            }
+            f[r] = m == top[r] ? 1.f : __builtin_amdgcn_exp2f(m - top[r]);
+            float d = row16_sum(lane < count ? s[r].y * f[r] : 0.f);
+            d = rows_sum(d, d);
+            sum[r] += halves_sum(d, d);
         }
-        for (int w0 = 0; w0 < chunks; w0 += 64) {
-            const int count = min(chunks - w0, 64);
-            float2 s[kRows];
+        for (int i = 0; i < count; i += 2) {
+            if (i > 0) load(i);
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) s[r] = ml[r][(w0 + min(lane, count - 1)) * next];
-            float f[kRows];
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const float m = lane < count ? s[r].x : -INFINITY, t = columns_max(row16_max(m));
-                if (t > top[r]) {                              // (uniform) what the chunks before left, to the new reference
-                    const float by = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top[r] - t);
-                    a0[r] *= by;
-                    a1[r] *= by;
-                    sum[r] *= by;
-                    top[r] = t;
+                for (int r = 0; r < kRows; ++r) {
+                    if (i + k >= count) continue;
+                    const float by = as_f32((unsigned)__builtin_amdgcn_readlane(__builtin_bit_cast(int, f[r]), i + k));
+                    a0[r] = __builtin_fmaf(x[k][r].x, by, a0[r]);
+                    a1[r] = __builtin_fmaf(x[k][r].y, by, a1[r]);
                 }
-                f[r] = m == top[r] ? 1.f : __builtin_amdgcn_exp2f(m - top[r]);
-                float d = row16_sum(lane < count ? s[r].y * f[r] : 0.f);
-                d = rows_sum(d, d);
-                sum[r] += halves_sum(d, d);
-            }
-            for (int i = 0; i < count; i += 2) {
-                float2 x[2][kRows];
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int r = 0; r < kRows; ++r)
-                        x[k][r] = *reinterpret_cast<const float2 *>(num[r] + (w0 + min(i + k, count - 1)) * next * kHeadDim);
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int r = 0; r < kRows; ++r) {
-                        if (i + k >= count) continue;
-                        const float by = as_f32((unsigned)__builtin_amdgcn_readlane(__builtin_bit_cast(int, f[r]), i + k));
-                        a0[r] = __builtin_fmaf(x[k][r].x, by, a0[r]);
-                        a1[r] = __builtin_fmaf(x[k][r].y, by, a1[r]);
-                    }
-            }
         }
+    }
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const float inv = 1.f / sum[r];
-            if (head + r < p.Hq)
-                reinterpret_cast<unsigned *>(p.out + ((size_t)token * p.Hq + head + r) * kHeadDim)[lane] = T::pack(a0[r] * inv, a1[r] * inv);
-        }
+    for (int r = 0; r < kRows; ++r) {
+        const float inv = 1.f / sum[r];
+        if (head + r < p.Hq)
+            reinterpret_cast<unsigned *>(p.out + ((size_t)token * p.Hq + head + r) * kHeadDim)[lane] = T::pack(a0[r] * inv, a1[r] * inv);
     }
 }
 
@@ -641,7 +654,7 @@ hipError_t launch_kv_prefill(const KvPromptProblem &p, hipStream_t s)
     const hipError_t e = p.pool.store == kE4m3 ? launch(f16 ? kv_prefill_kernel<F16, true> : kv_prefill_kernel<BF16, true>, grid, dim3(256), s, p)
                                                : launch(f16 ? kv_prefill_kernel<F16, false> : kv_prefill_kernel<BF16, false>, grid, dim3(256), s, p);
     if (e != hipSuccess || p.C >= p.Smax) return e;
-    return launch(f16 ? kv_prefill_join_kernel<F16> : kv_prefill_join_kernel<BF16>, dim3(p.n_tokens), dim3(256), s, p);
+    return launch(f16 ? kv_prefill_join_kernel<F16> : kv_prefill_join_kernel<BF16>, dim3(p.n_tokens, (p.Hq + kJoinHeads - 1) / kJoinHeads), dim3(256), s, p);
 }
 
 }  // namespace fd

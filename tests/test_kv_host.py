@@ -130,6 +130,16 @@ def test_picked_chunks_are_taken(batch, hq, hkv, max_seq):
         assert nbytes <= 1 << 28                                        # what a serving program can set aside
 
 
+@pytest.mark.parametrize("hq,tokens", [(1, (1 << 23) + 1), (16 * 65535 + 1, 1)])
+def test_cut_launches_stay_within_their_grid(hq, tokens):
+    # the launch that joins pieces: a token's 16 heads a workgroup of 256 threads, fewer than 2^32 threads along x, 2^16 workgroups along y
+    cut, whole = (fd.make_shape(1, hq, 1, 128, 4096, chunk, 0.1) for chunk in (2048, 4096))
+    assert fd.fd_kv_prefill_workspace_bytes(cut, tokens) == 0
+    assert fd.fd_kv_prefill_workspace_bytes(whole, tokens) > 0
+    assert fd.fd_kv_prefill_pick_chunk(whole, tokens) == 4096
+    assert fd.fd_kv_prefill_workspace_bytes(fd.make_shape(1, hq - 1, 1, 128, 4096, 2048, 0.1) if hq > 1 else cut, tokens - (hq == 1)) > 0
+
+
 def test_queries_of_sizes_refuse_bad_shapes():
     for call in (fd.fd_kv_workspace_bytes, fd.fd_kv_pick_chunk):
         assert call(fd.make_shape(2, 8, 2, 64, 1024, 256, 0.1)) == 0
