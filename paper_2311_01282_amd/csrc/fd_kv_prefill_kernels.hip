@@ -11,6 +11,14 @@
 //   output   O^T[d][row] = V^T . P^T: A = V^T by the transposing LDS read.
 // Softmax with a running maximum per row; the weights are of the type (one rounding, as large as the output's own), their sum
 // is that of the rounded ones, in fp32.
+//
+// What bounds it: 4 x 128 products of 16 bits for each (row, key), the matrix cores' at 1.34 .. 1.40 PFLOP/s of a plain product of 8192^3,
+// and in long calls the power that they draw: one prompt of 8001 tokens, 32/8 heads, bf16, takes 506 us (1.04 PFLOP/s), with queries
+// and keys of zeros 399 (1.31).  A wavefront's 32 rows take a step's keys and values from LDS once, 16 KiB for 2 x 16 KFLOP x 32; a tile in
+// registers that needs the softmax only within lanes (c, 0) and (c, 1); two workgroups a compute unit, of which one has products while
+// the other has exponentials.  A step takes 1.05 us (both), one workgroup alone 0.62.  Outside its loop a workgroup takes 8 us: 2 until
+// it knows its sequence, 3 to 4 until the page table, the first rows and the queries have arrived one after the other, 2 for the
+// output; five prompts of 150 to 2000 tokens, 32 heads, fp16, take 105 us for 51 of products.
 #include <utility>
 
 #include "fd_kv.h"
@@ -205,7 +213,10 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
     __shared__ union { PromptLds lds; WaveSums sums; } both;
     PromptLds &lds = both.lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
-    const int hkv = blockIdx.x % p.pool.Hkv, unit = blockIdx.x / p.pool.Hkv;
+    // Of launches that give no compute unit more than two workgroups the first one each go in reverse: the longest of the others join the
+    // shortest of them.  (2000 tokens, 32/8 heads 54.4 -> 50.5 us, 1500 over 500 52.8 -> 47.5, 300 and 800, 64/8 24.8 -> 21.6.)
+    const int hkv = blockIdx.x % p.pool.Hkv, turn = blockIdx.x / p.pool.Hkv, alone = kComputeUnits / p.pool.Hkv;
+    const int unit = gridDim.x <= 2 * kComputeUnits && gridDim.x > kComputeUnits && turn < alone ? alone - 1 - turn : turn;
     const Sequence at = find_sequence(p, lane, [&](const Sequence &x) { return unit < x.before + x.units; });
     if (at.b < 0) return;
     const int index = unit - at.before;
