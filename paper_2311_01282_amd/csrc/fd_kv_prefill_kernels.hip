@@ -12,11 +12,11 @@
 // Softmax with a running maximum per row; the weights are of the type (one rounding, as large as the output's own), their sum
 // is that of the rounded ones, in fp32.
 //
-// What bounds it: 4 x 128 products of 16 bits for each (row, key), the matrix cores' at 1.34 .. 1.40 PFLOP/s of a plain product of 8192^3,
-// and in long calls the power that they draw: one prompt of 8001 tokens, 32/8 heads, bf16, takes 506 us (1.04 PFLOP/s), with queries
-// and keys of zeros 399 (1.31).  A wavefront's 32 rows take a step's keys and values from LDS once, 16 KiB for 2 x 16 KFLOP x 32; a tile in
-// registers that needs the softmax only within lanes (c, 0) and (c, 1); two workgroups a compute unit, of which one has products while
-// the other has exponentials.  A step takes 1.05 us (both), one workgroup alone 0.62.  Outside its loop a workgroup takes 8 us: 2 until
+// What bounds it: 512 operations for each (row, key), of which a plain product of 8192^3 reaches 1.34 (fp16) and 1.40 (bf16) PFLOP/s, and
+// in long calls the power that they draw: one prompt of 8001 tokens, 32/8 heads, bf16, takes 506 us (1.04 PFLOP/s), with queries
+// and keys of zeros 399 (1.31).  So products of 32 x 32, whose operands serve twice as many rows or keys as those of 16 x 16 (a wavefront
+// reads 16 KiB of LDS for 0.5 MFLOP), rows in lanes, so that a softmax needs one exchange, of two lanes, and two workgroups a compute
+// unit, one with products while the other has exponentials.  A step takes 1.05 us (both), one workgroup alone 0.62.  Outside its loop a workgroup takes 8 us: 2 until
 // it knows its sequence, 3 to 4 until the page table, the first rows and the queries have arrived one after the other, 2 for the
 // output; five prompts of 150 to 2000 tokens, 32 heads, fp16, take 105 us for 51 of products.
 #include <utility>

@@ -240,3 +240,44 @@ def test_repeats_bit_for_bit(dtype, coded):
         outs = [prefill(pool, table, dlens, starts, q, chunk, 94 * 16, SCALE, ws) for _ in range(4)]
         assert all(torch.equal(outs[0], x) for x in outs[1:])
         assert (ws[:1 << 14] == 0).all()
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("hq,hkv,chunk,lens,new", [
+    (20, 5, 1, [64 * 139 + 7, 500, 4160], [1, 4, 3]),                   # few rows: pieces of 64 keys
+    (20, 5, 30, [64 * 139 + 7, 500, 4160], [40, 9, 1]),                 # two tiles: pieces of 64; one: 64
+    (18, 1, 20, [128 * 70 + 1, 64], [20, 64]),                          # three tiles of 18 heads: pieces of 64; nine: 192
+])
+def test_many_pieces(dtype, coded, hq, hkv, chunk, lens, new):
+    """More pieces of a row than lanes; the largest logits behind the first 64 pieces."""
+    def change(b, which, x):
+        if which == 0:
+            x = x * 0.05
+            x[:, -200:-100] = 2.0
+        return x
+    width = -(-max(lens) // 64) + 1
+    pool, table, k, v = filled(dtype, coded, hkv, 64, lens, 43, width, 1.0, change)
+    q = fused(sum(new), hq, dtype)
+    q[:, ::2] = 1.0
+    table, dlens, starts = device(lens, table, new)
+    got = prefill(pool, table, dlens, starts, q, chunk, width * 64, 0.05)
+    check_all(got, pool, lens, new, q, k, v, 0.05, heads=sorted({0, 1, hq // 2, hq - 2, hq - 1}))
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("hq,hkv", [(24, 12), (300, 300), (33, 11)])
+def test_launches_of_up_to_two_workgroups_a_compute_unit(dtype, coded, hq, hkv):
+    """257 to 512 workgroups, also of head numbers that do not divide 256 or are larger."""
+    batch = 360 // hkv
+    g = torch.Generator().manual_seed(batch)
+    new = [int(x) for x in torch.randint(0, 30, (batch,), generator=g)]
+    new[0] = max(new[0], 2)
+    lens = [n + int(x) for n, x in zip(new, torch.randint(0, 200, (batch,), generator=g))]
+    assert 256 < (sum(new) * hq // hkv // 128 + batch) * hkv <= 512
+    pool, table, k, v = filled(dtype, coded, hkv, 16, lens, 47, 15)
+    q = fused(sum(new), hq, dtype)
+    table, dlens, starts = device(lens, table, new)
+    got = prefill(pool, table, dlens, starts, q, 240, 240, SCALE)
+    check_all(got, pool, lens, new, q, k, v, heads=sorted({0, hq // 2, hq - 1}))
