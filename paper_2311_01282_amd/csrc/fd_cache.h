@@ -98,6 +98,7 @@ struct KvProblem {
     int32_t *counters;
     int B, Hq, G, tiles, C, nc, Smax, width;
     int by_length;                                 // the longest sequences first; set at launch
+    int shares;                                    // pieces of the sequences altogether, by their lengths; 0: chunks of C; set at launch
     float scale;
 };
 hipError_t launch_kv_decode(const KvProblem &p, hipStream_t s);

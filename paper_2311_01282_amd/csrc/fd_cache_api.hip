@@ -454,15 +454,18 @@ int32_t fd_kv_pick_chunk(const fd_shape *shape)
     if (check_shape(shape, fd::kHeadDim) != FD_OK) return 0;
     const long long units = (long long)shape->batch * shape->n_kv_heads * ((shape->n_q_heads / shape->n_kv_heads + 15) / 16);
     // A workgroup draws what its compute unit can take (four wavefronts, a block each under way), and costs three round trips to memory
-    // before its first keys arrive; a join is a launch.  So one workgroup a compute unit where that fills the chip once, in
-    // chunks of 256 keys at least, and whole rows, which the launch sorts by length, where there are more; but no chunk that alone
-    // takes longer than 50 us.
-    // (Whole call, us, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 32 x 64/8 heads x 4096, 8 bits 64 / 57 / 49 / 48 /
-    // *44, 16 x 32 x 512 .. 4096, 8 bits 65 / 63 / 65 / 67 / *56, 64 x 32/8 x 500 .. 4000, 16 bits 114 / 104 / 103 / 107 / *93, 12 x 32/8 x
-    // 5000 .. 20001, 16 bits 122 / 113 / 115 / *115 / 137, 2 x 32/8 x 30000, 16 bits 49 / 47 / 44 / *42 / 66, 1 x 32 x 8192, 8 bits 19 /
-    // 16.3 / *15.7 / 23 / 37, 4 x 64/8 x 2000, 8 bits *9.7 / 11.2 / 15.0 / 19.5.)
-    const int32_t most = units >= fd::kComputeUnits && shape->max_seq <= 4096 ? 4096 : 2048;
-    const long long nc = std::max(units > 0 ? fd::kComputeUnits / units : 1, ((long long)shape->max_seq + most - 1) / most);
+    // before its first keys arrive.  So whole rows, which the launch sorts by length, where they fill the chip and are short enough not to
+    // outlast the others; where chunks of 512 keys would fill it more than once and the launch makes pieces by the sequences' lengths, of
+    // a chunk at least, those; otherwise one workgroup a compute unit, in chunks of 256 keys at least and 2048 at most.
+    // (Whole call, us, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 32 x 64/8 heads x 4096, 8 bits 51 / 51 / 51 / 51 /
+    // *44, 16 x 32 x 512 .. 4096, 8 bits 65 / 65 / 65 / 70 / *56, 64 x 32/8 x 500 .. 4000, 16 bits 115 / 112 / 111 / 109 / *93, 12 x 32/8 x
+    // 5000 .. 20001, 16 bits 103 / *102 / 102 / 102 / 105, 4 x 32/8 x 1000 .. 30000, 16 bits 33 / *33 / 33 / 38 / 64, 1 x 32 x 8192, 8 bits 19 /
+    // 16.3 / *15.7 / 23 / 37, 4 x 64/8 x 2000, 8 bits *9.5 / 11.2 / 14.6 / 15.5.)
+    const long long S = shape->max_seq, chip = fd::kComputeUnits;
+    if (units >= chip && S <= 4096) return chunk_for(shape->max_seq, 1, 1, 256, 64);
+    if (shape->batch > 1 && shape->batch <= 64 && units <= 2 * chip && units * ((S + 511) / 512) > chip)   // (128 chunks a row at most)
+        return (int32_t)std::min<long long>(std::max<long long>(512, (S / 128 + 63) / 64 * 64), 16384);
+    const long long nc = std::max(units > 0 ? chip / units : 1, (S + 2047) / 2048);
     return chunk_for(shape->max_seq, 1, nc, 256, 64);
 }
 

@@ -120,11 +120,19 @@ template <class T, bool k8> __global__ __launch_bounds__(256) void kv_read_kerne
 // it; nothing of the cache passes through LDS.  The wavefronts' sums are joined at the end, those of chunks by the
 // workgroup that arrives last or by a launch of its own.
 // Memory bounds it, at 6.5 TB/s for rows in this order: 32 sequences of 4096 keys, 64/8 heads, 8 bits, take 44.9 us (6.05 TB/s), 16 of 512
-// .. 4096, 32 heads, 56.1 (6.1), 12 of 5000 .. 20001, 32/8 heads, 16 bits, 114.5 (5.3: 600 chunks in 512 places, and a join of 4.6).  One
-// sequence of 1024 keys takes 7.4: the launch, three round trips before the first keys, the hand-over.
+// .. 4096, 32 heads, 56.1 (6.1), 12 of 5000 .. 20001, 32/8 heads, 16 bits, 102.1 (5.95).  One sequence of 1024 keys takes 7.4: the
+// launch, three round trips before the first keys, the hand-over.
 constexpr int kBlock = 32;
 constexpr int kJoinWorkgroups = 512;             // of a launch that joins its rows itself
 constexpr int kJoinInPlace = 16;                 // chunks of a row that the launch itself can join
+// Launches of more chunks than this are cut by the sequences' own lengths instead, where there are 2 to 64 of them and no more than 512
+// groups: chunks of a number are many short ones where lengths differ, and a workgroup that begins while others run leaves its half of a
+// compute unit's loads idle for three round trips.  (us, in chunks of the best number and so: 12 x 32/8 heads x 5000 .. 20001 112.5 / 102.1,
+// 8 x 32/8 x 1000 .. 30000 112 / 83, 30 x 8/1 x 1000 .. 20000 37 / 31.8, 16 x 32/8 x 2000 .. 16000, 8 bits 69.5 / 54.6, 64 x 32/8 x 1000 ..
+// 16000 392 / 376; of one length 2 x 30000 41.0 / 41.6, 8 x 8000 42.9 / 44.1, 24 x 8192 124 / 132.)
+constexpr int kSharesFrom = 256;
+constexpr int kMostSequences = 64;               // a lane each
+constexpr int kMostShared = 1 << 26;             // max_seq (see pieces_of)
 struct DecodeLds {
     WaveSums sums;
     int last;
@@ -145,20 +153,69 @@ __device__ __forceinline__ int by_length(const KvProblem &p, int at, int per, in
     return (int)__builtin_ctzll(it) * per + at % per;
 }
 
+// ceil(n / by), n + by < 2^21: the quotient of n + by - 1/2 stays 1 / (2 by) away from whole numbers, which no rounding bridges.
+__device__ __forceinline__ int pieces_of(int n, int by, float inv_by) { return (int)(((float)(n + by) - 0.5f) * inv_by); }
+
+// Piece `at` of the sequences (of at most 64), which are cut into equal ones of as few keys, a multiple of 128 and at least p.C, as
+// leave no more than p.shares of them, two workgroups a compute unit; or half as many, one each, where those are no longer than kOne times
+// the others' two (1 and 1.05 measure the same; with 1.15 16 x 32/8 heads x 2000 .. 16000, 8 bits, take 58 us for 55).
+struct Piece {
+    int b, index, keys;                          // b < 0: there is none
+};
+__device__ __forceinline__ Piece find_piece(const KvProblem &p, int at, int lane)
+{
+    constexpr int kUnit = 128;
+    constexpr float kOne = 1.05f;
+    const int len = lane < p.B ? min(max(p.seq_lens[lane], 0), p.Smax) : 0, units = (len + kUnit - 1) / kUnit;
+    const int total = __builtin_amdgcn_readlane(lanes_scan(units), 63);
+    // Of n units at most n / k + 1 pieces of k: enough of most units each.  32 lengths from the least to that one in the lanes, for
+    // half as many pieces and for all.
+    const int room = lane < 32 ? p.shares >> 1 : p.shares;
+    const int least = max((p.C + kUnit - 1) / kUnit, (total + room - 1) / room);
+    const int most = max(least, (total + room - p.B - 1) / (room - p.B));
+    const int mine = least + ((most - least) * (lane & 31) + 30) / 31;
+    const float inv = 1.f / (float)mine;
+    int count = 0;
+    for (int b = 0; b < p.B; ++b) count += max(pieces_of(__builtin_amdgcn_readlane(units, b), mine, inv), 1);
+    const unsigned long long fits = __ballot(count <= room);
+    const int one = __builtin_ctz((unsigned)fits | 1u << 31), two = 32 + __builtin_ctz((unsigned)(fits >> 32) | 1u << 31);
+    const float ahead = 2.f * kOne * (float)__builtin_amdgcn_readlane(mine, two);
+    const int chosen = (float)__builtin_amdgcn_readlane(mine, one) <= ahead ? one : two;
+    const int size = __builtin_amdgcn_readlane(mine, chosen);
+    const float by = as_f32((unsigned)__builtin_amdgcn_readlane(__builtin_bit_cast(int, inv), chosen));
+    // (a sequence without keys has a piece too; as many, but equal ones)
+    const int pieces = lane < p.B ? max(pieces_of(units, size, by), 1) : 0, before = lanes_scan(pieces) - pieces;
+    const int keys = kUnit * max(pieces_of(units, max(pieces, 1), 1.f / (float)max(pieces, 1)), 1);
+    const unsigned long long it = __ballot(before <= at && at < before + pieces);
+    if (!it) return Piece{-1, 0, 0};
+    const int b = __builtin_ctzll(it);
+    return Piece{b, at - __builtin_amdgcn_readlane(before, b), __builtin_amdgcn_readlane(keys, b)};
+}
+
 template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_kernel(KvProblem p)
 {
     __shared__ DecodeLds lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     // The first chunk of every row, then the second: every XCD (index modulo 8) has as many of a chunk, which the short rows do not
     // have, as of another.
-    const int groups = gridDim.x / p.nc, chunk = blockIdx.x / groups, per = p.pool.Hkv * p.tiles;
-    int group = blockIdx.x % groups;
-    if (p.by_length) group = __builtin_amdgcn_readfirstlane(by_length(p, group, per, lane));
+    const int groups = p.B * p.pool.Hkv * p.tiles, per = p.pool.Hkv * p.tiles;
+    int group, chunk, keys = p.C;
+    if (p.shares) {
+        const Piece at = find_piece(p, blockIdx.x / per, lane);
+        if (at.b < 0) return;
+        group = at.b * per + blockIdx.x % per;
+        chunk = at.index;
+        keys = at.keys;
+    } else {
+        chunk = blockIdx.x / groups;
+        group = blockIdx.x % groups;
+        if (p.by_length) group = __builtin_amdgcn_readfirstlane(by_length(p, group, per, lane));
+    }
     int unit = group;
     const int tile = unit % p.tiles;
     unit /= p.tiles;
     const int hkv = unit % p.pool.Hkv, b = unit / p.pool.Hkv;
-    const int start = chunk * p.C;
+    const int start = chunk * keys;
     const int heads = min(p.G - 16 * tile, 16), head0 = hkv * p.G + 16 * tile;      // query heads of this tile
     // Everything that does not depend on the length is under way before it: the queries (which are first in the order of arrival, so that
     // no wait for them is one for keys) and the pages of the first block.
@@ -171,7 +228,7 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
     int key0 = start + kBlock * wave;
     BlockPages pages = block_pages(table, p.pool.page_shift, key0, p.Smax - 1);
     const int len = min(max(((scalar_i32)(uintptr_t)p.seq_lens)[b], 0), p.Smax);
-    const int end = min(len, start + p.C);
+    const int end = min(len, start + keys);
     if (start >= end) {
         // a sequence without keys: zero rows, by the first chunk (other chunks without keys leave nothing)
         if (chunk == 0)
@@ -184,7 +241,7 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
     walk_keys<T, k8, false>(p.pool, hkv, table, pages, key0, end, 0, q, p.scale * kLog2e, lane, state);
     lds.sums.put(state, wave, lane, heads);
     __syncthreads();
-    const int chunks = (len + p.C - 1) / p.C;                              // of this sequence
+    const int chunks = (len + keys - 1) / keys;                            // of this sequence
     for (int h = wave; h < heads; h += 4) {
         float a0, a1, top, sum;
         lds.sums.row(h, lane, a0, a1, top, sum);
@@ -219,24 +276,35 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_decode_
     if (!lds.last) return;
     for (int h = wave; h < heads; h += 4) {
         const size_t out_row = (size_t)b * p.Hq + head0 + h, slot = out_row * p.nc;
-        // chunk i's reference and denominator in lane i of every 16; all partial vectors under way before the first is used
-        unsigned long long x[kJoinInPlace];
-        const unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + min(n, chunks - 1)));
+        // 16 chunks at a time, chunk i's reference and denominator in lane i of every 16; all their partial vectors under way before
+        // the first is used
+        float top = -INFINITY, a0 = 0.f, a1 = 0.f, sum = 0.f;
+        for (int w0 = 0; w0 < chunks; w0 += kJoinInPlace) {
+            const int count = min(chunks - w0, kJoinInPlace);
+            unsigned long long x[kJoinInPlace];
+            const unsigned long long s = load_coherent(reinterpret_cast<const unsigned long long *>(p.ml + slot + w0 + min(n, count - 1)));
 #pragma unroll
-        for (int i = 0; i < kJoinInPlace; ++i)
-            x[i] = load_coherent(reinterpret_cast<const unsigned long long *>(p.num + (slot + min(i, chunks - 1)) * kHeadDim) + lane);
-        const float mi = n < chunks ? as_f32((unsigned)s) : -INFINITY, top = row16_max(mi);
-        const float f = n >= chunks ? 0.f : mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
-        const float sum = row16_sum(n < chunks ? as_f32((unsigned)(s >> 32)) * f : 0.f);
-        float a0 = 0.f, a1 = 0.f;
-        each16(std::make_integer_sequence<int, kJoinInPlace>{}, [&](auto of) {
-            constexpr int i = decltype(of)::value;
-            if (i < chunks) {
-                const float fi = row16_lane<i>(f);
-                a0 = __builtin_fmaf(as_f32((unsigned)x[i]), fi, a0);
-                a1 = __builtin_fmaf(as_f32((unsigned)(x[i] >> 32)), fi, a1);
+            for (int i = 0; i < kJoinInPlace; ++i)
+                x[i] = load_coherent(reinterpret_cast<const unsigned long long *>(p.num + (slot + w0 + min(i, count - 1)) * kHeadDim) + lane);
+            const float mi = n < count ? as_f32((unsigned)s) : -INFINITY, most = row16_max(mi);
+            if (most > top) {                                  // (uniform) what the chunks before left, to the new reference
+                const float by = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - most);
+                a0 *= by;
+                a1 *= by;
+                sum *= by;
+                top = most;
             }
-        });
+            const float f = n >= count ? 0.f : mi == top ? 1.f : __builtin_amdgcn_exp2f(mi - top);
+            sum += row16_sum(n < count ? as_f32((unsigned)(s >> 32)) * f : 0.f);
+            each16(std::make_integer_sequence<int, kJoinInPlace>{}, [&](auto of) {
+                constexpr int i = decltype(of)::value;
+                if (i < count) {
+                    const float fi = row16_lane<i>(f);
+                    a0 = __builtin_fmaf(as_f32((unsigned)x[i]), fi, a0);
+                    a1 = __builtin_fmaf(as_f32((unsigned)(x[i] >> 32)), fi, a1);
+                }
+            });
+        }
         const float inv = 1.f / sum;
         reinterpret_cast<unsigned *>(p.out + out_row * kHeadDim)[lane] = T::pack(a0 * inv, a1 * inv);
     }
@@ -268,9 +336,16 @@ hipError_t launch_kv_read(const KvPool &pool, const TokenRows &rows, hipStream_t
 hipError_t launch_kv_decode(const KvProblem &p_, hipStream_t s)
 {
     KvProblem p = p_;
-    const long long workgroups = (long long)p.B * p.pool.Hkv * p.tiles * p.nc;
-    if (p.nc > kJoinInPlace || workgroups > kJoinWorkgroups) p.counters = nullptr;
-    p.by_length = p.nc == 1 && p.B > 1 && p.B <= 64 && workgroups > kComputeUnits;
+    const long long per = (long long)p.pool.Hkv * p.tiles, groups = p.B * per;
+    long long workgroups = groups * p.nc;
+    if (p.nc > 1 && workgroups > kSharesFrom && p.B > 1 && p.B <= kMostSequences && groups <= kJoinWorkgroups && p.Smax <= kMostShared) {
+        // a round of two workgroups a compute unit, or as many rounds as give a sequence four pieces
+        p.shares = (int)((4 * groups + kJoinWorkgroups - 1) / kJoinWorkgroups * kJoinWorkgroups / per);
+        workgroups = p.shares * per;
+    } else if (p.nc > kJoinInPlace || workgroups > kJoinWorkgroups) {
+        p.counters = nullptr;
+    }
+    p.by_length = p.nc == 1 && p.B > 1 && p.B <= kMostSequences && workgroups > kComputeUnits;
     const hipError_t e = by_type(p.pool, [&](auto type, auto k8) {
         return launch(kv_decode_kernel<decltype(type), decltype(k8)::value>, dim3((unsigned)workgroups), dim3(256), s, p);
     });

@@ -204,3 +204,67 @@ def test_agrees_with_the_calibrated_call_over_its_pool():
                             synth.PHI, synth.BOUNDS, other.data_ptr(), ws.data_ptr(), ws.numel(), stream)
     check_all(got, pool, lens, q, k, v)
     check_all(other, pool, lens, q, k, v)
+
+
+@TYPED
+@BOTH
+@pytest.mark.parametrize("hq,hkv,chunk,lens", [
+    (1, 1, 64, [40000, 33000]),                                         # hundreds of pieces of a row, joined 16 at a time
+    (4, 2, 64, [128 * 129, 1, 0, 128 * 64 + 1, 127]),
+    (20, 1, 128, [20000, 0, 0, 19999, 5000]),                           # two tiles of heads
+    (12, 12, 64, [0] * 12), (8, 8, 64, [3000] * 8),
+    (3, 3, 512, [9000, 100, 4000, 8999, 1, 777, 0, 6000, 5, 4321, 8192, 2048]),
+    (8, 8, 192, [100 + 37 * i for i in range(64)]),                     # four rounds of the chip
+])
+def test_pieces_by_the_lengths(dtype, coded, hq, hkv, chunk, lens):
+    """Launches of more than 256 chunks.  The largest logits of every row at its end."""
+    def change(b, which, x):
+        if which == 0:
+            x = x * 0.05
+            x[:, -150:-90] = 2.0
+        return x
+    width = -(-max(max(lens), 64 * 40) // 64) + 1
+    assert len(lens) * hkv * -(-hq // hkv // 16) * -(-width * 64 // chunk) > 256
+    pool, table, k, v = filled(dtype, coded, hkv, 64, lens, 53, width, 1.0, change)
+    q = queries(len(lens), hq, dtype)
+    q[:, ::2] = 1.0
+    table, dlens = device(lens, table)
+    fd = lib()
+    shape = fd.make_shape(len(lens), hq, hkv, 128, width * 64, chunk, 0.05)
+    ws = workspace(fd.fd_kv_workspace_bytes(shape))
+    got = decode(pool, table, dlens, q, chunk, width * 64, 0.05, ws)
+    some = [b for b in range(len(lens)) if b < 12 or b > len(lens) - 3]
+    out, qc, share = got.cpu(), q.cpu(), hq // hkv
+    for b in range(len(lens)):
+        assert (out[b] == 0).all() if lens[b] == 0 else not out[b].isnan().any()
+        for h in range(hkv) if b in some and lens[b] else ():
+            check(out[b, h * share:(h + 1) * share], dtype, 2, qc[b, h * share:(h + 1) * share], k[b][h], v[b][h], 0.05, what="sequence %d, KV head %d" % (b, h))
+    assert (ws[:1 << 14] == 0).all()
+    for _ in range(3):
+        assert torch.equal(decode(pool, table, dlens, q, chunk, width * 64, 0.05, ws), got)
+    assert (ws[:1 << 14] == 0).all()
+
+
+@BOTH
+def test_pieces_follow_the_lengths_of_a_replay(coded):
+    """A captured call, replayed with other lengths: other pieces, other joins."""
+    dtype, lens = torch.bfloat16, [9000, 200, 4097, 1, 6000, 33]
+    pool, table, k, v = filled(dtype, coded, 2, 64, lens, 59, 141)
+    q = queries(len(lens), 8, dtype)
+    table, dlens = device(lens, table)
+    fd = lib()
+    shape = fd.make_shape(len(lens), 8, 2, 128, 141 * 64, 256, SCALE)
+    ws = workspace(fd.fd_kv_workspace_bytes(shape))
+    out = torch.full_like(q, float("nan"))
+    graph = torch.cuda.CUDAGraph()
+    decode(pool, table, dlens, q, 256, 141 * 64, SCALE, ws, out)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        decode(pool, table, dlens, q, 256, 141 * 64, SCALE, ws, out)
+    for now in ([9000, 200, 4097, 1, 6000, 33], [1, 0, 4000, 1, 128, 32], [0] * 6, [8999, 200, 1, 1, 5999, 33], [9000, 200, 4097, 1, 6000, 33]):
+        dlens.copy_(torch.tensor(now, dtype=torch.int32))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_all(out, pool, now, q, [x[:, :n] for x, n in zip(k, now)], [x[:, :n] for x, n in zip(v, now)])
+        assert torch.equal(out, decode(pool, table, dlens, q, 256, 141 * 64, SCALE))
