@@ -302,18 +302,17 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
             byte_v = __builtin_amdgcn_raw_buffer_load_b8(buffer(p.pool.v_scales + place, n), lane >> 3, 0, 0);
         }
     };
+    auto put = [&](unsigned at, const int (&off)[2], u32x4_t codes, unsigned byte) {
+        const float by = scale_of(byte);
+        *(lds_u32x4)(uintptr_t)(at + off[0]) = from_codes<T>(codes[0], codes[1], by);
+        *(lds_u32x4)(uintptr_t)(at + off[1]) = from_codes<T>(codes[2], codes[3], by);
+    };
     auto put_k = [&] {
-        const unsigned at = lds_k + k_to * kStepBytes;
-        const float by = scale_of(byte_k);
-        *(lds_u32x4)(uintptr_t)(at + koff[0]) = from_codes<T>(codes_k[0], codes_k[1], by);
-        *(lds_u32x4)(uintptr_t)(at + koff[1]) = from_codes<T>(codes_k[2], codes_k[3], by);
+        put(lds_k + k_to * kStepBytes, koff, codes_k, byte_k);
         next_k();
     };
     auto put_v = [&] {
-        const unsigned at = lds_v + v_to * kStepBytes;
-        const float by = scale_of(byte_v);
-        *(lds_u32x4)(uintptr_t)(at + voff[0]) = from_codes<T>(codes_v[0], codes_v[1], by);
-        *(lds_u32x4)(uintptr_t)(at + voff[1]) = from_codes<T>(codes_v[2], codes_v[3], by);
+        put(lds_v + v_to * kStepBytes, voff, codes_v, byte_v);
         next_v();
     };
     // Entering step s, K of s + 2 and V of s are in LDS.  16 bits: the step fetches K of s + 4 and V of s + 2, whose places were
@@ -331,17 +330,36 @@ template <class T, bool k8> __global__ __launch_bounds__(256, 2) void kv_prefill
         asm volatile("" ::"s"(entries[0]), "s"(entries[1]), "s"(entries[2]), "s"(entries[3]), "s"(entries[4]), "s"(entries[4 + kAhead]));
 #pragma unroll
         for (int i = 0; i < 4 + kAhead; ++i) first[i] = row_place(entries[i], i);
+        if constexpr (!k8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            fetch_k(first[i], rows_of(i));
-            if constexpr (k8) put_k();
-            if (i < 2) continue;
-            fetch_v(first[i - 2], rows_of(i - 2));
-            if constexpr (k8) put_v();
-        }
-        if constexpr (k8) {
+            for (int i = 0; i < 4; ++i) {
+                fetch_k(first[i], rows_of(i));
+                if (i >= 2) fetch_v(first[i - 2], rows_of(i - 2));
+            }
+        } else {
+            // (all of them under way before the first is put in its place)
+            u32x4_t k[4], v[2];
+            unsigned kb[4], vb[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fetch_k(first[i], rows_of(i));
+                k[i] = codes_k;
+                kb[i] = byte_k;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fetch_v(first[i], rows_of(i));
+                v[i] = codes_v;
+                vb[i] = byte_v;
+            }
             fetch_k(first[4], rows_of(4));
             fetch_v(first[2], rows_of(2));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put(lds_k + i * kStepBytes, koff, k[i], kb[i]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) put(lds_v + i * kStepBytes, voff, v[i], vb[i]);
+            v_to = 2;                                          // (and k_to 0 again)
         }
         place[0] = first[2 + kAhead];
         place[1] = first[3 + kAhead];
