@@ -463,8 +463,11 @@ int32_t fd_kv_pick_chunk(const fd_shape *shape)
     // 16.3 / *15.7 / 23 / 37, 4 x 64/8 x 2000, 8 bits *9.5 / 11.2 / 14.6 / 15.5.)
     const long long S = shape->max_seq, chip = fd::kComputeUnits;
     if (units >= chip && S <= 4096) return chunk_for(shape->max_seq, 1, 1, 256, 64);
-    if (shape->batch > 1 && shape->batch <= 64 && units <= 2 * chip && units * ((S + 511) / 512) > chip)   // (128 chunks a row at most)
-        return (int32_t)std::min<long long>(std::max<long long>(512, (S / 128 + 63) / 64 * 64), 16384);
+    if (shape->batch > 1 && shape->batch <= 64 && units <= 2 * chip && units * ((S + 511) / 512) > chip) {
+        // (at most 128 chunks a row, and their sums, 520 bytes for each head, 128 MiB)
+        const long long slots = (128ll << 20) / (520ll * shape->batch * shape->n_q_heads), nc = std::max(std::min(slots, 128ll), 1ll);
+        return (int32_t)std::min<long long>(std::max<long long>(512, ((S + nc - 1) / nc + 63) / 64 * 64), 16384);
+    }
     const long long nc = std::max(units > 0 ? chip / units : 1, (S + 2047) / 2048);
     return chunk_for(shape->max_seq, 1, nc, 256, 64);
 }

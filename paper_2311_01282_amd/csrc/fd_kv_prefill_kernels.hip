@@ -16,9 +16,11 @@
 // in long calls the power that they draw: one prompt of 8001 tokens, 32/8 heads, bf16, takes 506 us (1.04 PFLOP/s), with queries
 // and keys of zeros 399 (1.31).  So products of 32 x 32, whose operands serve twice as many rows or keys as those of 16 x 16 (a wavefront
 // reads 16 KiB of LDS for 0.5 MFLOP), rows in lanes, so that a softmax needs one exchange, of two lanes, and two workgroups a compute
-// unit, one with products while the other has exponentials.  A step takes 1.05 us (both), one workgroup alone 0.62.  Outside its loop a workgroup takes 8 us: 2 until
-// it knows its sequence, 3 to 4 until the page table, the first rows and the queries have arrived one after the other, 2 for the
-// output; five prompts of 150 to 2000 tokens, 32 heads, fp16, take 105 us for 51 of products.
+// unit, one with products while the other has exponentials.  A step takes 1.05 us (both), one workgroup alone 0.62.  Outside its loop a
+// workgroup takes 8 us: 2 until it knows its sequence, 3 to 4 until the page table, the first rows and the queries have arrived one
+// after the other, 2 for the output; five prompts of 150 to 2000 tokens, 32 heads, fp16, take 103 us for 51 of products.
+// Rows of 8 bits are converted once a workgroup, a vector instruction an element: 700 .. 3000 tokens over up to 1500, 32/4 heads, bf16, take
+// 244 us (0.90 PFLOP/s), 512 over 30000, 64/8, fp16, 533 (0.95).
 #include <utility>
 
 #include "fd_kv.h"

@@ -122,6 +122,8 @@ def test_picked_chunks_are_taken(batch, hq, hkv, max_seq):
     shape.chunk = fd.fd_kv_pick_chunk(shape)
     assert shape.chunk % 64 == 0 and 64 <= shape.chunk <= 16384
     assert fd.fd_kv_workspace_bytes(shape) > 0 or batch * hq * -(-max_seq // shape.chunk) > 1 << 23
+    if batch <= 64 and max_seq <= 32768:
+        assert fd.fd_kv_workspace_bytes(shape) <= 1 << 28
     for tokens in (0, 1, batch, 1000, 100000):
         shape.chunk = fd.fd_kv_prefill_pick_chunk(shape, tokens)
         assert 1 <= shape.chunk <= max_seq
