@@ -513,23 +513,38 @@ int32_t fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens)
     if (shape->batch == 0 || n_tokens == 0) return shape->max_seq;
     const long long B = shape->batch, Hkv = shape->n_kv_heads, S = shape->max_seq;
     const long long tiles = (long long)n_tokens * (shape->n_q_heads / shape->n_kv_heads) / 128, whole = std::max(tiles, std::min<long long>(B, n_tokens));
-    // Two workgroups fit a compute unit, and take 1.05 us for a step of 32 keys each that one alone takes 0.62 for.  Launches that leave
-    // compute units without a unit, or with one only, are cut so that they have about 512, in pieces of 768 keys at least: the sums of
-    // pieces, 520 bytes a row written and read again, and their join cost what shorter ones save.
-    // (Uncut / as picked here / in twice as many pieces, us: 512 tokens over 30000, 64/8 heads, 8 bits 625 / 535 / 540, 256 over 30000, 32/8
-    // 499 / 143 / 157, 100 over 8000, 64/8 138 / 60 / 78, 8 x 64 over 2000 .. 4000, 32/8 72 / 53 / 67, 16 single tokens over 2000 .. 3800, 32/8
-    // 63 / 49 / 54, 4000 of 8 heads that share one 72 / 66 / -; of more units: 1600 over 3000, 32/8 113 / 113 / 124.)
-    // Sequences of few rows are bound by memory and cut as for fd_kv_decode_attn; where there are as many units without that, only
-    // walks that would outlast the others are.
     const bool single = tiles < B;
-    if (S <= 1024) return shape->max_seq;
-    long long chunk;
-    if (whole * Hkv >= fd::kComputeUnits * 5 / 4) {
-        chunk = S <= (single ? 4096 : 8192) ? S : single ? 2048 : 4096;
+    long long chunk = S;
+    if (single || whole * Hkv >= 2 * fd::kComputeUnits) {
+        // Sequences of few rows are bound by memory and cut into one workgroup a compute unit, of 768 keys at least; where there are as
+        // many units without that, only walks that would outlast the others are cut.
+        if (whole * Hkv >= fd::kComputeUnits * 5 / 4)
+            chunk = S <= (single ? 4096 : 8192) ? S : single ? 2048 : 4096;
+        else if (S > 1024)
+            chunk = std::min<long long>(std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), 768ll), 2048);
     } else {
+        // Prompts, us in n pieces.  A step of 32 keys takes 0.62 alone on a compute unit and 1.05 beside another workgroup, of which longer
+        // units have less the shorter the others are; sums of pieces, 520 bytes a row, are written and read again, by a launch more.
+        // (Uncut / as picked / in the pieces that measured best: 512 tokens over 30000, 64/8 heads, 8 bits 645 / 533 / 533, 256 over 30000,
+        // 32/8 533 / 141 / 141, 100 over 8000, 64/8 147 / 52 / 48, 8 x 64 over 2000 .. 4000, 32/8 76 / 53 / 52, 64 over 1000, 32/8 25 / 19 / 19,
+        // 4000 of 8 heads that share one 77 / 58 / 58, 5000 of 4 heads 93 / 49 / 49; not cut: 1200, 32/8 29, in two 33, 1600 over 3000 109, in
+        // two 128.)
+        const double chip = fd::kComputeUnits, W = (double)(whole * Hkv), steps = S / 32.0, rows = (double)n_tokens * shape->n_q_heads;
+        const double f = 1.0 - std::fmin((double)n_tokens / (double)(2 * B * S), 0.5);      // keys of a row on the average, of S
+        double least = 0.0;
+        long long pieces = 1;
+        for (long long n = 1; n <= 64; ++n) {
+            const double some = f + (1.0 - f) / n, units = W * n * some, even = f / some;   // units with keys; their mean length, of the longest
+            const double pair = 0.62 + 0.43 * std::fmax(2.0 * even - 1.0, 0.0), rounds = units / (2.0 * chip);
+            double t = steps / n * (units <= chip ? 0.62 : rounds <= 1.0 ? pair : 0.525 * (2.0 * rounds + 1.0));
+            if (n > 1) t += 5.0 + 8.0 * std::fmax(rounds - 1.0, 0.0) + units * rows / W * 1040.0 / 5e6;
+            if (n == 1 || t < least) {
+                least = t;
+                pieces = n;
+            }
+        }
         const long long each = std::max<long long>(tiles / B, 1);
-        chunk = std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), (768 + each - 1) / each);
-        if (single) chunk = std::min<long long>(chunk, 2048);
+        if (pieces > 1) chunk = (S + pieces * each - 1) / (pieces * each);
     }
     // ... and no workspace of more than 256 MiB
     fd_shape cut = *shape;
