@@ -515,28 +515,30 @@ int32_t fd_kv_prefill_pick_chunk(const fd_shape *shape, int32_t n_tokens)
     const long long tiles = (long long)n_tokens * (shape->n_q_heads / shape->n_kv_heads) / 128, whole = std::max(tiles, std::min<long long>(B, n_tokens));
     const bool single = tiles < B;
     long long chunk = S;
-    if (single || whole * Hkv >= 2 * fd::kComputeUnits) {
+    if (single) {
         // Sequences of few rows are bound by memory and cut into one workgroup a compute unit, of 768 keys at least; where there are as
         // many units without that, only walks that would outlast the others are cut.
         if (whole * Hkv >= fd::kComputeUnits * 5 / 4)
-            chunk = S <= (single ? 4096 : 8192) ? S : single ? 2048 : 4096;
+            chunk = S <= 4096 ? S : 2048;
         else if (S > 1024)
-            chunk = std::min<long long>(std::max((B * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), 768ll), 2048);
+            chunk = std::min<long long>(std::max((whole * Hkv * S + 2 * fd::kComputeUnits - 1) / (2 * fd::kComputeUnits), 768ll), 2048);
     } else {
         // Prompts, us in n pieces.  A step of 32 keys takes 0.62 alone on a compute unit and 1.05 beside another workgroup, of which longer
         // units have less the shorter the others are; sums of pieces, 520 bytes a row, are written and read again, by a launch more.
         // (Uncut / as picked / in the pieces that measured best: 512 tokens over 30000, 64/8 heads, 8 bits 645 / 533 / 533, 256 over 30000,
         // 32/8 533 / 141 / 141, 100 over 8000, 64/8 147 / 52 / 48, 8 x 64 over 2000 .. 4000, 32/8 76 / 53 / 52, 64 over 1000, 32/8 25 / 19 / 19,
-        // 4000 of 8 heads that share one 77 / 58 / 58, 5000 of 4 heads 93 / 49 / 49; not cut: 1200, 32/8 29, in two 33, 1600 over 3000 109, in
-        // two 128.)
+        // 4000 of 8 heads that share one 77 / 58 / 58, 5000 of 4 heads 93 / 49 / 49, 2500 over 20000, 32/8 1005 / 905 / 896; not cut: 1200, 32/8
+        // 29, in two 33, 1600 over 3000 109, in two 128, 16000 2039, in two 2145.)
         const double chip = fd::kComputeUnits, W = (double)(whole * Hkv), steps = S / 32.0, rows = (double)n_tokens * shape->n_q_heads;
         const double f = 1.0 - std::fmin((double)n_tokens / (double)(2 * B * S), 0.5);      // keys of a row on the average, of S
         double least = 0.0;
         long long pieces = 1;
         for (long long n = 1; n <= 64; ++n) {
             const double some = f + (1.0 - f) / n, units = W * n * some, even = f / some;   // units with keys; their mean length, of the longest
-            const double pair = 0.62 + 0.43 * std::fmax(2.0 * even - 1.0, 0.0), rounds = units / (2.0 * chip);
-            double t = steps / n * (units <= chip ? 0.62 : rounds <= 1.0 ? pair : 0.525 * (2.0 * rounds + 1.0));
+            // (half-full last rounds cost the more the more alike the units are: 0 where they go down to nothing)
+            const double alike = std::fmax(2.0 * even - 1.0, 0.0), rounds = units / (2.0 * chip);
+            const double step = units <= chip ? 0.62 : rounds <= 1.0 ? 0.62 + 0.43 * alike : std::fmax(0.525 * (2.0 * rounds * even + alike), 0.62);
+            double t = steps / n * step;
             if (n > 1) t += 5.0 + 8.0 * std::fmax(rounds - 1.0, 0.0) + units * rows / W * 1040.0 / 5e6;
             if (n == 1 || t < least) {
                 least = t;
