@@ -179,8 +179,9 @@ template <class T> struct Softmax {
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    // z: this lane's eight logits, in units of log2; odd: there may be values in `a` that are not finite
-    __device__ __forceinline__ void block(float (&z)[8], u32x4_t (&a)[8], bool odd)
+    // A block's two steps; z: this lane's eight logits, in units of log2.  The reference first: it multiplies the sums, by 0 where they had
+    // none, and a summand of infinity has to come after that.
+    __device__ __forceinline__ void refer(const float (&z)[8])
     {
         float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
         top = columns_max(top) - T::kLift;
@@ -191,6 +192,10 @@ template <class T> struct Softmax {
             for (int dt = 0; dt < 8; ++dt) acc[dt] *= f;
             ref = to;
         }
+    }
+    // odd: there may be values in `a` that are not finite
+    __device__ __forceinline__ void weigh(const float (&z)[8], u32x4_t (&a)[8], bool odd)
+    {
         const float from = ref == -INFINITY ? 0.f : ref;
         u32x4_t hi, lo;                                        // the weights as the sum of two numbers of the type
 #pragma unroll
@@ -264,6 +269,7 @@ __device__ __forceinline__ void walk_keys(const KvPool &pool, int hkv, scalar_i3
         }
         // (no code of 8 bits is infinite, and NaN stay what they are)
         const bool odd = (!k8 || (kMasks && kTail)) && any_not_finite<T>(a);
+        state.refer(z);
         if constexpr (kMasks && kTail)
             if (odd) {
                 // keys behind a row have the weight 0: what they hold must not reach it, be it infinite
@@ -278,7 +284,7 @@ __device__ __forceinline__ void walk_keys(const KvPool &pool, int hkv, scalar_i3
                     a[dt] = finite<T>(a[dt]);
                 }
             }
-        state.block(z, a, odd);
+        state.weigh(z, a, odd);
     };
     const std::true_type yes;
     const std::false_type no;
