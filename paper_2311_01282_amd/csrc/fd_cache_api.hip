@@ -469,7 +469,11 @@ int32_t fd_kv_pick_chunk(const fd_shape *shape)
         return (int32_t)std::min<long long>(std::max<long long>(512, ((S + nc - 1) / nc + 63) / 64 * 64), 16384);
     }
     const long long nc = std::max(units > 0 ? chip / units : 1, (S + 2047) / 2048);
-    return chunk_for(shape->max_seq, 1, nc, 256, 64);
+    int32_t chunk = chunk_for(shape->max_seq, 1, nc, 256, 64);
+    // (longer where there would be more of them than a launch may have)
+    const long long rows = (long long)shape->batch * shape->n_q_heads;
+    while (chunk < 16384 && rows * ((S + chunk - 1) / chunk) > kMostThreads / 512) chunk = std::min(2 * chunk, 16384);
+    return chunk;
 }
 
 fd_status fd_kv_decode_attn(const fd_shape *shape, const fd_kv_pool *pool, const void *q, const int32_t *block_table, const int32_t *seq_lens,
