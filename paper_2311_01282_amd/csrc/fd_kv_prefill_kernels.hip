@@ -143,10 +143,10 @@ __device__ __forceinline__ Sequence load_sequences(const KvPromptProblem &p, int
     const unsigned most = (unsigned)(p.Smax + 63) & ~63u;
     x.piece = (int)most;
     x.units = x.tiles;
-    if (p.C < p.Smax && x.len > 0) {             // in pieces of one length, as many as those of p.C t keys
+    if (p.C < p.Smax && x.len > 0 && x.tiles > 0) {        // in pieces of one length, as many as those of p.C t keys (64 or more)
         const int piece = (int)min(__umulhi((unsigned)p.C, (unsigned)x.tiles) ? most : min((unsigned)p.C * (unsigned)x.tiles, most) + 63, most) & ~63;
-        const int n = (x.len + piece - 1) / max(piece, 64);
-        x.piece = ((x.len + n - 1) / max(n, 1) + 63) & ~63;
+        const int n = (x.len + piece - 1) / piece;
+        x.piece = ((x.len + n - 1) / n + 63) & ~63;
         x.units = x.tiles * ((x.len + x.piece - 1) / x.piece);
     }
     x.before = before + lanes_scan(x.units) - x.units;
