@@ -644,8 +644,9 @@ fd_status fd_kv_read(const fd_kv_pool *pool, const int32_t *slot_map, int32_t n_
  * of 64 from 64 to 16384 keys, for example fd_kv_pick_chunk(shape).  Query heads that share a KV head read it once (16 at a time).
  * Scores and sums in fp32; the weights enter the second product as two numbers of dtype each.  A sequence of length 0 gives zero
  * rows.  With groups = batch * n_kv_heads * ceil(n_q_heads / n_kv_heads / 16) and n = ceil(max_seq / chunk): of 2 to 64 sequences with n > 1,
- * groups * n > 256 and groups <= 512 (and max_seq <= 2^26) the keys are cut into equal pieces by the sequences' lengths, of a chunk at
- * least, in one launch; otherwise into chunks, in one launch for n <= 16 and groups * n <= 512, else two.
+ * groups * n > 256 and groups <= 512 (and max_seq <= 2^26) the keys are cut by the sequences' lengths, in one launch: each sequence into
+ * equal pieces, multiples of 128 keys, at most ceil(length / chunk) of them (they may be shorter than a chunk: 640 keys with chunks of 512 make
+ * 384 and 256); otherwise into chunks, in one launch for n <= 16 and groups * n <= 512, else two.
  */
 size_t    fd_kv_workspace_bytes(const fd_shape *shape);
 int32_t   fd_kv_pick_chunk(const fd_shape *shape);

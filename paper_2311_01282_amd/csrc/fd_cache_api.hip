@@ -455,8 +455,8 @@ int32_t fd_kv_pick_chunk(const fd_shape *shape)
     const long long units = (long long)shape->batch * shape->n_kv_heads * ((shape->n_q_heads / shape->n_kv_heads + 15) / 16);
     // A workgroup draws what its compute unit can take (four wavefronts, a block each under way), and costs three round trips to memory
     // before its first keys arrive.  So whole rows, which the launch sorts by length, where they fill the chip and are short enough not to
-    // outlast the others; where chunks of 512 keys would fill it more than once and the launch makes pieces by the sequences' lengths, of
-    // a chunk at least, those; otherwise one workgroup a compute unit, in chunks of 256 keys at least and 2048 at most.
+    // outlast the others; where chunks of 512 keys would fill it more than once and the launch makes pieces by the sequences' lengths, no
+    // more of a sequence than it has chunks, those; otherwise one workgroup a compute unit, in chunks of 256 keys at least and 2048 at most.
     // (Whole call, us, chunks of 256 / 512 / 1024 / 2048 / 4096 keys, the choice marked: 32 x 64/8 heads x 4096, 8 bits 51 / 51 / 51 / 51 /
     // *44, 16 x 32 x 512 .. 4096, 8 bits 65 / 65 / 65 / 70 / *56, 64 x 32/8 x 500 .. 4000, 16 bits 115 / 112 / 111 / 109 / *93, 12 x 32/8 x
     // 5000 .. 20001, 16 bits 103 / *102 / 102 / 102 / 105, 4 x 32/8 x 1000 .. 30000, 16 bits 33 / *33 / 33 / 38 / 64, 1 x 32 x 8192, 8 bits 19 /

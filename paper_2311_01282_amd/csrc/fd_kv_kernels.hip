@@ -156,9 +156,11 @@ __device__ __forceinline__ int by_length(const KvProblem &p, int at, int per, in
 // ceil(n / by), n + by < 2^21: the quotient of n + by - 1/2 stays 1 / (2 by) away from whole numbers, which no rounding bridges.
 __device__ __forceinline__ int pieces_of(int n, int by, float inv_by) { return (int)(((float)(n + by) - 0.5f) * inv_by); }
 
-// Piece `at` of the sequences (of at most 64), which are cut into equal ones of as few keys, a multiple of 128 and at least p.C, as
-// leave no more than p.shares of them, two workgroups a compute unit; or half as many, one each, where those are no longer than kOne times
-// the others' two (1 and 1.05 measure the same; with 1.15 16 x 32/8 heads x 2000 .. 16000, 8 bits, take 58 us for 55).
+// Piece `at` of the sequences (of at most 64).  A piece's most keys are as few, a multiple of 128 and at least p.C, as leave no more than
+// p.shares pieces, two workgroups a compute unit; or half as many, one each, where those are no longer than kOne times the others' two (1
+// and 1.05 measure the same; with 1.15 16 x 32/8 heads x 2000 .. 16000, 8 bits, take 58 us for 55).  Each sequence is then cut into equal ones,
+// which may be shorter than p.C; as many as with the most keys each, so that their number is ceil(length / p.C) at most, and their
+// indexes stay below p.nc, the places that a row has for its sums.
 struct Piece {
     int b, index, keys;                          // b < 0: there is none
 };
