@@ -70,7 +70,9 @@ template <int NW, int DS, int TPW> struct LatentLds {
 __device__ __forceinline__ constexpr int c_key(int r) { return ((r & 1) << 1) | (((r >> 1) & 1) << 2) | (((r >> 3) & 1) << 3); }
 __device__ __forceinline__ constexpr int r_key(int r) { return (((r >> 3) & 1) << 1) | (((r >> 1) & 1) << 2); }
 
-// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+// (In assembly: of loads into LDS that the compiler knows it would wait before every transposing read.  That the window's scalar
+// registers have settled, five states behind a vector instruction, is as the code around it comes out; tests/test_wait_states_host.py
+// follows them through the assembly.)
 __device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, int soff, unsigned lds_1k)
 {
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs), "s"(soff) : "memory");

@@ -48,7 +48,9 @@ __device__ __forceinline__ unsigned lds_address(const void *p)
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t *lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4_t *lds_u32x4;
-// (in assembly: of loads into LDS that the compiler knows it would wait before every transposing read)
+// (In assembly: of loads into LDS that the compiler knows it would wait before every transposing read.  That the window's scalar
+// registers have settled, five states behind a vector instruction, is as the code around it comes out; tests/test_wait_states_host.py
+// follows them through the assembly.)
 __device__ __forceinline__ void load_to_lds(u32x4_t rs, int voff, int soff, unsigned lds_1k)
 {
     asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(lds_1k), "v"(voff), "s"(rs), "s"(soff) : "memory");

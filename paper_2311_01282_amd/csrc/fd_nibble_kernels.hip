@@ -237,6 +237,7 @@ template <int R> struct NibbleLds {
 // Loads into LDS, 1 KiB at lds_1k.  In assembly: of those that the compiler knows it would wait before every transposing
 // read.  They are older than the loads of K's codes of the same step, and loads arrive in order: once K's codes are there,
 // so are they.
+// (That the scalar registers of an address have settled: tests/test_wait_states_host.py.)
 __device__ __forceinline__ void load_to_lds(const unsigned char *base, int voff, unsigned lds_1k)
 {
     const unsigned long long at = reinterpret_cast<unsigned long long>(base);
