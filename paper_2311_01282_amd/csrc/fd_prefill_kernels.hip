@@ -162,7 +162,8 @@ struct TileWave {
     // In assembly, because the compiler waits for the loads it knows to write LDS before every transposing LDS read
     // (a step then takes 1120 cycles instead of 920); no register is written -- the LDS address goes into m0 as an operand, so that
     // the compiler knows what m0 holds -- and the waits are wait_fetches.  KNOWN: the builtin, for the prologue, whose loads the
-    // compiler has to tell from those of Q^T; all_landed tells it that they are there.
+    // compiler has to tell from those of Q^T; all_landed tells it that they are there.  (That the scalar registers of a window have
+    // settled: tests/test_wait_states_host.py.)
     template <bool KNOWN> static __device__ __forceinline__ void load(u32x4 rs, int voff, int soff, unsigned char *lds_1k)
     {
         auto *to = (__attribute__((address_space(3))) unsigned char *)lds_1k;
